@@ -429,6 +429,98 @@ int sw_selective_scan_bwd_ex(const void* x, const void* delta, const float* A, c
 int64_t sw_selective_scan_bwd_workspace(int64_t B, int64_t D, int64_t N, int64_t L, int ckpt,
                                         int z, int s_pre);
 
+/*
+ * Linear attention with a log decay for each head: the affine recurrence with a
+ * K x V matrix as each head's state,
+ *
+ *   S_t = e^{g_t} S_{t-1} + k_t v_t^T        (Eq. (3) with a_t = e^{g_t})
+ *   o_t = scale * S_t^T q_t
+ *   h_last = the state after the last step; S_{-1} = h0, or zero
+ *
+ *   q, k : (B, L, Hk, K) of dtype      v : (B, L, H, V) of dtype
+ *   g    : (B, L, H) fp32 log decays, or, with SW_LINEAR_G_HEAD, (H) fp32, one
+ *          for all of a head's steps.  g <= 0 decays; any value is taken, and
+ *          e^g is zero for g < -10000, -inf included.
+ *   o    : (B, L, H, V) of dtype, dense
+ *   h0, h_last : (nseq, H, K, V) fp32, dense, or NULL
+ * H is a multiple of Hk; head h reads the q and k of head h / (H / Hk).
+ * 1 <= K, V <= 256, else SW_ERR_UNSUPPORTED.
+ *
+ * strides: host array of element strides, all >= 0, of q, k, v and g in turn,
+ * each over (B, L, heads); the width is contiguous (parts of a fused
+ * projection, broadcast inputs and transposed orders need no copy).  Loads are
+ * 16 bytes wide where address, strides and width allow it; results do not
+ * depend on it.
+ *
+ * cu_seqlens: NULL (then nseq = B), or (nseq + 1) int32 device values, ascending
+ * from 0 to L: B = 1 and the row of L steps holds nseq sequences, sequence n the
+ * steps cu_seqlens[n] .. cu_seqlens[n+1] - 1, each with its own state.  They are
+ * read by the kernels only and held to [0, L]; o at steps that no sequence
+ * covers is not written.  A sequence may be empty: its h_last is its h0 (or
+ * zero).
+ *
+ * The state and all sums are fp32; bf16 inputs run on bf16 matrix instructions
+ * with the state's increments split so that they keep fp32 accuracy, and o is
+ * rounded once more where the chunk's weights and the state become operands.
+ * An infinity or NaN in q, k, v or g reaches the steps from its own on, as in
+ * the recurrence, and no earlier one.
+ *
+ * workspace: 16-byte aligned device memory of at least
+ * sw_linear_attn_fwd_workspace bytes (flags as for the call; packed nonzero with
+ * cu_seqlens) that nothing else uses until the call completes on its stream
+ * (SW_ERR_INVALID_ARG if the call needs more), or NULL: taken from the device's
+ * stream-ordered pool for the call (then the call cannot be captured into a HIP
+ * graph; otherwise it can).  Other conventions as above.
+ */
+enum { SW_LINEAR_G_HEAD = 1 /* g is (H): one log decay for a head */ };
+int sw_linear_attn_fwd(const void* q, const void* k, const void* v, const float* g,
+                       const float* h0, const int32_t* cu_seqlens, void* o, float* h_last,
+                       int64_t B, int64_t L, int64_t Hk, int64_t H, int64_t K, int64_t V,
+                       int64_t nseq, const int64_t* strides, int dtype, int flags, float scale,
+                       void* workspace, int64_t workspace_bytes);
+int64_t sw_linear_attn_fwd_workspace(int64_t B, int64_t L, int64_t Hk, int64_t H, int64_t K,
+                                     int64_t V, int64_t nseq, int dtype, int flags, int packed);
+
+/*
+ * Backward of sw_linear_attn_fwd: the gradients of sum(dout * o) +
+ * sum(dh_last * h_last).  With dS_t the gradient with respect to S_t,
+ *
+ *   dS_t = scale q_t dout_t^T + e^{g_{t+1}} dS_{t+1}    (the last step's: + dh_last)
+ *   dq_t = scale S_t dout_t,  dk_t = dS_t v_t  (summed over the heads that share them)
+ *   dv_t = dS_t^T k_t,  dg_t = e^{g_t} <dS_t, S_{t-1}>,  dh0 = e^{g_0} dS_0
+ *
+ *   dout : (B, L, H, V) of dtype; its strides follow g's in `strides` (15 values)
+ *   dh_last : (nseq, H, K, V) fp32 or NULL (zero)
+ *   dq, dk, dv : dense, of dtype, rounded once from fp32;  dg : (B, L, H) fp32, or
+ *   (H) with SW_LINEAR_G_HEAD;  dh0 : (nseq, H, K, V) fp32 or NULL
+ * Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
+ * Otherwise as sw_linear_attn_fwd.
+ */
+int sw_linear_attn_bwd(const void* q, const void* k, const void* v, const float* g,
+                       const float* h0, const int32_t* cu_seqlens, const void* dout,
+                       const float* dh_last, void* dq, void* dk, void* dv, float* dg, float* dh0,
+                       int64_t B, int64_t L, int64_t Hk, int64_t H, int64_t K, int64_t V,
+                       int64_t nseq, const int64_t* strides, int dtype, int flags, float scale,
+                       void* workspace, int64_t workspace_bytes);
+int64_t sw_linear_attn_bwd_workspace(int64_t B, int64_t L, int64_t Hk, int64_t H, int64_t K,
+                                     int64_t V, int64_t nseq, int dtype, int flags, int packed);
+
+/*
+ * One step of B sequences, their states updated in place (serving):
+ *   S <- e^g S + k v^T,  o = scale * S^T q
+ *   q, k : (B, Hk, K), v : (B, H, V), o : (B, H, V) dense, all of dtype
+ *   g : (B, H) fp32, or (H) with SW_LINEAR_G_HEAD
+ *   state : (pool, H, K, V) fp32;  slots : (B) int32 device values or NULL.
+ * Sequence b's state is state[slots[b]] (state[b] if NULL; pool >= B then).  A
+ * slot outside [0, pool) is no sequence: its o is zero and no state changes.
+ * Two sequences must not share a slot.  strides: element strides of q, k, v and
+ * g over (B, heads), 8 values >= 0.  Launches one kernel; can be captured.
+ */
+int sw_linear_attn_step(const void* q, const void* k, const void* v, const float* g, float* state,
+                        const int32_t* slots, void* o, int64_t B, int64_t Hk, int64_t H, int64_t K,
+                        int64_t V, int64_t pool, const int64_t* strides, int dtype, int flags,
+                        float scale);
+
 /* Stream used by the calling thread's subsequent calls (a hipStream_t;
  * NULL = the null stream).  Always SW_OK. */
 int sw_set_stream(void* hip_stream);

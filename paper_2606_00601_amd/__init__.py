@@ -27,6 +27,11 @@ C ABI one function per entry point; ``lib()`` is the same ABI through ctypes.
   every gradient of the fused form (fp32), deterministic.
 * ``selective_scan_fn(...)``: the fused form as a torch autograd function
   (forward with checkpoints, the library's backward).
+* ``linear_attn_fwd(q, k, v, g, ...)``: linear attention with a log decay for
+  each head (a K x V state), chunked on the matrix cores; batches or packed
+  sequences, returning ``(o, h_last)``; ``linear_attn_bwd`` / ``linear_attn_fn``
+  are its gradients and the autograd function, ``linear_attn_step(q, k, v, g,
+  state)`` one token of each sequence of a batch, the states updated in place.
 * ``selective_scan_plan(B, D, N, L, ...)``: the kernels, segments and form
   the fused forward would take for those sizes, without launching anything.
 """
@@ -34,13 +39,16 @@ from __future__ import annotations
 
 import torch
 
+from ._bind import _need, _on, _ptr
 from ._lib import (SW_DELTA_SOFTPLUS, SW_DTYPE_BF16, SW_DTYPE_F32,  # noqa: F401
                    ScanWeaverError, check, fast, last_error, lib, status_string)
+from ._linear import linear_attn_bwd, linear_attn_fn, linear_attn_fwd, linear_attn_step
 
 __all__ = ["last_launch", "selective_scan_plan", "affine_scan", "affine_scan_noalloc", "affine_scan_i32", "affine_scan_schedule", "affine_scan_schedule_i32",
            "affine_scan_proj", "affine_scan_proj_i32",
            "selective_scan_fwd", "selective_scan_fwd_schedule", "selective_scan_bwd", "new_ckpt",
            "selective_scan_fn",
+           "linear_attn_fwd", "linear_attn_bwd", "linear_attn_fn", "linear_attn_step",
            "ScanWeaverError",
            "version"]
 
@@ -75,68 +83,6 @@ def selective_scan_plan(B, D, N, L, dtype="f32", y_dtype=None, train=False, cus=
         "sw_selective_scan_plan")
     return {"layout": layout.value, "segments": nseg.value, "segment_steps": lseg.value,
             "form": _FORMS[form.value]}
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _need(t, name, dtype, shape=None):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on a GPU (got {t.device})")
-    if t.dtype is not dtype:  # dtypes are singletons
-        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if shape is not None and t.shape != shape:  # torch.Size compares as a tuple
-        raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
-
-
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_get_device = getattr(torch._C, "_cuda_getDevice", None)
-
-
-def _current_device():
-    # the binding only runs once a GPU tensor exists, so torch's GPU state is
-    # initialised and its raw query is enough
-    if _get_device is not None:
-        return _get_device()
-    return torch.cuda.current_device()
-
-
-def _stream_handle(idx):
-    """torch's current HIP stream on GPU idx, as a raw handle."""
-    if _raw_stream is not None:
-        return _raw_stream(idx)
-    return torch.cuda.current_stream(idx).cuda_stream
-
-
-class _on:
-    """``with _on(device):`` makes the tensor's GPU current (switching only when
-    another one is) and hands torch's current stream on it to the library, for
-    the library calls inside the block."""
-
-    __slots__ = ("idx", "prev")
-
-    def __init__(self, device):
-        idx = device.index
-        self.idx = idx if idx is not None else _current_device()
-        self.prev = -1
-
-    def __enter__(self):
-        cur = _current_device()
-        if cur != self.idx:
-            torch.cuda.set_device(self.idx)
-            self.prev = cur
-        fast().sw_set_stream(_stream_handle(self.idx))
-        return self
-
-    def __exit__(self, *exc):
-        if self.prev >= 0:
-            torch.cuda.set_device(self.prev)
-        return False
 
 
 def _affine(fn, where, dtype, a, bx, h0, out):

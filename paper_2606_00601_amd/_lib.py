@@ -19,11 +19,13 @@ SW_ERR_ALLOC = 4
 SW_DTYPE_F32 = 0
 SW_DTYPE_BF16 = 1
 SW_DELTA_SOFTPLUS = 1
+SW_LINEAR_G_HEAD = 1
 SW_SCHED_DEFAULT = 0
 SW_SCHED_BLELLOCH = 1
 
 # name -> (restype, argtypes), mirroring include/scanweaver.h
 _vp, _i64, _int = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
+_f32, _strides = ctypes.c_float, ctypes.POINTER(ctypes.c_int64)
 SIGNATURES = {
     "sw_version": (_int, []),
     "sw_affine_scan": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64]),
@@ -45,6 +47,11 @@ SIGNATURES = {
     "sw_selective_scan_fwd_ex": (_int, [_vp] * 11 + [_i64] * 4 + [_int] * 3),
     "sw_selective_scan_fwd_ws": (_int, [_vp] * 11 + [_i64] * 4 + [_int] * 3 + [_vp, _i64]),
     "sw_selective_scan_fwd_workspace": (_i64, [_i64] * 4 + [_int] * 3),
+    "sw_linear_attn_fwd": (_int, [_vp] * 8 + [_i64] * 7 + [_strides, _int, _int, _f32, _vp, _i64]),
+    "sw_linear_attn_fwd_workspace": (_i64, [_i64] * 7 + [_int] * 3),
+    "sw_linear_attn_bwd": (_int, [_vp] * 13 + [_i64] * 7 + [_strides, _int, _int, _f32, _vp, _i64]),
+    "sw_linear_attn_bwd_workspace": (_i64, [_i64] * 7 + [_int] * 3),
+    "sw_linear_attn_step": (_int, [_vp] * 7 + [_i64] * 6 + [_strides, _int, _int, _f32]),
     "sw_set_stream": (_int, [_vp]),
     "sw_get_stream": (_vp, []),
     "sw_status_string": (ctypes.c_char_p, [_int]),

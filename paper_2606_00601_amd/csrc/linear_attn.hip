@@ -1,0 +1,687 @@
+// linear_attn.hip -- linear attention with a log decay for each head: plans
+// the chunked walks of linear_walk.h, composes their segments, forms the
+// decays' gradient and the sums over shared heads; and the one-step form.
+#include "linear_walk.h"
+
+namespace sw {
+namespace lin {
+namespace {
+
+// Segments composed: carry (slots, H, KV) holds what each segment adds to a
+// zero state, and gets each segment's initial state; 1024 elements of one
+// (sequence, head) per workgroup, the segments in the walk's order.
+struct FoldArgs {
+  struct {
+    float* carry;
+    const float *decay, *init;
+    bool reverse;
+  } job[2];
+  const int32_t* cu;
+  int64_t L, nseq, H, KV, lseg, per_seq, blocks;
+};
+
+__global__ __launch_bounds__(256) void fold_kernel(FoldArgs a) {
+  int64_t w = blockIdx.x;
+  const int64_t blk = w % a.blocks;
+  w /= a.blocks;
+  const int64_t h = w % a.H;
+  w /= a.H;
+  const int64_t n = w % a.nseq;
+  const auto& job = a.job[w / a.nseq];
+  int64_t first, parts;
+  if (a.cu) {
+    const int64_t c0 = cu_at(a.cu, n, a.L), c1 = cu_at(a.cu, n + 1, a.L);
+    first = c0 / a.lseg + n;
+    parts = c1 > c0 ? (c1 - c0 + a.lseg - 1) / a.lseg : 1;
+  } else {
+    first = n * a.per_seq;
+    parts = a.per_seq;
+  }
+  constexpr int U = 4;  // elements of a thread
+  const int64_t e0 = blk * (256 * U) + threadIdx.x;
+  float s[U];
+  bool in[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    in[u] = e0 + 256 * u < a.KV;
+    s[u] = in[u] && job.init ? job.init[(n * a.H + h) * a.KV + e0 + 256 * u] : 0.0f;
+  }
+  constexpr int D = 4;  // segments whose carries are in flight
+  for (int64_t j0 = 0; j0 < parts; j0 += D) {
+    float c[D][U], dec[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int64_t j = j0 + d, slot = first + (job.reverse ? parts - 1 - j : j);
+      const bool has = j < parts - 1;  // the last one hands nothing on
+      dec[d] = has ? job.decay[slot * a.H + h] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        c[d][u] = has && in[u] ? job.carry[(slot * a.H + h) * a.KV + e0 + 256 * u] : 0.0f;
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int64_t j = j0 + d, slot = first + (job.reverse ? parts - 1 - j : j);
+      if (j < parts) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (in[u]) job.carry[(slot * a.H + h) * a.KV + e0 + 256 * u] = s[u];
+          s[u] = __builtin_fmaf(dec[d], s[u], c[d][u]);
+        }
+      }
+    }
+  }
+}
+
+// dg of up to ANCHOR steps of one head: with r = q . dq and c = k . dk,
+//   dg_t = sum_{t <= i < e} (r_i - c_i) + dg_e,
+//   dg_e = e^{g_e} <dS_e, S_{e-1}> from the states kept at the interval's end e
+// (<dh_last, h_last> at the sequence's).  The difference telescopes: sums that
+// cancel never run over more than ANCHOR steps, in fp64.
+struct DgArgs {
+  const float *rdots, *cdots;  // [tile][H][B * L]
+  int tiles;
+  const float* g;
+  int64_t g_sb, g_sl, g_sh;
+  const int32_t* cu;
+  const float *S, *dS, *dh_last;
+  float* dg;        // (B, L, H), or NULL
+  double* by_slot;  // (slots, H): sums over the interval, or NULL
+  int64_t B, L, nseq, H, KV, per_seq;
+};
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+__global__ __launch_bounds__(256) void dg_kernel(DgArgs a) {
+  __shared__ double part[4], whole[4], sums[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const Place pl = place_of(a.cu, slot, ANCHOR, a.per_seq, a.nseq, a.L);
+  if (!pl.valid || pl.len == 0) {
+    if (a.by_slot && tid == 0) a.by_slot[slot * a.H + h] = 0.0;
+    return;
+  }
+  const int64_t b = a.cu ? 0 : pl.n;
+  const int64_t t0 = pl.part * ANCHOR, t1 = t0 + ANCHOR < pl.len ? t0 + ANCHOR : pl.len;
+  const float* gp = a.g + b * a.g_sb + pl.first * a.g_sl + h * a.g_sh;
+
+  // the state product at the interval's end
+  const float *s = nullptr, *d = nullptr;
+  if (t1 < pl.len) {
+    s = a.S + (slot * a.H + h) * a.KV;
+    d = a.dS + (slot * a.H + h) * a.KV;
+  } else if (a.dh_last) {
+    s = a.S + (slot * a.H + h) * a.KV;
+    d = a.dh_last + (pl.n * a.H + h) * a.KV;
+  }
+  double dot = 0.0;
+  if (s)
+    for (int64_t e = tid; e < a.KV; e += 256) dot += (double)s[e] * d[e];
+  dot = wave_sum(dot);
+  if (lane == 0) part[wave] = dot;
+
+  // a thread's steps, summed from the end
+  constexpr int U = ANCHOR / 256;
+  double v[U];
+  const int64_t at = b * a.L + pl.first;
+#pragma unroll
+  for (int u = U - 1; u >= 0; --u) {
+    const int64_t t = t0 + U * tid + u;
+    double x = 0.0;
+    if (t < t1)
+      for (int q = 0; q < a.tiles; ++q) {
+        const int64_t i = ((int64_t)q * a.H + h) * (a.B * a.L) + at + t;
+        x += (double)a.rdots[i] - a.cdots[i];
+      }
+    v[u] = u + 1 < U ? v[u + 1] + x : x;
+  }
+  double suf = v[0];  // this thread's and later lanes'
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const double o = __shfl_down(suf, k);
+    if (lane + k < 64) suf += o;
+  }
+  if (lane == 0) whole[wave] = suf;
+  __syncthreads();
+  double base = part[0] + part[1] + part[2] + part[3];
+  if (t1 < pl.len) base *= exp((double)clamp_g(gp[t1 * a.g_sl]));
+  base += suf - v[0];
+  for (int q = wave + 1; q < 4; ++q) base += whole[q];
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t t = t0 + U * tid + u;
+    if (t < t1) {
+      // where e^g is held at zero its derivative is zero too
+      const double x = gp[t * a.g_sl] < G_MIN ? 0.0 : v[u] + base;
+      sum += x;
+      if (a.dg) a.dg[(at + t) * a.H + h] = (float)x;
+    }
+  }
+  if (a.by_slot) {
+    sum = wave_sum(sum);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (tid == 0) a.by_slot[slot * a.H + h] = sums[0] + sums[1] + sums[2] + sums[3];
+  }
+}
+
+// The gradient of a decay per head: the intervals' sums, in a fixed order.
+__global__ __launch_bounds__(64) void dg_head_kernel(const double* by_slot, float* dg,
+                                                     int64_t slots, int64_t H) {
+  const int64_t h = blockIdx.x;
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < slots; i += 64) s += by_slot[i * H + h];
+  s = wave_sum(s);
+  if (threadIdx.x == 0) dg[h] = (float)s;
+}
+
+// Gradients of shared heads: rows of r * W fp32 values, summed over the r heads
+// of a group in order and rounded once.
+template <bool BF16>
+__global__ __launch_bounds__(256) void share_kernel(const float* __restrict__ part,
+                                                    void* __restrict__ out, int64_t groups, int r,
+                                                    int W) {
+  const int64_t n = groups * W;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+    const int64_t gi = i / W;
+    const float* p = part + gi * r * W + (i - gi * W);
+    float s = 0.0f;
+    for (int j = 0; j < r; ++j) s += p[(int64_t)j * W];
+    if (BF16)
+      ((uint16_t*)out)[i] = (uint16_t)bf16_rne(s);
+    else
+      ((float*)out)[i] = s;
+  }
+}
+
+// -------------------------------------------------------------- planning
+
+struct Plan {
+  int nt_v = 1, nt_k = 1;          // tiles of 64 nt columns: of V (fwd, dv), of K (dq, dk)
+  int64_t tiles_v = 1, tiles_k = 1;
+  int64_t lseg = CHUNK, per_seq = 1, slots = 0;  // segments
+  bool cut = false;                // some sequence may have several
+  int64_t aper = 1, aslots = 0;    // intervals of ANCHOR steps
+};
+
+int nt_of(int64_t contracted, int64_t cols) { return cols <= 64 || contracted > 128 ? 1 : 2; }
+
+// Segments: whole sequences where their heads and tiles fill the GPU, else
+// rows cut so that about two workgroups reach every compute unit.  A cut costs
+// a walk of the keys and values alone before the walk itself.
+Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
+  Plan p;
+  p.nt_v = nt_of(a.K, a.V);
+  p.nt_k = nt_of(a.V, a.K);
+  p.tiles_v = (a.V + 64 * p.nt_v - 1) / (64 * p.nt_v);
+  p.tiles_k = (a.K + 64 * p.nt_k - 1) / (64 * p.nt_k);
+  const int64_t per_step = a.H * (bwd ? 2 * p.tiles_k : p.tiles_v);  // workgroups of one sequence
+  const int64_t steps = a.B * a.L, longest = a.L;
+  const int64_t want = 2 * (int64_t)cus;
+  int64_t lseg = (steps * per_step + want - 1) / want;
+  lseg = (lseg + CHUNK - 1) / CHUNK * CHUNK;
+  if (lseg < 4 * CHUNK) lseg = 4 * CHUNK;
+  // a cut into two does not pay: the first walk costs about half the second
+  if (lseg * 3 / 2 >= longest) lseg = (longest + CHUNK - 1) / CHUNK * CHUNK;
+  if (lseg < CHUNK) lseg = CHUNK;
+  p.lseg = lseg;
+  p.cut = lseg < longest;
+  p.per_seq = longest > 0 ? (longest + lseg - 1) / lseg : 1;
+  p.slots = a.cu ? a.L / lseg + a.nseq : a.B * p.per_seq;
+  p.aper = longest > 0 ? (longest + ANCHOR - 1) / ANCHOR : 1;
+  p.aslots = a.cu ? a.L / ANCHOR + a.nseq : a.B * p.aper;
+  return p;
+}
+
+// The workspace's parts, in bytes from its start; every one 256-byte aligned.
+struct Layout {
+  size_t carry[2] = {0, 0}, decay[2] = {0, 0}, S = 0, dS = 0, rdots = 0, cdots = 0, dq = 0, dk = 0,
+         by_slot = 0, bytes = 0;
+};
+
+Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool dh_last) {
+  Layout l;
+  auto take = [&](size_t n) {
+    const size_t at = l.bytes;
+    l.bytes += (n + 255) / 256 * 256;
+    return at;
+  };
+  const size_t HKV = (size_t)(a.H * a.K * a.V), T = (size_t)(a.B * a.L);
+  if (p.cut)
+    for (int i = 0; i < (bwd ? 2 : 1); ++i) {
+      l.carry[i] = take((size_t)p.slots * HKV * 4);
+      l.decay[i] = take((size_t)(p.slots * a.H) * 4);
+    }
+  if (bwd) {
+    if (a.L > ANCHOR || dh_last) l.S = take((size_t)p.aslots * HKV * 4);
+    if (a.L > ANCHOR) l.dS = take((size_t)p.aslots * HKV * 4);
+    l.rdots = take((size_t)(p.tiles_k * a.H) * T * 4);
+    l.cdots = take((size_t)(p.tiles_k * a.H) * T * 4);
+    if (a.H != a.Hk) {
+      l.dq = take(T * (size_t)(a.H * a.K) * 4);
+      l.dk = take(T * (size_t)(a.H * a.K) * 4);
+    }
+    if (a.g_head) l.by_slot = take((size_t)(p.aslots * a.H) * 8);
+  }
+  return l;
+}
+
+// Whole 16-byte granules: the address, the strides and the width allow them.
+bool rows_vec(const HeadRows& x, int64_t width, bool bf16) {
+  const int64_t G = bf16 ? 8 : 4;
+  return (uintptr_t)x.p % 16 == 0 && x.sb % G == 0 && x.sl % G == 0 && x.sh % G == 0 &&
+         width % G == 0;
+}
+
+WalkArgs walk_args(const LinAttnArgs& a, const Plan& p) {
+  WalkArgs w{};
+  w.g = a.g;
+  w.g_sb = a.g_head ? 0 : a.g_sb;
+  w.g_sl = a.g_head ? 0 : a.g_sl;
+  w.g_sh = a.g_sh;
+  w.cu = a.cu;
+  w.B = a.B;
+  w.L = a.L;
+  w.nseq = a.nseq;
+  w.H = a.H;
+  w.KV = a.K * a.V;
+  w.lseg = p.lseg;
+  w.per_seq = p.per_seq;
+  w.slots = p.slots;
+  w.njobs = 1;
+  return w;
+}
+
+struct Role {
+  HeadRows rows;
+  int div;
+};
+
+// The roles of one job; `swapped`: the walk's state is (V, K).
+Job make_job(const LinAttnArgs& a, const Role& X, const Role& Y, const Role& Z, bool swapped) {
+  Job j{};
+  const int64_t cw = swapped ? a.V : a.K, zw = swapped ? a.K : a.V;
+  j.X = X.rows;
+  j.Y = Y.rows;
+  j.Z = Z.rows;
+  j.xdiv = X.div;
+  j.ydiv = Y.div;
+  j.zdiv = Z.div;
+  j.adiv = 1;
+  j.xvec = rows_vec(X.rows, cw, a.bf16);
+  j.yvec = rows_vec(Y.rows, cw, a.bf16);
+  j.zvec = rows_vec(Z.rows, zw, a.bf16);
+  j.skk = swapped ? 1 : a.V;
+  j.svv = swapped ? a.V : 1;
+  j.pscale = a.scale;
+  j.wscale = 1.0f;
+  j.rscale = 1.0f;
+  return j;
+}
+
+void set_out(Job& j, const LinAttnArgs& a, void* out, int64_t heads, int64_t width, bool f32) {
+  j.out = out;
+  j.oh = width;
+  j.ol = heads * width;
+  j.ob = a.L * j.ol;
+  j.out_f32 = f32;
+  j.ovec = (uintptr_t)out % 16 == 0 && width % 8 == 0;  // a lane's columns: 4 or 8
+}
+
+int launch_walk_any(const LinAttnArgs& a, WalkArgs& w, Mode m, int64_t KK, int64_t VV, int nt,
+                    int64_t tiles, hipStream_t st) {
+  w.KK = (int)KK;
+  w.VV = (int)VV;
+  w.tiles = (int)tiles;
+  return a.bf16 ? launch_walk_bf16(w, m, nt, st) : launch_walk_f32(w, m, nt, st);
+}
+
+int launch_fold(const LinAttnArgs& a, const Plan& p, FoldArgs& f, int njobs, hipStream_t s) {
+  f.cu = a.cu;
+  f.L = a.L;
+  f.nseq = a.nseq;
+  f.H = a.H;
+  f.KV = a.K * a.V;
+  f.lseg = p.lseg;
+  f.per_seq = p.per_seq;
+  f.blocks = (f.KV + 1023) / 1024;
+  hipLaunchKernelGGL(fold_kernel, dim3((unsigned)(f.blocks * a.H * a.nseq * njobs)), dim3(256), 0, s,
+                     f);
+  return check_launch("fold_kernel");
+}
+
+int check_grid(const LinAttnArgs& a, const Plan& p, bool bwd) {
+  const int64_t tiles = p.tiles_k > p.tiles_v ? p.tiles_k : p.tiles_v;
+  const int64_t blocks = (a.K * a.V + 1023) / 1024;
+  int64_t n = p.slots > a.nseq ? p.slots : a.nseq;
+  if (bwd && p.aslots > n) n = p.aslots;
+  int64_t most;
+  if (__builtin_mul_overflow(n, a.H * 2 * (tiles > blocks ? tiles : blocks), &most) ||
+      most > SW_MAX_WGS)
+    return fail(SW_ERR_UNSUPPORTED, "%lld segments of %lld heads exceed the launch limit",
+                (long long)n, (long long)a.H);
+  return SW_OK;
+}
+
+// The call's workspace: the caller's, or the pool's for the call.
+struct Workspace {
+  char* p = nullptr;
+  bool own = false;
+  hipStream_t s;
+  explicit Workspace(hipStream_t st) : s(st) {}
+  ~Workspace() {
+    if (own) workspace_free(p, s);
+  }
+  int get(const LinAttnArgs& a, size_t bytes, const char* what) {
+    if (bytes == 0) return SW_OK;
+    if (a.ws) {
+      if (a.ws_bytes < bytes)
+        return fail(SW_ERR_INVALID_ARG, "workspace of %zu bytes, %zu needed", a.ws_bytes, bytes);
+      p = (char*)a.ws;
+      return SW_OK;
+    }
+    int st = refuse_capture(s, what);
+    if (st != SW_OK) return st;
+    void* v = nullptr;
+    if ((st = workspace_alloc(&v, bytes, s)) != SW_OK) return st;
+    p = (char*)v;
+    own = true;
+    return SW_OK;
+  }
+};
+
+}  // namespace
+}  // namespace lin
+
+using namespace lin;
+
+int64_t linear_attn_fwd_workspace(const LinAttnArgs& a) {
+  int cus;
+  if (device_cus(&cus) != SW_OK) return 0;
+  return (int64_t)make_layout(a, make_plan(a, false, cus), false, false).bytes;
+}
+
+int64_t linear_attn_bwd_workspace(const LinAttnArgs& a) {
+  int cus;
+  if (device_cus(&cus) != SW_OK) return 0;
+  return (int64_t)make_layout(a, make_plan(a, true, cus), true, true).bytes;
+}
+
+int linear_attn_fwd(const LinAttnArgs& a) {
+  int cus, st;
+  if ((st = device_cus(&cus)) != SW_OK) return st;
+  const Plan p = make_plan(a, false, cus);
+  if ((st = check_grid(a, p, false)) != SW_OK) return st;
+  const Layout l = make_layout(a, p, false, false);
+  const hipStream_t s = current_stream();
+  Workspace ws(s);
+  if ((st = ws.get(a, l.bytes, "sw_linear_attn_fwd")) != SW_OK) return st;
+  const int r = (int)(a.H / a.Hk);
+  WalkArgs w = walk_args(a, p);
+  Job j = make_job(a, {a.q, r}, {a.k, r}, {a.v, 1}, false);
+  j.rscale = a.scale;
+  j.init = a.h0;
+  j.last = a.h_last;
+  set_out(j, a, a.o, a.H, a.V, !a.bf16);
+  if (p.cut) {
+    j.carry = (float*)(ws.p + l.carry[0]);
+    j.decay = (float*)(ws.p + l.decay[0]);
+    w.job[0] = j;
+    if ((st = launch_walk_any(a, w, CARRY, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
+    FoldArgs f{};
+    f.job[0] = {j.carry, j.decay, a.h0, false};
+    if ((st = launch_fold(a, p, f, 1, s)) != SW_OK) return st;
+  }
+  w.job[0] = j;
+  return launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s);
+}
+
+int linear_attn_bwd(const LinAttnArgs& a) {
+  int cus, st;
+  if ((st = device_cus(&cus)) != SW_OK) return st;
+  const Plan p = make_plan(a, true, cus);
+  if ((st = check_grid(a, p, true)) != SW_OK) return st;
+  const Layout l = make_layout(a, p, true, a.dh_last != nullptr);
+  const hipStream_t s = current_stream();
+  Workspace ws(s);
+  if ((st = ws.get(a, l.bytes, "sw_linear_attn_bwd")) != SW_OK) return st;
+  const int r = (int)(a.H / a.Hk);
+  const Role q{a.q, r}, k{a.k, r}, v{a.v, 1}, dout{a.dout, 1};
+  const bool shared = r > 1;
+  auto at = [&](size_t off) { return (float*)(ws.p + off); };
+
+  WalkArgs w = walk_args(a, p);
+  Job jq = make_job(a, dout, v, k, true);
+  jq.rscale = a.scale;
+  jq.init = a.h0;
+  Job jk = make_job(a, v, dout, q, true);
+  jk.reverse = true;
+  jk.wscale = a.scale;
+  jk.init = a.dh_last;
+  Job jv = make_job(a, k, q, dout, false);
+  jv.reverse = true;
+  jv.wscale = a.scale;
+  jv.init = a.dh_last;
+  jv.last = a.dh0;
+  set_out(jv, a, a.dv, a.H, a.V, !a.bf16);
+  set_out(jq, a, shared ? at(l.dq) : a.dq, a.H, a.K, shared || !a.bf16);
+  set_out(jk, a, shared ? at(l.dk) : a.dk, a.H, a.K, shared || !a.bf16);
+  if (p.cut) {
+    jq.carry = at(l.carry[0]);
+    jq.decay = at(l.decay[0]);
+    jk.carry = jv.carry = at(l.carry[1]);
+    jk.decay = jv.decay = at(l.decay[1]);
+    w.job[0] = jq;
+    w.job[1] = jk;
+    w.njobs = 2;
+    if ((st = launch_walk_any(a, w, CARRY, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
+    FoldArgs f{};
+    f.job[0] = {jq.carry, jq.decay, a.h0, false};
+    f.job[1] = {jk.carry, jk.decay, a.dh_last, true};
+    if ((st = launch_fold(a, p, f, 2, s)) != SW_OK) return st;
+  }
+  // dq and dk: their products with q and k are the decays' gradient
+  jq.A = a.q;
+  jq.adiv = r;
+  jq.avec = rows_vec(a.q, a.K, a.bf16) && a.K % 8 == 0;
+  jq.dots = at(l.rdots);
+  jk.A = a.k;
+  jk.adiv = r;
+  jk.avec = rows_vec(a.k, a.K, a.bf16) && a.K % 8 == 0;
+  jk.dots = at(l.cdots);
+  if (a.L > ANCHOR || a.dh_last) jq.anchors = at(l.S);
+  jq.last_anchor = a.dh_last != nullptr;
+  if (a.L > ANCHOR) jk.anchors = at(l.dS);
+  w.job[0] = jq;
+  w.job[1] = jk;
+  w.njobs = 2;
+  if ((st = launch_walk_any(a, w, GRAD, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
+  w.job[0] = jv;
+  w.njobs = 1;
+  if ((st = launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
+
+  DgArgs d{};
+  d.rdots = at(l.rdots);
+  d.cdots = at(l.cdots);
+  d.tiles = (int)p.tiles_k;
+  d.g = a.g;
+  d.g_sb = w.g_sb;
+  d.g_sl = w.g_sl;
+  d.g_sh = w.g_sh;
+  d.cu = a.cu;
+  d.S = at(l.S);
+  d.dS = at(l.dS);
+  d.dh_last = a.dh_last;
+  d.dg = a.g_head ? nullptr : a.dg;
+  d.by_slot = a.g_head ? (double*)at(l.by_slot) : nullptr;
+  d.B = a.B;
+  d.L = a.L;
+  d.nseq = a.nseq;
+  d.H = a.H;
+  d.KV = a.K * a.V;
+  d.per_seq = p.aper;
+  if (p.aslots > 0) {
+    hipLaunchKernelGGL(dg_kernel, dim3((unsigned)(p.aslots * a.H)), dim3(256), 0, s, d);
+    if ((st = check_launch("dg_kernel")) != SW_OK) return st;
+  }
+  if (a.g_head) {
+    hipLaunchKernelGGL(dg_head_kernel, dim3((unsigned)a.H), dim3(64), 0, s, d.by_slot, a.dg, p.aslots,
+                       a.H);
+    if ((st = check_launch("dg_head_kernel")) != SW_OK) return st;
+  }
+  const int64_t groups = a.B * a.L * a.Hk;
+  if (shared && groups > 0) {
+    int64_t wgs = (groups * a.K + 255) / 256;
+    if (wgs > 16384) wgs = 16384;
+    for (int i = 0; i < 2; ++i) {
+      const float* part = at(i ? l.dk : l.dq);
+      void* out = i ? a.dk : a.dq;
+      if (a.bf16)
+        hipLaunchKernelGGL(share_kernel<true>, dim3((unsigned)wgs), dim3(256), 0, s, part, out, groups,
+                           r, (int)a.K);
+      else
+        hipLaunchKernelGGL(share_kernel<false>, dim3((unsigned)wgs), dim3(256), 0, s, part, out, groups,
+                           r, (int)a.K);
+      if ((st = check_launch("share_kernel")) != SW_OK) return st;
+    }
+  }
+  return SW_OK;
+}
+
+// ---------------------------------------------------------------- one step
+
+namespace lin {
+namespace {
+
+// S <- e^g S + k v^T, o = scale S^T q for one (sequence, head) and tile of 4 LC
+// columns: LC lanes hold four columns each of one row of S, 256 / LC rows at a
+// time, so that a row of the tile is one contiguous read and write; the rows'
+// parts of o meet in LDS.  Bound by the state's traffic, read and written once.
+template <class E, bool VEC>
+__global__ __launch_bounds__(256) void step_kernel(LinStepArgs a, int lc, int tiles) {
+  __shared__ float sk[LINATTN_MAX_WIDTH], sq[LINATTN_MAX_WIDTH];
+  __shared__ __align__(16) float so[1024];
+  const int tid = threadIdx.x;
+  uint32_t w = blockIdx.x;
+  const int tile = w % (uint32_t)tiles;
+  w /= (uint32_t)tiles;
+  const int h = w % (uint32_t)a.H, K = (int)a.K, V = (int)a.V;
+  const int64_t b = w / (uint32_t)a.H;
+  const int64_t slot = a.slots ? a.slots[b] : b;
+  const int hk = h / (int)(a.H / a.Hk);
+  const int v0 = tile * 4 * lc, cols = V - v0 < 4 * lc ? V - v0 : 4 * lc;
+  E* o = (E*)a.o + (b * a.H + h) * a.V + v0;
+  auto put = [&](int c, float x) {
+    if constexpr (sizeof(E) == 2)
+      o[c] = (E)bf16_rne(x);
+    else
+      o[c] = x;
+  };
+  if (slot < 0 || slot >= a.pool) {
+    for (int c = tid; c < cols; c += 256) put(c, 0.0f);
+    return;
+  }
+  const int col = tid % lc * 4, row0 = tid / lc, rows = 256 / lc;
+  float* S = a.state + (slot * a.H + h) * a.K * a.V + v0 + col;
+  constexpr int U = 8;  // rows of a thread in flight
+  f4 s[U];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * rows;
+      s[u] = f4{0.f, 0.f, 0.f, 0.f};
+      if (i < K) {
+        if (VEC) {
+          if (col < cols) s[u] = *reinterpret_cast<const f4*>(S + (int64_t)i * V);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (col + c < cols) s[u][c] = S[(int64_t)i * V + c];
+        }
+      }
+    }
+  };
+  load(row0);
+  const E* q = (const E*)a.q + b * a.q_sb + hk * a.q_sh;
+  const E* k = (const E*)a.k + b * a.k_sb + hk * a.k_sh;
+  const E* v = (const E*)a.v + b * a.v_sb + h * a.v_sh + v0 + col;
+  if (tid < K) {
+    sk[tid] = widen1(k[tid]);
+    sq[tid] = widen1(q[tid]);
+  }
+  f4 vv;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) vv[c] = col + c < cols ? widen1(v[c]) : 0.0f;
+  const float dec =
+      exp2_of((double)clamp_g(a.g[b * a.g_sb + h * a.g_sh]) * 1.4426950408889634);
+  __syncthreads();
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = row0; i0 < K; i0 += U * rows) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * rows;
+      if (i < K) {
+        const float kk = sk[i], qq = sq[i];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s[u][c] = __builtin_fmaf(kk, vv[c], dec * s[u][c]);
+          acc[c] = __builtin_fmaf(qq, s[u][c], acc[c]);
+        }
+        if (VEC) {
+          if (col < cols) *reinterpret_cast<f4*>(S + (int64_t)i * V) = s[u];
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (col + c < cols) S[(int64_t)i * V + c] = s[u][c];
+        }
+      }
+    }
+    if (i0 + U * rows < K) load(i0 + U * rows);
+  }
+  *reinterpret_cast<f4*>(so + row0 * 4 * lc + col) = acc;
+  __syncthreads();
+  if (tid < cols) {
+    float x = 0.0f;
+    for (int i = 0; i < rows; ++i) x += so[i * 4 * lc + tid];
+    put(tid, a.scale * x);
+  }
+}
+
+}  // namespace
+}  // namespace lin
+
+int linear_attn_step(const LinStepArgs& a) {
+  if (a.B * a.H == 0) return SW_OK;
+  int cus, st;
+  if ((st = device_cus(&cus)) != SW_OK) return st;
+  const bool vec = a.V % 4 == 0 && (uintptr_t)a.state % 16 == 0;
+  // tiles of 128 columns, or of fewer where that leaves compute units without work
+  int lc = 32;
+  while (lc > 1 && 2 * lc >= a.V) lc /= 2;  // no wider than the state
+  while (lc > 8 && a.B * a.H * ((a.V + 4 * lc - 1) / (4 * lc)) < 2 * (int64_t)cus) lc /= 2;
+  const int64_t tiles = (a.V + 4 * lc - 1) / (4 * lc);
+  const int64_t wgs = a.B * a.H * tiles;
+  if (wgs > SW_MAX_WGS)
+    return fail(SW_ERR_UNSUPPORTED, "%lld sequences of %lld heads exceed the launch limit",
+                (long long)a.B, (long long)a.H);
+  const dim3 grid((unsigned)wgs), block(256);
+  const hipStream_t s = current_stream();
+  if (a.bf16) {
+    if (vec)
+      hipLaunchKernelGGL((step_kernel<uint16_t, true>), grid, block, 0, s, a, lc, (int)tiles);
+    else
+      hipLaunchKernelGGL((step_kernel<uint16_t, false>), grid, block, 0, s, a, lc, (int)tiles);
+  } else {
+    if (vec)
+      hipLaunchKernelGGL((step_kernel<float, true>), grid, block, 0, s, a, lc, (int)tiles);
+    else
+      hipLaunchKernelGGL((step_kernel<float, false>), grid, block, 0, s, a, lc, (int)tiles);
+  }
+  return check_launch("step_kernel");
+}
+
+}  // namespace sw

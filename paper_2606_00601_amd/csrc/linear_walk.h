@@ -1,0 +1,784 @@
+// linear_walk.h -- the chunked walk of linear attention (device code and its
+// launch), included by one source file per element type so that they compile
+// side by side.
+//
+// With roles X (read-out), Y (key), Z (value) and log decays g, one walk
+// evaluates, over the steps of a sequence in the walk's order,
+//     S_i = e^{g_i} S_{i-1} + w Y_i Z_i^T,     out_i = S_i^T X_i
+// and so serves the forward (q, k, v) and, with the roles exchanged, every
+// gradient: dq walks forward with (do, v, k), dk backwards with (v, do, q),
+// dv backwards with (k, q, do).  Backwards, the decay between a step and the
+// one walked before it is that of the later step in time.
+//
+// C steps at a time (G_i: the decays' running sum inside the chunk):
+//     P_ts = (X_t . Y_s) e^{G_t - G_s}  for s <= t, else 0
+//     out  = P Z + e^G X S        S <- e^{G_C} S + (e^{G_C - G} Z)^T-weighted Y^T
+// All four products run on the matrix cores.  A workgroup of four waves walks
+// one (sequence, segment, head, tile of Z's columns); a wave owns 16 NT
+// columns and keeps its part of S in accumulators, fp32, from the first step
+// to the last.  The lane that holds an accumulator's column is the lane that
+// the next product wants as an operand's row, and the contraction order is
+// free, so S and the weighted Z go from accumulators to operands without
+// moving between lanes.
+//
+// Rounding (bf16): products of inputs are exact in fp32 accumulators.  The
+// weighted Z is split in three bf16 parts whose sum is the fp32 value, so S
+// keeps fp32 accuracy whatever the number of chunks.  For an output in bf16
+// (NS = 1), P and S are rounded to bf16 once as operands; for outputs whose
+// products with an input feed an fp32 gradient (NS = 3), both are split in
+// three.  fp32 inputs run on the fp32 matrix instructions throughout.
+#pragma once
+
+#include "linear_attn.h"
+
+namespace sw {
+namespace lin {
+
+constexpr int CHUNK = 64;      // steps between the places where walks may start or stop
+constexpr int ANCHOR = 256;    // steps between the states kept for dg
+constexpr float G_MIN = -1.0e4f;  // e^g is zero in fp32 far above this
+
+struct Job {
+  HeadRows X, Y, Z, A;   // A: the input whose products with out are summed (dots)
+  int xdiv, ydiv, zdiv, adiv;  // head h reads head h / div
+  bool xvec, yvec, zvec, avec, ovec;  // rows are 16-byte aligned whole vectors
+  void* out;
+  int64_t ob, ol, oh;
+  bool out_f32;
+  bool reverse;
+  float* dots;           // [tile][H][B * L] or NULL
+  const float* init;     // (sequences, H, K, V): the state before the first step, or NULL
+  float* last;           // the state after the last step, or NULL
+  float* carry;          // (slots, H, K, V): carries written, or initial states read, or NULL
+  float* decay;          // (slots, H): the segments' decays (written with the carries)
+  float* anchors;        // (anchor slots, H, K, V) or NULL
+  bool last_anchor;      // the state after the last step is an anchor too
+  int64_t skk, svv;      // where state element (Y's column, Z's column) lies in (K, V)
+  float pscale, wscale, rscale;
+};
+
+struct WalkArgs {
+  Job job[2];
+  const float* g;
+  int64_t g_sb, g_sl, g_sh;
+  const int32_t* cu;
+  int64_t B, L, nseq, H;
+  int KK, VV;            // widths: of X and Y, of Z and out
+  int64_t KV;            // K * V
+  int64_t lseg;          // steps of a segment, a multiple of CHUNK
+  int64_t per_seq;       // segments of a sequence (cu == NULL)
+  int64_t slots;
+  int tiles, njobs;
+};
+
+// Where slot `slot` of width `w` steps lies: packed sequence n's slots start at
+// cu[n] / w + n, which leaves room for each one's ceil(length / w).
+struct Place {
+  int64_t n, first, len, part, parts;  // sequence, its first step, length, which slot of how many
+  bool valid;
+};
+
+__device__ __forceinline__ int64_t cu_at(const int32_t* cu, int64_t i, int64_t L) {
+  const int64_t c = cu[i];
+  return c < 0 ? 0 : c > L ? L : c;  // never outside the row, whatever cu holds
+}
+
+__device__ __forceinline__ Place place_of(const int32_t* cu, int64_t slot, int64_t w,
+                                          int64_t per_seq, int64_t nseq, int64_t L) {
+  Place p;
+  if (!cu) {
+    p.n = slot / per_seq;
+    p.part = slot - p.n * per_seq;
+    p.first = 0;
+    p.len = L;
+  } else {
+    int64_t lo = 0, hi = nseq - 1;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi + 1) / 2;
+      if (cu_at(cu, mid, L) / w + mid <= slot) lo = mid; else hi = mid - 1;
+    }
+    p.n = lo;
+    p.first = cu_at(cu, lo, L);
+    const int64_t end = cu_at(cu, lo + 1, L);
+    p.len = end > p.first ? end - p.first : 0;
+    p.part = slot - (p.first / w + lo);
+  }
+  p.parts = p.len > 0 ? (p.len + w - 1) / w : 1;
+  p.valid = p.n < nseq && p.part >= 0 && p.part < p.parts;
+  return p;
+}
+
+__device__ __forceinline__ int64_t first_slot(const Place& p, const int32_t* cu, int64_t w,
+                                              int64_t per_seq) {
+  return cu ? p.first / w + p.n : p.n * per_seq;
+}
+
+// e^g of a decay as the walks use it.
+__device__ __forceinline__ float clamp_g(float g) { return g < G_MIN ? G_MIN : g; }
+
+// 2^x of a double, to fp32 rounding.
+__device__ __forceinline__ float exp2_of(double x) {
+  const double n = rint(x);
+  const float f = __builtin_amdgcn_exp2f((float)(x - n));
+  const float e = (float)n;
+  return e < -300.0f ? 0.0f : e > 300.0f ? INFINITY : ldexpf(f, (int)e);
+}
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+
+struct Bf16 {
+  typedef uint16_t E;
+  static constexpr int C = 64, G = 8, GB = 3;  // steps of a chunk; elements of 16 bytes
+  static constexpr int NW = 3;                 // parts of the weighted Z
+  static constexpr bool SPLIT = true;
+};
+struct F32 {
+  typedef float E;
+  static constexpr int C = 32, G = 4, GB = 2;
+  static constexpr int NW = 1;
+  static constexpr bool SPLIT = false;
+};
+
+// An operand fragment of a 16 x 16 product over 32 contraction indices: lane
+// (g = lane / 16, r = lane % 16) holds row r at indices 8 g .. 8 g + 7.
+template <class T> struct Frag;
+template <> struct Frag<Bf16> { s8 v; };
+template <> struct Frag<F32> { float v[8]; };
+
+__device__ __forceinline__ f4 mma(const Frag<Bf16>& a, const Frag<Bf16>& b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a.v),
+                                                 __builtin_bit_cast(b8, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 mma(const Frag<F32>& a, const Frag<F32>& b, f4 c) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+  return c;
+}
+
+// LDS tiles are rows of W elements and 16 bytes of padding, so that one
+// granule of 16 bytes of eight neighbouring rows, and four granules of rows
+// four apart, lie in different banks, and every fragment of a lane is at a
+// constant offset from its first.
+template <class T, int W>
+constexpr int ROW = W + T::G;
+
+// The contraction over a chunk's steps runs in blocks of 32; in each, place q
+// of an operand (lane group q / 8, element q % 8) is step 4 (q % 8) + q / 8.
+__device__ __forceinline__ int step_of(int q) { return (q & ~31) + 4 * (q & 7) + ((q >> 3) & 3); }
+__device__ __forceinline__ int place_in(int s) { return (s & ~31) + 8 * (s & 3) + ((s >> 2) & 7); }
+
+__device__ __forceinline__ Frag<Bf16> row_frag(const uint16_t* t) {
+  return {*reinterpret_cast<const s8*>(t)};
+}
+__device__ __forceinline__ Frag<F32> row_frag(const float* t) {
+  Frag<F32> f;
+  *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(t);
+  *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(t + 4);
+  return f;
+}
+
+// The transposed fragment of 32 steps: lane (g, r) holds column
+// STEP * (r / 4) + r % 4 at the steps 4 j + g, j = 0 .. 7.  col_base gives the
+// lane's address for the block's first step and the columns' first.
+template <int W, int STEP>
+__device__ __forceinline__ const uint16_t* col_base(const uint16_t* t, int g, int r) {
+  return t + (4 * (r >> 2) + g) * ROW<Bf16, W> + STEP * (r & 3);
+}
+template <int W, int STEP>
+__device__ __forceinline__ const float* col_base(const float* t, int g, int r) {
+  return t + g * ROW<F32, W> + STEP * (r >> 2) + (r & 3);
+}
+template <int W>
+__device__ __forceinline__ Frag<Bf16> col_frag(const uint16_t* t) {
+  typedef __attribute__((address_space(3))) s4* lds_s4;
+  const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)t);
+  const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(t + 16 * ROW<Bf16, W>));
+  return {s8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+template <int W>
+__device__ __forceinline__ Frag<F32> col_frag(const float* t) {
+  Frag<F32> f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j] = t[4 * j * ROW<F32, W>];
+  return f;
+}
+
+__device__ __forceinline__ s8 pack8(const float* x) {
+  uint4 u;
+  u.x = bf16x2_rne(x[0], x[1]);
+  u.y = bf16x2_rne(x[2], x[3]);
+  u.z = bf16x2_rne(x[4], x[5]);
+  u.w = bf16x2_rne(x[6], x[7]);
+  return __builtin_bit_cast(s8, u);
+}
+// x minus its bf16 rounding h (exact).
+__device__ __forceinline__ void take_off(float* x, s8 h) {
+  const uint4 u = __builtin_bit_cast(uint4, h);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] -= j & 1 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+}
+// Eight fp32 values as N operand parts.
+template <int N>
+__device__ __forceinline__ void parts_of(const float* x, Frag<Bf16>* f) {
+  float t[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t[j] = x[j];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    f[i].v = pack8(t);
+    if (i + 1 < N) take_off(t, f[i].v);
+  }
+}
+template <int N>
+__device__ __forceinline__ void parts_of(const float* x, Frag<F32>* f) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[0].v[j] = x[j];
+}
+__device__ __forceinline__ void widen(const Frag<Bf16>& f, float* x) {
+  const uint4 u = __builtin_bit_cast(uint4, f.v);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[2 * j] = bf16_lo(w[j]);
+    x[2 * j + 1] = bf16_hi(w[j]);
+  }
+}
+__device__ __forceinline__ void widen(const Frag<F32>& f, float* x) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = f.v[j];
+}
+
+__device__ __forceinline__ float widen1(uint16_t e) { return bf16_one(e); }
+__device__ __forceinline__ float widen1(float e) { return e; }
+
+// Bit 15 and 31 (bf16) or 31 (fp32) set where an element is not finite.
+template <class T>
+__device__ __forceinline__ uint32_t nonfinite(uint4 u) {
+  if (T::SPLIT) {
+    const uint32_t m = 0x7f807f80u, o = 0x00800080u;
+    return (((u.x & m) + o) | ((u.y & m) + o) | ((u.z & m) + o) | ((u.w & m) + o)) & 0x80008000u;
+  }
+  const uint32_t m = 0x7f800000u, o = 0x00800000u;
+  return (((u.x & m) + o) | ((u.y & m) + o) | ((u.z & m) + o) | ((u.w & m) + o)) & 0x80000000u;
+}
+
+// One thread's granules of a C x W tile: rows [0, n) of `rows` (row i lies
+// i * step elements on), columns below width; zero elsewhere.
+template <class T, int W>
+struct Tile {
+  static constexpr int NG = W / T::G, PER = T::C * NG / 256, RPG = 256 / NG;
+  static_assert(PER >= 1 && T::C * NG % 256 == 0, "whole granules per thread");
+  uint4 u[PER];
+  __device__ __forceinline__ void load(const typename T::E* rows, int64_t step, int n, int width,
+                                       bool vec, int tid) {
+    const int row = tid / NG, col = tid % NG * T::G;
+    const typename T::E* p = rows + row * step + col;
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        u[i] = make_uint4(0, 0, 0, 0);
+        if (row + i * RPG < n && col < width) u[i] = *reinterpret_cast<const uint4*>(p);
+        p += RPG * step;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        typename T::E e[T::G];
+#pragma unroll
+        for (int j = 0; j < T::G; ++j)
+          e[j] = row + i * RPG < n && col + j < width ? p[j] : (typename T::E)0;
+        __builtin_memcpy(&u[i], e, 16);
+        p += RPG * step;
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t store(typename T::E* lds, int tid) const {
+    uint32_t bad = 0;
+    typename T::E* p = lds + tid / NG * ROW<T, W> + tid % NG * T::G;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      *reinterpret_cast<uint4*>(p + i * RPG * ROW<T, W>) = u[i];
+      bad |= nonfinite<T>(u[i]);
+    }
+    return bad;
+  }
+};
+
+// What a walk is for: the segments' carries; an output; an output whose
+// products with an input are summed by step (with the states kept for dg).
+enum Mode { CARRY, OUT, GRAD };
+
+template <class T, int KP, int NT, Mode MODE>
+struct Shared {
+  static constexpr int VT = 64 * NT, C = T::C;
+  static constexpr int NS = MODE == GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
+  static constexpr bool XS = MODE != CARRY;
+  typename T::E y[C * ROW<T, KP>];
+  typename T::E z[C * ROW<T, VT>];
+  typename T::E x[XS ? C * ROW<T, KP> : 8];
+  typename T::E p[XS ? NS * C * ROW<T, C> : 8];
+  float gh[C], gl[C];  // by step: the running log2 decay, high and low parts
+  float er[C];         // by step: rscale 2^G
+  float ph[C], pl[C];  // by place: gh and gl
+  float ew[C];         // by place: wscale 2^(G_C - G)
+  float dots[MODE == GRAD ? 4 * C : 4];
+  float ec;            // 2^G_C
+  uint32_t bad[2];
+};
+
+// Waves per SIMD: what the accumulators of S, out and the loads in flight leave
+// room for (KP = 128, NT = 2: 64 + 32 + 48 registers of 256).
+constexpr int walk_waves(int KP, int NT, Mode m) {
+  return KP >= 256 ? 1 : KP <= 64 && NT == 1 && m != GRAD ? 3 : 2;
+}
+
+template <class T, int KP, int NT, Mode MODE>
+__global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(WalkArgs a) {
+  typedef typename T::E E;
+  typedef Shared<T, KP, NT, MODE> Sh;
+  constexpr bool XS = MODE != CARRY;
+  constexpr int C = T::C, KT = KP / 16, VT = 64 * NT, SB = C / 32, TT = C / 16, NS = Sh::NS;
+  // P: a wave's 16 steps t, and ST tiles of 16 steps s (all of them at C = 64,
+  // one of two at C = 32)
+  constexpr int ST = C * C / 1024;
+  constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, PR = ROW<T, C>;
+  __shared__ __align__(16) Sh sh;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
+  uint32_t w = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int tile = w % (uint32_t)a.tiles;
+  w /= (uint32_t)a.tiles;
+  const int h = w % (uint32_t)a.H;
+  w /= (uint32_t)a.H;
+  const int64_t slot = w % (uint32_t)a.slots;
+  const Job& job = a.job[w / (uint32_t)a.slots];
+  const Place pl = place_of(a.cu, slot, a.lseg, a.per_seq, a.nseq, a.L);
+  if (!pl.valid) return;
+  const bool rev = job.reverse;
+  // the last segment in the walk's order hands nothing on
+  const bool final_seg = rev ? pl.part == 0 : pl.part == pl.parts - 1;
+  if (MODE == CARRY && final_seg) return;
+  const int64_t b = a.cu ? 0 : pl.n;
+  const int v0 = tile * VT, vb = wave * 16 * NT;  // the tile's first column; the wave's in it
+
+  // steps [lo, hi) of the sequence, in chunks of at most C
+  const int len = (int)pl.len, lo = (int)(pl.part * a.lseg);
+  const int hi = len - lo < a.lseg ? len : lo + (int)a.lseg;
+  const int nch = hi > lo ? (hi - lo + C - 1) / C : 0;
+
+  // the rows of the sequence's first step
+  const E* X = nullptr;
+  if (XS) X = (const E*)job.X.p + b * job.X.sb + pl.first * job.X.sl + h / job.xdiv * job.X.sh;
+  const E* Y = (const E*)job.Y.p + b * job.Y.sb + pl.first * job.Y.sl + h / job.ydiv * job.Y.sh;
+  const E* Z = (const E*)job.Z.p + b * job.Z.sb + pl.first * job.Z.sl + h / job.zdiv * job.Z.sh + v0;
+  const float* gp = a.g + b * a.g_sb + pl.first * a.g_sl + h * a.g_sh;
+
+  f4 S[KT][NT];
+  // state element of accumulator (kt, nt, i): Y's column 32 (kt / 2) + 8 g + 4 (kt % 2) + i,
+  // Z's column v0 + vb + 4 NT (r / 4) + 4 nt + r % 4
+  auto each_state = [&](auto fn) __attribute__((always_inline)) {
+    int kk = 8 * g, vv = v0 + vb + 4 * NT * (r >> 2) + (r & 3);
+    asm volatile("" : "+v"(kk), "+v"(vv));  // worked out here, not kept across the walk
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (vv + 4 * nt < a.VV) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = kk + 32 * (kt >> 1) + 4 * (kt & 1) + i;
+            if (k < a.KK) fn(kt, nt, i, k * job.skk + (vv + 4 * nt) * job.svv);
+          }
+      }
+    }
+  };
+  auto store_state = [&](float* p, float f) __attribute__((always_inline)) {
+    each_state([&](int kt, int nt, int i, int64_t at) __attribute__((always_inline)) { p[at] = S[kt][nt][i] * f; });
+  };
+  auto anchor_at = [&](int64_t i) {  // the sequence's i-th
+    const int64_t per = (a.L + ANCHOR - 1) / ANCHOR;
+    return job.anchors + ((first_slot(pl, a.cu, ANCHOR, per) + i) * a.H + h) * a.KV;
+  };
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) S[kt][nt] = f4{0.f, 0.f, 0.f, 0.f};
+  if (XS) {
+    const float* p = job.carry ? job.carry + (slot * a.H + h) * a.KV
+                     : job.init ? job.init + (pl.n * a.H + h) * a.KV
+                                : nullptr;
+    if (p) each_state([&](int kt, int nt, int i, int64_t at) __attribute__((always_inline)) { S[kt][nt][i] = p[at]; });
+  }
+  float seg_decay = 1.0f;
+
+  Tile<T, KP> tx, ty;
+  Tile<T, VT> tz;
+  float tg = 0.0f;
+  int t0 = 0, n = 0;  // the chunk's steps: t0 .. t0 + n - 1
+  auto chunk_at = [&](int c) {
+    t0 = lo + (rev ? nch - 1 - c : c) * C;
+    n = hi - t0 < C ? hi - t0 : C;
+  };
+  // rows [i0, i0 + cnt) of the chunk, in the walk's order
+  auto load_rows = [&](int i0, int cnt) {
+    const int64_t t = rev ? t0 + n - 1 - i0 : t0 + i0;
+    const int64_t d = rev ? -1 : 1;
+    if (XS) tx.load(X + t * job.X.sl, d * job.X.sl, cnt, a.KK, job.xvec, tid);
+    ty.load(Y + t * job.Y.sl, d * job.Y.sl, cnt, a.KK, job.yvec, tid);
+    tz.load(Z + t * job.Z.sl, d * job.Z.sl, cnt, a.VV - v0, job.zvec, tid);
+    if (wave == 0) {
+      // backwards, a step's decay is that of the step after it in time; none at the end
+      const int64_t s = t + d * lane + (rev ? 1 : 0);
+      tg = lane < cnt && s < len ? gp[s * a.g_sl] : 0.0f;
+    }
+  };
+
+  // this lane's first address in each tile
+  const E* const xrow = sh.x + r * KR + 8 * g;               // steps 16 i + r
+  const E* const ycol = col_base<KP, 8>(sh.y, g, r);
+  const E* const zcol = col_base<VT, 4 * NT>(sh.z, g, r) + vb;
+  const E* const prow = sh.p + r * PR + 8 * g;
+
+  if (tid < 2) sh.bad[tid] = 0;
+  int par = 0, sub = -1;  // sub >= 0: one row at a time, of a chunk that holds what is not finite
+  int c = 0;
+  if (nch > 0) {
+    chunk_at(0);
+    load_rows(0, n);
+    __syncthreads();
+  }
+  while (c < nch) {
+    uint32_t bad = ty.store(sh.y, tid) | tz.store(sh.z, tid);
+    if (XS) bad |= tx.store(sh.x, tid);
+    if (bad && sub < 0) sh.bad[par] = 1;
+    const int rows = sub < 0 ? n : 1;
+    if (wave == 0) {
+      double G = lane < rows ? (double)clamp_g(tg) * 1.4426950408889634 : 0.0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const double up = __shfl_up(G, d);
+        if (lane >= d) G += up;
+      }
+      const double GC = __shfl(G, 63);
+      if (lane < C) {
+        const int q = place_in(lane);
+        const float hi_ = (float)G, lo_ = (float)(G - (double)hi_);
+        sh.gh[lane] = hi_;
+        sh.gl[lane] = lo_;
+        sh.ph[q] = hi_;
+        sh.pl[q] = lo_;
+        sh.er[lane] = exp2_of(G) * job.rscale;
+        sh.ew[q] = exp2_of(GC - G) * job.wscale;
+      }
+      if (lane == 0) sh.ec = exp2_of(GC);
+    }
+    __syncthreads();
+    if (sub < 0 && sh.bad[par]) {
+      // A product's zero weight does not silence an infinity or a NaN: walk this
+      // chunk a row at a time, so that a step only meets those at or before it.
+      __syncthreads();
+      sub = 0;
+      load_rows(0, 1);
+      continue;
+    }
+    if (tid == 0) sh.bad[par ^ 1] = 0;
+    par ^= 1;
+
+    const bool single = sub >= 0, ends = sub < 0 || sub == n - 1;
+    // rows of this pass: cnt, the first of them step tfirst, the next tstep on
+    const int cnt = single ? 1 : n, crow = single ? sub : 0;
+    const int tfirst = rev ? t0 + n - 1 - crow : t0 + crow, tstep = rev ? -1 : 1;
+    const int reached = rev ? t0 : t0 + n;  // after the chunk the state stands before this step
+    // what comes next; its loads fly during this pass's products
+    if (ends) {
+      sub = -1;
+      if (++c < nch) {
+        chunk_at(c);
+        load_rows(0, n);
+      }
+    } else {
+      ++sub;
+      load_rows(sub, 1);
+    }
+
+    f4 O[TT][NT];
+    if (XS) {
+      // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
+      const int tt = ST == 4 ? wave : wave & 1, q0 = ST == 4 ? 0 : 16 * (wave >> 1);
+      const int t = tt * 16 + r;
+      f4 acc[ST];
+#pragma unroll
+      for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
+      // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; step_of's terms in st are
+      // constants: 16 (st % 2) + st / 2
+      const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
+      const E* const xr = sh.x + t * KR + 8 * g;
+#pragma unroll
+      for (int p = 0; p < KP / 32; ++p) {
+        const Frag<T> xf = row_frag(xr + 32 * p);
+#pragma unroll
+        for (int st = 0; st < ST; ++st)
+          acc[st] = mma(row_frag(yr + (16 * (st & 1) + (st >> 1)) * KR + 32 * p), xf, acc[st]);
+      }
+      // this lane: step t, places qf .. qf + 4 ST - 1
+      const int qf = q0 + 4 * ST * g;
+      const float ght = sh.gh[t], glt = sh.gl[t];
+      const int sf = step_of(qf);
+      float pv[4 * ST];
+#pragma unroll
+      for (int st = 0; st < ST; ++st) {
+        const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
+        const f4 gl = *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float d = (ght - gh[i]) + (glt - gl[i]);
+          const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d) * job.pscale);
+          pv[4 * st + i] = sf + 16 * (st & 1) + (st >> 1) + 4 * i <= t ? e : 0.0f;
+        }
+      }
+      E* const pw = sh.p + t * PR + qf;
+      if constexpr (T::SPLIT) {
+#pragma unroll
+        for (int half = 0; half < ST / 2; ++half) {
+          Frag<T> f[NS];
+          parts_of<NS>(pv + 8 * half, f);
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+            *reinterpret_cast<s8*>(pw + i * C * PR + 8 * half) = f[i].v;
+        }
+      } else {
+        *reinterpret_cast<f4*>(pw) = f4{pv[0], pv[1], pv[2], pv[3]};
+      }
+
+      // X S
+#pragma unroll
+      for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < KP / 32; ++p) {
+        Frag<T> sfr[NT][NS];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = S[2 * p][nt][i];
+            x[4 + i] = S[2 * p + 1][nt][i];
+          }
+          parts_of<NS>(x, sfr[nt]);
+        }
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+          const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sfr[nt][q], xf, O[i][nt]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const float er = sh.er[i * 16 + r];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
+      }
+    }
+
+    // S <- e^{G_C} S + Y^T (weighted Z)
+    const float ec = sh.ec;
+    if (MODE == CARRY) seg_decay *= ec;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
+#pragma unroll
+    for (int sb = 0; sb < SB; ++sb) {
+      Frag<T> wf[NT][T::NW];
+      float ew[8];
+      *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
+      *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x[8];
+        widen(col_frag<VT>(zcol + 32 * sb * VR + 4 * nt), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= ew[j];
+        parts_of<T::NW>(x, wf[nt]);
+        if constexpr (T::SPLIT) {
+          if (single) {  // an infinity is its first part alone
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (!__builtin_isfinite(x[j])) wf[nt][1].v[j] = wf[nt][2].v[j] = 0;
+          }
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const Frag<T> yf = col_frag<KP>(ycol + 32 * sb * KR + 32 * (kt >> 1) + 4 * (kt & 1));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
+      }
+    }
+    if (single) {
+      // a padded column of Y is zero, and zero times an infinity is not
+      int kk = 8 * g;
+      asm volatile("" : "+v"(kk));
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (kk + 32 * (kt >> 1) + 4 * (kt & 1) + i >= a.KK)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[kt][nt][i] = 0.0f;
+    }
+
+    if (XS) {
+      __syncthreads();  // P is whole
+#pragma unroll
+      for (int sb = 0; sb < SB; ++sb) {
+        Frag<T> zf[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 4 * nt);
+#pragma unroll
+        for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
+#pragma unroll
+          for (int q = NS - 1; q >= 0; --q) {
+            const Frag<T> pf = row_frag(prow + (q * C + i * 16) * PR + 32 * sb);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
+          }
+      }
+
+      // this lane: rows i * 16 + r of the pass, columns vc .. vc + 4 NT - 1
+      const int vc = v0 + vb + 4 * NT * g;
+      const E* ap = nullptr;
+      if (MODE == GRAD)
+        ap = (const E*)job.A.p + b * job.A.sb + pl.first * job.A.sl + h / job.adiv * job.A.sh + vc;
+      const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh + vc;
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const int row = i * 16 + r;
+        const bool live = row < cnt && vc < a.VV;
+        const int64_t t = tfirst + tstep * row;
+        float y[4 * NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[4 * nt + j] = O[i][nt][j];
+        if constexpr (MODE == GRAD) {
+          float d = 0.0f;
+          if (live) {
+            const E* p = ap + t * job.A.sl;
+            if (job.avec) {
+              E e[4 * NT];
+              __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * NT * sizeof(E) < 16 ? 8 : 16),
+                               sizeof(e));
+#pragma unroll
+              for (int j = 0; j < 4 * NT; ++j) d = __builtin_fmaf(y[j], widen1(e[j]), d);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4 * NT; ++j)
+                if (vc + j < a.VV) d = __builtin_fmaf(y[j], widen1(p[j]), d);
+            }
+          }
+          d += __shfl_xor(d, 16);
+          d += __shfl_xor(d, 32);
+          if (g == 0) sh.dots[wave * C + row] = d;
+        }
+        if (live) {
+          const int64_t off = ob + t * job.ol;
+          if (T::SPLIT && !job.out_f32) {
+            uint16_t* op = (uint16_t*)job.out + off;
+            uint32_t u[2 * NT];
+#pragma unroll
+            for (int j = 0; j < 2 * NT; ++j) u[j] = bf16x2_rne(y[2 * j], y[2 * j + 1]);
+            if (job.ovec) {
+              __builtin_memcpy(__builtin_assume_aligned(op, 8 * NT), u, 8 * NT);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4 * NT; ++j)
+                if (vc + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
+            }
+          } else {
+            float* op = (float*)job.out + off;
+            if (job.ovec) {
+              __builtin_memcpy(__builtin_assume_aligned(op, 16), y, 16 * NT);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4 * NT; ++j)
+                if (vc + j < a.VV) op[j] = y[j];
+            }
+          }
+        }
+      }
+      if constexpr (MODE == GRAD) {
+        if (job.anchors && ends && reached > 0 && reached < len && reached % ANCHOR == 0)
+          store_state(anchor_at(reached / ANCHOR - 1), 1.0f);
+      }
+    }
+    __syncthreads();  // the tiles are free
+    if constexpr (MODE == GRAD) {
+      if (wave == 0 && lane < cnt) {
+        float d = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) d += sh.dots[q * C + lane];
+        job.dots[((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst +
+                 tstep * lane] = d;
+      }
+    }
+  }
+
+  if (MODE == CARRY) {
+    store_state(job.carry + (slot * a.H + h) * a.KV, 1.0f);
+    if (tile == 0 && tid == 0) job.decay[slot * a.H + h] = seg_decay;
+  } else if (final_seg) {
+    // backwards, the initial state reaches the first step through its decay
+    if (job.last)
+      store_state(job.last + (pl.n * a.H + h) * a.KV,
+                  rev && len > 0 ? exp2_of((double)clamp_g(gp[0]) * 1.4426950408889634) : 1.0f);
+    if (MODE == GRAD && job.anchors && job.last_anchor && len > 0)
+      store_state(anchor_at((len + ANCHOR - 1) / ANCHOR - 1), 1.0f);
+  }
+}
+
+template <class T, int KP, int NT>
+int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
+  const dim3 grid((unsigned)wgs), block(256);
+  if (m == CARRY)
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY>), grid, block, 0, st, a);
+  else if (m == GRAD)
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT>), grid, block, 0, st, a);
+  return check_launch("walk_kernel");
+}
+
+// The instance: X's and Y's columns rounded up to 32, 64, 128 or 256; tiles of
+// 64 nt of Z's columns (nt = 1 above 128 columns of Y: the state's registers).
+template <class T>
+int launch_walk(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
+  const int64_t wgs = a.slots * a.H * a.tiles * a.njobs;
+  if (wgs == 0) return SW_OK;
+#define SW_WALK(KP)                                      \
+  return nt == 1 ? launch_walk_at<T, KP, 1>(a, m, wgs, st) \
+                 : launch_walk_at<T, KP, 2>(a, m, wgs, st)
+  if (a.KK <= 32) SW_WALK(32);
+  if (a.KK <= 64) SW_WALK(64);
+  if (a.KK <= 128) SW_WALK(128);
+  return launch_walk_at<T, 256, 1>(a, m, wgs, st);
+#undef SW_WALK
+}
+
+int launch_walk_bf16(const WalkArgs& a, Mode m, int nt, hipStream_t st);
+int launch_walk_f32(const WalkArgs& a, Mode m, int nt, hipStream_t st);
+
+}  // namespace lin
+}  // namespace sw

@@ -2,7 +2,8 @@
  *
  * One METH_FASTCALL function per entry point of include/scanweaver.h, with
  * the entry point's name and arguments: pointers as Python ints (device
- * addresses) or None for NULL, sizes and enums as ints.  Each function only
+ * addresses) or None for NULL, sizes and enums as ints, floats as numbers, and
+ * the host arrays of strides as tuples of ints.  Each function only
  * converts its arguments and calls the entry point with the GIL released;
  * it returns the status (or the string / handle the entry point returns).
  * A ctypes call spends about a microsecond converting seven arguments; this
@@ -19,9 +20,12 @@ typedef union {
   void* p;
   long long l;
   int i;
+  float f;
+  int64_t s[16]; /* strides */
 } Arg;
 
-/* Convert args[0..n) by fmt: 'P' pointer (int or None), 'L' int64, 'I' int. */
+/* Convert args[0..n) by fmt: 'P' pointer (int or None), 'L' int64, 'I' int, 'F' float,
+ * 'a'..'p' a tuple of 1..16 int64. */
 static int parse(PyObject* const* args, Py_ssize_t n, const char* fmt, Arg* out,
                  const char* name) {
   const Py_ssize_t k = (Py_ssize_t)strlen(fmt);
@@ -43,6 +47,20 @@ static int parse(PyObject* const* args, Py_ssize_t n, const char* fmt, Arg* out,
       }
       out[i].p = PyLong_AsVoidPtr(o);
       if (PyErr_Occurred()) return 0;
+    } else if (fmt[i] == 'F') {
+      const double d = PyFloat_AsDouble(o);
+      if (d == -1.0 && PyErr_Occurred()) return 0;
+      out[i].f = (float)d;
+    } else if (fmt[i] >= 'a') {
+      const Py_ssize_t m = fmt[i] - 'a' + 1;
+      if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != m) {
+        PyErr_Format(PyExc_TypeError, "%s: argument %zd must be a tuple of %zd ints", name, i, m);
+        return 0;
+      }
+      for (Py_ssize_t j = 0; j < m; ++j) {
+        out[i].s[j] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, j));
+        if (out[i].s[j] == -1 && PyErr_Occurred()) return 0;
+      }
     } else {
       if (!PyLong_Check(o)) {
         PyErr_Format(PyExc_TypeError, "%s: argument %zd must be an int", name, i);
@@ -79,6 +97,8 @@ static int parse(PyObject* const* args, Py_ssize_t n, const char* fmt, Arg* out,
 #define AP(k) v[k].p
 #define AL(k) v[k].l
 #define AI(k) v[k].i
+#define AF(k) v[k].f
+#define AS(k) v[k].s
 
 SW_CALL(sw_affine_scan, "PPPPLLL", 7, sw_affine_scan(AP(0), AP(1), AP(2), AP(3), AL(4), AL(5), AL(6)))
 SW_CALL(sw_affine_scan_i32, "PPPPLLL", 7,
@@ -130,6 +150,34 @@ SW_CALL(sw_selective_scan_bwd_ex, "PPPPPPPPPPPPPPPPPPPPPPLLLLIIIIPL", 32,
                               AP(11), AP(12), AP(13), AP(14), AP(15), AP(16), AP(17), AP(18), AP(19),
                               AP(20), AP(21), AL(22), AL(23), AL(24), AL(25), AI(26), AI(27), AI(28),
                                  AI(29), AP(30), AL(31)))
+
+SW_CALL(sw_linear_attn_fwd, "PPPPPPPPLLLLLLLlIIFPL", 21,
+        sw_linear_attn_fwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AL(8), AL(9), AL(10),
+                           AL(11), AL(12), AL(13), AL(14), AS(15), AI(16), AI(17), AF(18), AP(19),
+                           AL(20)))
+SW_CALL(sw_linear_attn_bwd, "PPPPPPPPPPPPPLLLLLLLoIIFPL", 26,
+        sw_linear_attn_bwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AP(8), AP(9), AP(10),
+                           AP(11), AP(12), AL(13), AL(14), AL(15), AL(16), AL(17), AL(18), AL(19),
+                           AS(20), AI(21), AI(22), AF(23), AP(24), AL(25)))
+SW_CALL(sw_linear_attn_step, "PPPPPPPLLLLLLhIIF", 17,
+        sw_linear_attn_step(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AL(7), AL(8), AL(9), AL(10),
+                            AL(11), AL(12), AS(13), AI(14), AI(15), AF(16)))
+
+/* A query of sizes: int64 in, int64 out. */
+#define SW_QUERY(NAME, FMT, NARGS, CALL)                                                       \
+  static PyObject* py_##NAME(PyObject* self, PyObject* const* args, Py_ssize_t nargs) { \
+    (void)self;                                                                         \
+    Arg v[NARGS];                                                                       \
+    if (!parse(args, nargs, FMT, v, #NAME)) return NULL;                                \
+    return PyLong_FromLongLong(CALL);                                                   \
+  }
+
+SW_QUERY(sw_linear_attn_fwd_workspace, "LLLLLLLIII", 10,
+         sw_linear_attn_fwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8),
+                                      AI(9)))
+SW_QUERY(sw_linear_attn_bwd_workspace, "LLLLLLLIII", 10,
+         sw_linear_attn_bwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8),
+                                      AI(9)))
 
 static PyObject* py_sw_selective_scan_fwd_workspace(PyObject* self, PyObject* const* args,
                                                     Py_ssize_t nargs) {
@@ -218,6 +266,11 @@ static PyMethodDef methods[] = {
     FAST(sw_selective_scan_bwd_ex),
     FAST(sw_selective_scan_bwd_workspace),
     FAST(sw_selective_scan_plan),
+    FAST(sw_linear_attn_fwd),
+    FAST(sw_linear_attn_fwd_workspace),
+    FAST(sw_linear_attn_bwd),
+    FAST(sw_linear_attn_bwd_workspace),
+    FAST(sw_linear_attn_step),
     FAST(sw_set_stream),
     NOARG(sw_get_stream),
     FAST(sw_status_string),
