@@ -521,6 +521,67 @@ int sw_linear_attn_step(const void* q, const void* k, const void* v, const float
                         int64_t V, int64_t pool, const int64_t* strides, int dtype, int flags,
                         float scale);
 
+/*
+ * The norm before a block, with the residual addition and its scale:
+ *   R' = R + res_scale * x      (rounded to res_dtype, in residual_out)
+ *   y  = weight * R' / sqrt(mean(R'^2) + eps)
+ * over M rows of D columns, 1 <= D <= 16384.  y is the norm of R' as stored.
+ *   x, y : dtype     residual, residual_out : res_dtype (dtype, or fp32)
+ *   weight, res_scale : (D) fp32; res_scale may be NULL (ones)
+ * residual NULL: y is the norm of x; residual_out and res_scale are NULL then.
+ * x and residual have their rows x_stride, residual_stride elements apart; the
+ * outputs are dense.  Sums are fp32, outputs rounded once.  One launch; can be
+ * captured.  Other conventions as above.
+ */
+int sw_residual_norm_fwd(const void* x, const void* residual, const float* weight,
+                         const float* res_scale, void* y, void* residual_out, int64_t M, int64_t D,
+                         int64_t x_stride, int64_t residual_stride, int dtype, int res_dtype,
+                         float eps);
+
+/*
+ * Backward: given dy, dres (of y and residual_out; dres may be NULL) and
+ * residual_out (x itself, with res_dtype = dtype, where there was no residual),
+ * with n = R' / rms:
+ *   dR' = dres + (weight dy - n mean(weight dy n)) / rms
+ *   dresidual = dR', dx = res_scale * dR', dweight = sum dy n, dres_scale = sum x dR'
+ * dx and dresidual may be NULL (not written; without res_scale and with equal
+ * types they are the same values); x is needed with res_scale only.  The sums
+ * over rows are added in a fixed order.  workspace: 16-byte aligned, at least
+ * sw_norm_bwd_workspace(M, D, D, 1, or 2 with res_scale) bytes, or NULL: from
+ * the device's stream-ordered pool for the call (no capture then).
+ */
+int sw_residual_norm_bwd(const void* dy, const void* dres, const void* residual_out,
+                         const float* weight, const void* x, const float* res_scale, void* dx,
+                         void* dresidual, float* dweight, float* dres_scale, int64_t M, int64_t D,
+                         int64_t dy_stride, int64_t dres_stride, int64_t residual_out_stride,
+                         int64_t x_stride, int dtype, int res_dtype, float eps, void* workspace,
+                         int64_t workspace_bytes);
+int64_t sw_norm_bwd_workspace(int64_t M, int64_t D, int64_t width, int grads);
+
+/*
+ * The norm after a block's mixer, with its gate, over groups of `group` columns
+ * (group = D: the whole row; the width of a head: a norm for each head):
+ *   y = weight * u / sqrt(mean_group(u^2) + eps),  u = x silu(z)
+ *   with SW_GATE_AFTER:  y = weight * x / sqrt(mean_group(x^2) + eps) * silu(z)
+ * x, z, y : M rows of D of dtype, D a multiple of group, 1 <= group <= 16384; z
+ * NULL: no gate.  weight : (D) fp32.  Rows of x and z lie x_stride, z_stride
+ * elements apart.  Otherwise as sw_residual_norm_fwd.
+ */
+enum { SW_GATE_AFTER = 1 /* the gate multiplies the normed values */ };
+int sw_gated_norm_fwd(const void* x, const void* z, const float* weight, void* y, int64_t M,
+                      int64_t D, int64_t group, int64_t x_stride, int64_t z_stride, int dtype,
+                      int flags, float eps);
+
+/*
+ * Its gradients: dx, dz (with z) dense, of dtype; dweight (D) fp32, its sums over
+ * the rows in a fixed order.  workspace as for sw_residual_norm_bwd, of
+ * sw_norm_bwd_workspace(M, D, group, 1) bytes.
+ */
+int sw_gated_norm_bwd(const void* dy, const void* x, const void* z, const float* weight, void* dx,
+                      void* dz, float* dweight, int64_t M, int64_t D, int64_t group,
+                      int64_t dy_stride, int64_t x_stride, int64_t z_stride, int dtype, int flags,
+                      float eps, void* workspace, int64_t workspace_bytes);
+
 /* Stream used by the calling thread's subsequent calls (a hipStream_t;
  * NULL = the null stream).  Always SW_OK. */
 int sw_set_stream(void* hip_stream);

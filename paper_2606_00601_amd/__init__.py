@@ -32,6 +32,9 @@ C ABI one function per entry point; ``lib()`` is the same ABI through ctypes.
   sequences, returning ``(o, h_last)``; ``linear_attn_bwd`` / ``linear_attn_fn``
   are its gradients and the autograd function, ``linear_attn_step(q, k, v, g,
   state)`` one token of each sequence of a batch, the states updated in place.
+* ``residual_norm_fwd(x, weight, residual, ...)`` and ``gated_norm_fwd(x, z,
+  weight, ...)``: the norms before and after a block, fused with the residual
+  addition and its scale and with the block's gate; ``_bwd`` and ``_fn`` as above.
 * ``selective_scan_plan(B, D, N, L, ...)``: the kernels, segments and form
   the fused forward would take for those sizes, without launching anything.
 """
@@ -43,12 +46,16 @@ from ._bind import _need, _on, _ptr
 from ._lib import (SW_DELTA_SOFTPLUS, SW_DTYPE_BF16, SW_DTYPE_F32,  # noqa: F401
                    ScanWeaverError, check, fast, last_error, lib, status_string)
 from ._linear import linear_attn_bwd, linear_attn_fn, linear_attn_fwd, linear_attn_step
+from ._norm import (gated_norm_bwd, gated_norm_fn, gated_norm_fwd, residual_norm_bwd,
+                    residual_norm_fn, residual_norm_fwd)
 
 __all__ = ["last_launch", "selective_scan_plan", "affine_scan", "affine_scan_noalloc", "affine_scan_i32", "affine_scan_schedule", "affine_scan_schedule_i32",
            "affine_scan_proj", "affine_scan_proj_i32",
            "selective_scan_fwd", "selective_scan_fwd_schedule", "selective_scan_bwd", "new_ckpt",
            "selective_scan_fn",
            "linear_attn_fwd", "linear_attn_bwd", "linear_attn_fn", "linear_attn_step",
+           "residual_norm_fwd", "residual_norm_bwd", "residual_norm_fn",
+           "gated_norm_fwd", "gated_norm_bwd", "gated_norm_fn",
            "ScanWeaverError",
            "version"]
 

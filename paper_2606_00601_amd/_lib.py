@@ -20,6 +20,7 @@ SW_DTYPE_F32 = 0
 SW_DTYPE_BF16 = 1
 SW_DELTA_SOFTPLUS = 1
 SW_LINEAR_G_HEAD = 1
+SW_GATE_AFTER = 1
 SW_SCHED_DEFAULT = 0
 SW_SCHED_BLELLOCH = 1
 
@@ -52,6 +53,11 @@ SIGNATURES = {
     "sw_linear_attn_bwd": (_int, [_vp] * 13 + [_i64] * 7 + [_strides, _int, _int, _f32, _vp, _i64]),
     "sw_linear_attn_bwd_workspace": (_i64, [_i64] * 7 + [_int] * 3),
     "sw_linear_attn_step": (_int, [_vp] * 7 + [_i64] * 6 + [_strides, _int, _int, _f32]),
+    "sw_residual_norm_fwd": (_int, [_vp] * 6 + [_i64] * 4 + [_int] * 2 + [_f32]),
+    "sw_residual_norm_bwd": (_int, [_vp] * 10 + [_i64] * 6 + [_int] * 2 + [_f32, _vp, _i64]),
+    "sw_gated_norm_fwd": (_int, [_vp] * 4 + [_i64] * 5 + [_int] * 2 + [_f32]),
+    "sw_gated_norm_bwd": (_int, [_vp] * 7 + [_i64] * 6 + [_int] * 2 + [_f32, _vp, _i64]),
+    "sw_norm_bwd_workspace": (_i64, [_i64] * 3 + [_int]),
     "sw_set_stream": (_int, [_vp]),
     "sw_get_stream": (_vp, []),
     "sw_status_string": (ctypes.c_char_p, [_int]),

@@ -163,6 +163,19 @@ SW_CALL(sw_linear_attn_step, "PPPPPPPLLLLLLhIIF", 17,
         sw_linear_attn_step(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AL(7), AL(8), AL(9), AL(10),
                             AL(11), AL(12), AS(13), AI(14), AI(15), AF(16)))
 
+SW_CALL(sw_residual_norm_fwd, "PPPPPPLLLLIIF", 13,
+        sw_residual_norm_fwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AL(6), AL(7), AL(8), AL(9), AI(10),
+                             AI(11), AF(12)))
+SW_CALL(sw_residual_norm_bwd, "PPPPPPPPPPLLLLLLIIFPL", 21,
+        sw_residual_norm_bwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AP(8), AP(9), AL(10),
+                             AL(11), AL(12), AL(13), AL(14), AL(15), AI(16), AI(17), AF(18), AP(19), AL(20)))
+SW_CALL(sw_gated_norm_fwd, "PPPPLLLLLIIF", 12,
+        sw_gated_norm_fwd(AP(0), AP(1), AP(2), AP(3), AL(4), AL(5), AL(6), AL(7), AL(8), AI(9), AI(10),
+                          AF(11)))
+SW_CALL(sw_gated_norm_bwd, "PPPPPPPLLLLLLIIFPL", 18,
+        sw_gated_norm_bwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AL(7), AL(8), AL(9), AL(10),
+                          AL(11), AL(12), AI(13), AI(14), AF(15), AP(16), AL(17)))
+
 /* A query of sizes: int64 in, int64 out. */
 #define SW_QUERY(NAME, FMT, NARGS, CALL)                                                       \
   static PyObject* py_##NAME(PyObject* self, PyObject* const* args, Py_ssize_t nargs) { \
@@ -175,6 +188,7 @@ SW_CALL(sw_linear_attn_step, "PPPPPPPLLLLLLhIIF", 17,
 SW_QUERY(sw_linear_attn_fwd_workspace, "LLLLLLLIII", 10,
          sw_linear_attn_fwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8),
                                       AI(9)))
+SW_QUERY(sw_norm_bwd_workspace, "LLLI", 4, sw_norm_bwd_workspace(AL(0), AL(1), AL(2), AI(3)))
 SW_QUERY(sw_linear_attn_bwd_workspace, "LLLLLLLIII", 10,
          sw_linear_attn_bwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8),
                                       AI(9)))
@@ -271,6 +285,11 @@ static PyMethodDef methods[] = {
     FAST(sw_linear_attn_bwd),
     FAST(sw_linear_attn_bwd_workspace),
     FAST(sw_linear_attn_step),
+    FAST(sw_residual_norm_fwd),
+    FAST(sw_residual_norm_bwd),
+    FAST(sw_gated_norm_fwd),
+    FAST(sw_gated_norm_bwd),
+    FAST(sw_norm_bwd_workspace),
     FAST(sw_set_stream),
     NOARG(sw_get_stream),
     FAST(sw_status_string),
