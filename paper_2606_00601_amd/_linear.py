@@ -28,7 +28,7 @@ def _need_rows(t, name, dtype, shape):
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
     st = t.stride()
-    if shape[-1] > 1 and st[-1] != 1:
+    if shape[-1] > 1 and st[-1] != 1 and t.numel():
         raise ValueError(f"{name} must be contiguous along its last dimension")
     return tuple(s if n > 1 else 0 for s, n in zip(st[:-1], shape[:-1]))
 
