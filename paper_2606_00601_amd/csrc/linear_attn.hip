@@ -219,14 +219,14 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   p.nt_k = nt_of(a.V, a.K);
   p.tiles_v = (a.V + 64 * p.nt_v - 1) / (64 * p.nt_v);
   p.tiles_k = (a.K + 64 * p.nt_k - 1) / (64 * p.nt_k);
-  const int64_t per_step = a.H * (bwd ? 2 * p.tiles_k : p.tiles_v);  // workgroups of one sequence
-  const int64_t steps = a.B * a.L, longest = a.L;
-  const int64_t want = 2 * (int64_t)cus;
-  int64_t lseg = (steps * per_step + want - 1) / want;
-  lseg = (lseg + CHUNK - 1) / CHUNK * CHUNK;
-  if (lseg < 4 * CHUNK) lseg = 4 * CHUNK;
-  // a cut into two does not pay: the first walk costs about half the second
-  if (lseg * 3 / 2 >= longest) lseg = (longest + CHUNK - 1) / CHUNK * CHUNK;
+  const int64_t per_seq_wgs = a.H * (bwd ? 2 * p.tiles_k : p.tiles_v);
+  const int64_t longest = a.L, chunks = (longest + CHUNK - 1) / CHUNK;
+  const int64_t want = 2 * (int64_t)cus, whole = a.B * per_seq_wgs;
+  // the most parts that still run side by side: one more would wait for a whole round
+  int64_t parts = whole > 0 ? want / whole : 1;
+  if (parts > chunks / 4) parts = chunks / 4;
+  if (parts < 3) parts = 1;  // a cut into two does not pay: the first walk costs about half the second
+  int64_t lseg = (chunks + parts - 1) / parts * CHUNK;
   if (lseg < CHUNK) lseg = CHUNK;
   p.lseg = lseg;
   p.cut = lseg < longest;
@@ -270,11 +270,12 @@ Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool dh_last) 
   return l;
 }
 
-// Whole 16-byte granules: the address, the strides and the width allow them.
+// Whole 16-byte granules: the address, the strides and the width allow them, and
+// a chunk's rows follow each other within a buffer load's offsets.
 bool rows_vec(const HeadRows& x, int64_t width, bool bf16) {
   const int64_t G = bf16 ? 8 : 4;
   return (uintptr_t)x.p % 16 == 0 && x.sb % G == 0 && x.sl % G == 0 && x.sh % G == 0 &&
-         width % G == 0;
+         width % G == 0 && x.sl >= width && x.sl < ((int64_t)1 << 22);
 }
 
 WalkArgs walk_args(const LinAttnArgs& a, const Plan& p) {
@@ -308,13 +309,17 @@ Job make_job(const LinAttnArgs& a, const Role& X, const Role& Y, const Role& Z, 
   j.X = X.rows;
   j.Y = Y.rows;
   j.Z = Z.rows;
+  if (a.L <= 1) {  // the only step's stride says nothing
+    j.X.sl = j.Y.sl = cw;
+    j.Z.sl = zw;
+  }
   j.xdiv = X.div;
   j.ydiv = Y.div;
   j.zdiv = Z.div;
   j.adiv = 1;
-  j.xvec = rows_vec(X.rows, cw, a.bf16);
-  j.yvec = rows_vec(Y.rows, cw, a.bf16);
-  j.zvec = rows_vec(Z.rows, zw, a.bf16);
+  j.xvec = rows_vec(j.X, cw, a.bf16);
+  j.yvec = rows_vec(j.Y, cw, a.bf16);
+  j.zvec = rows_vec(j.Z, zw, a.bf16);
   j.skk = swapped ? 1 : a.V;
   j.svv = swapped ? a.V : 1;
   j.pscale = a.scale;

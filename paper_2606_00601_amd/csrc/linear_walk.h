@@ -125,6 +125,7 @@ __device__ __forceinline__ float exp2_of(double x) {
 }
 
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
@@ -256,56 +257,70 @@ __device__ __forceinline__ void widen(const Frag<F32>& f, float* x) {
 __device__ __forceinline__ float widen1(uint16_t e) { return bf16_one(e); }
 __device__ __forceinline__ float widen1(float e) { return e; }
 
-// Bit 15 and 31 (bf16) or 31 (fp32) set where an element is not finite.
-template <class T>
-__device__ __forceinline__ uint32_t nonfinite(uint4 u) {
-  if (T::SPLIT) {
-    const uint32_t m = 0x7f807f80u, o = 0x00800080u;
-    return (((u.x & m) + o) | ((u.y & m) + o) | ((u.z & m) + o) | ((u.w & m) + o)) & 0x80008000u;
-  }
-  const uint32_t m = 0x7f800000u, o = 0x00800000u;
-  return (((u.x & m) + o) | ((u.y & m) + o) | ((u.z & m) + o) | ((u.w & m) + o)) & 0x80000000u;
+// Adds zero times each element of a granule to acc: NaN once one is not finite.
+__device__ __forceinline__ float check_finite(u4 u, float acc, Bf16*) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  const b2 zero = {(__bf16)0.0f, (__bf16)0.0f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, (uint32_t)u[j]), zero, acc, false);
+  return acc;
+}
+__device__ __forceinline__ float check_finite(u4 u, float acc, F32*) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc = __builtin_fmaf(__uint_as_float(u[j]), 0.0f, acc);
+  return acc;
 }
 
-// One thread's granules of a C x W tile: rows [0, n) of `rows` (row i lies
-// i * step elements on), columns below width; zero elsewhere.
-template <class T, int W>
+// One thread's granules of a C x W tile of rows `step` elements apart, `rows` the
+// one lowest in memory: row i of the tile is row i there (rev: row n - 1 - i),
+// rows from n and columns from width are zero.
+// VEC: 16-byte buffer loads without a branch, so that they stay in flight until
+// the granules are stored.  What lies outside the tile has an offset past the
+// buffer's end (rows from n do since a row is no longer than a step; backwards
+// their offsets are negative) and reads zero.
+template <class T, int W, bool VEC>
 struct Tile {
   static constexpr int NG = W / T::G, PER = T::C * NG / 256, RPG = 256 / NG;
   static_assert(PER >= 1 && T::C * NG % 256 == 0, "whole granules per thread");
-  uint4 u[PER];
-  __device__ __forceinline__ void load(const typename T::E* rows, int64_t step, int n, int width,
-                                       bool vec, int tid) {
+  typedef typename T::E E;
+  u4 u[PER];
+  __device__ __forceinline__ void load(const E* rows, int64_t step, int n, bool rev, int width,
+                                       int tid) {
+    asm volatile("" : "+v"(tid));  // offsets worked out here, not kept across the walk
     const int row = tid / NG, col = tid % NG * T::G;
-    const typename T::E* p = rows + row * step + col;
-    if (vec) {
+    if constexpr (VEC) {
+      const int st = (int)step * (int)sizeof(E);
+      const int end = n > 0 ? (n - 1) * st + (width < W ? width : W) * (int)sizeof(E) : 0;
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)rows, 0, end, 0x00020000);
+      uint32_t off = (uint32_t)((rev ? n - 1 - row : row) * st) +
+                     (col < width ? col * (uint32_t)sizeof(E) : 0x40000000u);
+      const int next = (rev ? -RPG : RPG) * st;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        u[i] = make_uint4(0, 0, 0, 0);
-        if (row + i * RPG < n && col < width) u[i] = *reinterpret_cast<const uint4*>(p);
-        p += RPG * step;
+        u[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+        off += next;
       }
     } else {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        typename T::E e[T::G];
+        const int r = row + i * RPG;
+        const E* p = rows + (rev ? n - 1 - r : r) * step + col;
+        E e[T::G];
 #pragma unroll
-        for (int j = 0; j < T::G; ++j)
-          e[j] = row + i * RPG < n && col + j < width ? p[j] : (typename T::E)0;
+        for (int j = 0; j < T::G; ++j) e[j] = r < n && col + j < width ? p[j] : (E)0;
         __builtin_memcpy(&u[i], e, 16);
-        p += RPG * step;
       }
     }
   }
-  __device__ __forceinline__ uint32_t store(typename T::E* lds, int tid) const {
-    uint32_t bad = 0;
-    typename T::E* p = lds + tid / NG * ROW<T, W> + tid % NG * T::G;
+  __device__ __forceinline__ float store(E* lds, int tid, float acc) const {
+    E* p = lds + tid / NG * ROW<T, W> + tid % NG * T::G;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      *reinterpret_cast<uint4*>(p + i * RPG * ROW<T, W>) = u[i];
-      bad |= nonfinite<T>(u[i]);
+      *reinterpret_cast<u4*>(p + i * RPG * ROW<T, W>) = u[i];
+      acc = check_finite(u[i], acc, (T*)nullptr);
     }
-    return bad;
+    return acc;
   }
 };
 
@@ -327,8 +342,9 @@ struct Shared {
   float ph[C], pl[C];  // by place: gh and gl
   float ew[C];         // by place: wscale 2^(G_C - G)
   float dots[MODE == GRAD ? 4 * C : 4];
+  float g1[C];         // by step: its own log2 decay
   float ec;            // 2^G_C
-  uint32_t bad[2];
+  uint32_t bad[2];     // the chunk (of odd or even number) holds what is not finite
 };
 
 // Waves per SIMD: what the accumulators of S, out and the loads in flight leave
@@ -337,7 +353,7 @@ constexpr int walk_waves(int KP, int NT, Mode m) {
   return KP >= 256 ? 1 : KP <= 64 && NT == 1 && m != GRAD ? 3 : 2;
 }
 
-template <class T, int KP, int NT, Mode MODE>
+template <class T, int KP, int NT, Mode MODE, bool VEC>
 __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(WalkArgs a) {
   typedef typename T::E E;
   typedef Shared<T, KP, NT, MODE> Sh;
@@ -416,25 +432,21 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   }
   float seg_decay = 1.0f;
 
-  Tile<T, KP> tx, ty;
-  Tile<T, VT> tz;
+  Tile<T, KP, VEC> tx, ty;
+  Tile<T, VT, VEC> tz;
   float tg = 0.0f;
-  int t0 = 0, n = 0;  // the chunk's steps: t0 .. t0 + n - 1
-  auto chunk_at = [&](int c) {
+  int t0 = 0, n = 0;  // a chunk's steps: t0 .. t0 + n - 1; its row i is the walk's i-th of them
+  auto load_chunk = [&](int c) __attribute__((always_inline)) {  // c = nch: nothing
     t0 = lo + (rev ? nch - 1 - c : c) * C;
-    n = hi - t0 < C ? hi - t0 : C;
-  };
-  // rows [i0, i0 + cnt) of the chunk, in the walk's order
-  auto load_rows = [&](int i0, int cnt) {
-    const int64_t t = rev ? t0 + n - 1 - i0 : t0 + i0;
-    const int64_t d = rev ? -1 : 1;
-    if (XS) tx.load(X + t * job.X.sl, d * job.X.sl, cnt, a.KK, job.xvec, tid);
-    ty.load(Y + t * job.Y.sl, d * job.Y.sl, cnt, a.KK, job.yvec, tid);
-    tz.load(Z + t * job.Z.sl, d * job.Z.sl, cnt, a.VV - v0, job.zvec, tid);
+    n = c >= nch ? 0 : hi - t0 < C ? hi - t0 : C;
+    const int64_t t = c >= nch ? lo : t0;
+    if (XS) tx.load(X + t * job.X.sl, job.X.sl, n, rev, a.KK, tid);
+    ty.load(Y + t * job.Y.sl, job.Y.sl, n, rev, a.KK, tid);
+    tz.load(Z + t * job.Z.sl, job.Z.sl, n, rev, a.VV - v0, tid);
     if (wave == 0) {
       // backwards, a step's decay is that of the step after it in time; none at the end
-      const int64_t s = t + d * lane + (rev ? 1 : 0);
-      tg = lane < cnt && s < len ? gp[s * a.g_sl] : 0.0f;
+      const int64_t s = rev ? t + n - lane : t + lane;
+      tg = lane < n && s < len ? gp[s * a.g_sl] : 0.0f;
     }
   };
 
@@ -443,22 +455,23 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   const E* const ycol = col_base<KP, 8>(sh.y, g, r);
   const E* const zcol = col_base<VT, 4 * NT>(sh.z, g, r) + vb;
   const E* const prow = sh.p + r * PR + 8 * g;
+  const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh;
+  const E* ap = nullptr;
+  if (MODE == GRAD)
+    ap = (const E*)job.A.p + b * job.A.sb + pl.first * job.A.sl + h / job.adiv * job.A.sh;
 
   if (tid < 2) sh.bad[tid] = 0;
-  int par = 0, sub = -1;  // sub >= 0: one row at a time, of a chunk that holds what is not finite
-  int c = 0;
   if (nch > 0) {
-    chunk_at(0);
-    load_rows(0, n);
+    load_chunk(0);
     __syncthreads();
   }
-  while (c < nch) {
-    uint32_t bad = ty.store(sh.y, tid) | tz.store(sh.z, tid);
-    if (XS) bad |= tx.store(sh.x, tid);
-    if (bad && sub < 0) sh.bad[par] = 1;
-    const int rows = sub < 0 ? n : 1;
+  for (int c = 0; c < nch; ++c) {
+    float fin = ty.store(sh.y, tid, tz.store(sh.z, tid, 0.0f));
+    if (XS) fin = tx.store(sh.x, tid, fin);
+    if (fin != fin) sh.bad[c & 1] = 1;
     if (wave == 0) {
-      double G = lane < rows ? (double)clamp_g(tg) * 1.4426950408889634 : 0.0;
+      const double g1 = (double)clamp_g(tg) * 1.4426950408889634;
+      double G = lane < n ? g1 : 0.0;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const double up = __shfl_up(G, d);
@@ -474,255 +487,276 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         sh.pl[q] = lo_;
         sh.er[lane] = exp2_of(G) * job.rscale;
         sh.ew[q] = exp2_of(GC - G) * job.wscale;
+        sh.g1[lane] = exp2_of(g1);
       }
       if (lane == 0) sh.ec = exp2_of(GC);
     }
     __syncthreads();
-    if (sub < 0 && sh.bad[par]) {
-      // A product's zero weight does not silence an infinity or a NaN: walk this
-      // chunk a row at a time, so that a step only meets those at or before it.
-      __syncthreads();
-      sub = 0;
-      load_rows(0, 1);
-      continue;
-    }
-    if (tid == 0) sh.bad[par ^ 1] = 0;
-    par ^= 1;
+    const bool bad = sh.bad[c & 1];
+    if (tid == 0) sh.bad[(c + 1) & 1] = 0;
 
-    const bool single = sub >= 0, ends = sub < 0 || sub == n - 1;
-    // rows of this pass: cnt, the first of them step tfirst, the next tstep on
-    const int cnt = single ? 1 : n, crow = single ? sub : 0;
-    const int tfirst = rev ? t0 + n - 1 - crow : t0 + crow, tstep = rev ? -1 : 1;
+    // rows of this chunk: cnt, the first of them step tfirst, the next tstep on
+    const int cnt = n, tfirst = rev ? t0 + n - 1 : t0, tstep = rev ? -1 : 1;
     const int reached = rev ? t0 : t0 + n;  // after the chunk the state stands before this step
-    // what comes next; its loads fly during this pass's products
-    if (ends) {
-      sub = -1;
-      if (++c < nch) {
-        chunk_at(c);
-        load_rows(0, n);
-      }
-    } else {
-      ++sub;
-      load_rows(sub, 1);
-    }
 
-    f4 O[TT][NT];
-    if (XS) {
-      // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
-      const int tt = ST == 4 ? wave : wave & 1, q0 = ST == 4 ? 0 : 16 * (wave >> 1);
-      const int t = tt * 16 + r;
-      f4 acc[ST];
-#pragma unroll
-      for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
-      // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; step_of's terms in st are
-      // constants: 16 (st % 2) + st / 2
-      const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
-      const E* const xr = sh.x + t * KR + 8 * g;
-#pragma unroll
-      for (int p = 0; p < KP / 32; ++p) {
-        const Frag<T> xf = row_frag(xr + 32 * p);
-#pragma unroll
-        for (int st = 0; st < ST; ++st)
-          acc[st] = mma(row_frag(yr + (16 * (st & 1) + (st >> 1)) * KR + 32 * p), xf, acc[st]);
-      }
-      // this lane: step t, places qf .. qf + 4 ST - 1
-      const int qf = q0 + 4 * ST * g;
-      const float ght = sh.gh[t], glt = sh.gl[t];
-      const int sf = step_of(qf);
-      float pv[4 * ST];
-#pragma unroll
-      for (int st = 0; st < ST; ++st) {
-        const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
-        const f4 gl = *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float d = (ght - gh[i]) + (glt - gl[i]);
-          const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d) * job.pscale);
-          pv[4 * st + i] = sf + 16 * (st & 1) + (st >> 1) + 4 * i <= t ? e : 0.0f;
-        }
-      }
-      E* const pw = sh.p + t * PR + qf;
-      if constexpr (T::SPLIT) {
-#pragma unroll
-        for (int half = 0; half < ST / 2; ++half) {
-          Frag<T> f[NS];
-          parts_of<NS>(pv + 8 * half, f);
-#pragma unroll
-          for (int i = 0; i < NS; ++i)
-            *reinterpret_cast<s8*>(pw + i * C * PR + 8 * half) = f[i].v;
-        }
-      } else {
-        *reinterpret_cast<f4*>(pw) = f4{pv[0], pv[1], pv[2], pv[3]};
-      }
-
-      // X S
-#pragma unroll
-      for (int i = 0; i < TT; ++i)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int p = 0; p < KP / 32; ++p) {
-        Frag<T> sfr[NT][NS];
+    if (__builtin_expect(bad, 0)) {
+      // A zero weight does not silence an infinity or a NaN in a product: such a
+      // chunk goes step by step, as the recurrence says, on plain arithmetic.
+#pragma unroll 1
+      for (int i = 0; i < cnt; ++i) {
+        const float a1 = sh.g1[i];
+        int vc = v0 + vb + 4 * NT * (r >> 2) + (r & 3), kg = 8 * g;
+        asm volatile("" : "+v"(vc), "+v"(kg));  // worked out here, not kept across the walk
+        float xy = 0.0f, acc[NT], z[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float x[8];
+          acc[nt] = 0.0f;
+          z[nt] = widen1(sh.z[i * VR + vc - v0 + 4 * nt]);
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int kk = kg + 32 * (kt >> 1) + 4 * (kt & 1) + j;
+            if (kk < a.KK) {
+              const float y = widen1(sh.y[i * KR + kk]);
+              const float x = XS ? widen1(sh.x[i * KR + kk]) : 0.0f;
+              xy = __builtin_fmaf(x, y, xy);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                acc[nt] = __builtin_fmaf(x, S[kt][nt][j], acc[nt]);
+                S[kt][nt][j] = __builtin_fmaf(y, job.wscale * z[nt], a1 * S[kt][nt][j]);
+              }
+            }
+          }
+        if (MODE == CARRY) seg_decay *= a1;
+        if (XS) {
+          const int64_t t = tfirst + tstep * i;
+          xy += __shfl_xor(xy, 16);
+          xy += __shfl_xor(xy, 32);
+          float d = 0.0f;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            acc[nt] += __shfl_xor(acc[nt], 16);
+            acc[nt] += __shfl_xor(acc[nt], 32);
+            const float y = a1 * job.rscale * acc[nt] + job.pscale * xy * z[nt];
+            if (g == 0 && vc + 4 * nt < a.VV) {
+              const int64_t off = ob + t * job.ol + vc + 4 * nt;
+              if (T::SPLIT && !job.out_f32)
+                ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
+              else
+                ((float*)job.out)[off] = y;
+              if (MODE == GRAD) d += y * widen1(ap[t * job.A.sl + vc + 4 * nt]);
+            }
+          }
+          if (MODE == GRAD) {
+#pragma unroll
+            for (int q = 1; q < 16; q <<= 1) d += __shfl_xor(d, q);
+            if (lane == 0) sh.dots[wave * C + i] = d;
+          }
+        }
+      }
+      load_chunk(c + 1);
+    } else {
+      f4 O[TT][NT];
+      if (XS) {
+        // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
+        const int tt = ST == 4 ? wave : wave & 1, q0 = ST == 4 ? 0 : 16 * (wave >> 1);
+        const int t = tt * 16 + r;
+        f4 acc[ST];
+#pragma unroll
+        for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
+        // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; step_of's terms in st are
+        // constants: 16 (st % 2) + st / 2
+        const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
+        const E* const xr = sh.x + t * KR + 8 * g;
+#pragma unroll
+        for (int p = 0; p < KP / 32; ++p) {
+          const Frag<T> xf = row_frag(xr + 32 * p);
+#pragma unroll
+          for (int st = 0; st < ST; ++st)
+            acc[st] = mma(row_frag(yr + (16 * (st & 1) + (st >> 1)) * KR + 32 * p), xf, acc[st]);
+        }
+        // this lane: step t, places qf .. qf + 4 ST - 1
+        const int qf = q0 + 4 * ST * g;
+        const float ght = sh.gh[t], glt = sh.gl[t];
+        int ahead = t - step_of(qf);  // steps from the first place's to t
+        asm volatile("" : "+v"(ahead));  // compared here: sixteen masks are not kept
+        float pv[4 * ST];
+#pragma unroll
+        for (int st = 0; st < ST; ++st) {
+          const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
+          const f4 gl = *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            x[i] = S[2 * p][nt][i];
-            x[4 + i] = S[2 * p + 1][nt][i];
+            const float d = (ght - gh[i]) + (glt - gl[i]);
+            const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d) * job.pscale);
+            pv[4 * st + i] = 16 * (st & 1) + (st >> 1) + 4 * i <= ahead ? e : 0.0f;
           }
-          parts_of<NS>(x, sfr[nt]);
+        }
+        E* const pw = sh.p + t * PR + qf;
+        if constexpr (T::SPLIT) {
+#pragma unroll
+          for (int half = 0; half < ST / 2; ++half) {
+            Frag<T> f[NS];
+            parts_of<NS>(pv + 8 * half, f);
+#pragma unroll
+            for (int i = 0; i < NS; ++i)
+              *reinterpret_cast<s8*>(pw + i * C * PR + 8 * half) = f[i].v;
+          }
+        } else {
+          *reinterpret_cast<f4*>(pw) = f4{pv[0], pv[1], pv[2], pv[3]};
+        }
+
+        // X S
+#pragma unroll
+        for (int i = 0; i < TT; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < KP / 32; ++p) {
+          Frag<T> sfr[NT][NS];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[i] = S[2 * p][nt][i];
+              x[4 + i] = S[2 * p + 1][nt][i];
+            }
+            parts_of<NS>(x, sfr[nt]);
+          }
+#pragma unroll
+          for (int i = 0; i < TT; ++i) {
+            const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sfr[nt][q], xf, O[i][nt]);
+          }
         }
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
-          const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
+          const float er = sh.er[i * 16 + r];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sfr[nt][q], xf, O[i][nt]);
+          for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
         }
       }
-#pragma unroll
-      for (int i = 0; i < TT; ++i) {
-        const float er = sh.er[i * 16 + r];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
-      }
-    }
 
-    // S <- e^{G_C} S + Y^T (weighted Z)
-    const float ec = sh.ec;
-    if (MODE == CARRY) seg_decay *= ec;
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
-#pragma unroll
-    for (int sb = 0; sb < SB; ++sb) {
-      Frag<T> wf[NT][T::NW];
-      float ew[8];
-      *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
-      *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float x[8];
-        widen(col_frag<VT>(zcol + 32 * sb * VR + 4 * nt), x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= ew[j];
-        parts_of<T::NW>(x, wf[nt]);
-        if constexpr (T::SPLIT) {
-          if (single) {  // an infinity is its first part alone
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (!__builtin_isfinite(x[j])) wf[nt][1].v[j] = wf[nt][2].v[j] = 0;
-          }
-        }
-      }
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        const Frag<T> yf = col_frag<KP>(ycol + 32 * sb * KR + 32 * (kt >> 1) + 4 * (kt & 1));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
-      }
-    }
-    if (single) {
-      // a padded column of Y is zero, and zero times an infinity is not
-      int kk = 8 * g;
-      asm volatile("" : "+v"(kk));
+      load_chunk(c + 1);  // in flight while the state moves on; earlier, its registers would spill
+
+      // S <- e^{G_C} S + Y^T (weighted Z)
+      const float ec = sh.ec;
+      if (MODE == CARRY) seg_decay *= ec;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (kk + 32 * (kt >> 1) + 4 * (kt & 1) + i >= a.KK)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) S[kt][nt][i] = 0.0f;
-    }
-
-    if (XS) {
-      __syncthreads();  // P is whole
+        for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
 #pragma unroll
       for (int sb = 0; sb < SB; ++sb) {
-        Frag<T> zf[NT];
+        Frag<T> wf[NT][T::NW];
+        float ew[8];
+        *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
+        *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 4 * nt);
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[8];
+          widen(col_frag<VT>(zcol + 32 * sb * VR + 4 * nt), x);
 #pragma unroll
-        for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
+          for (int j = 0; j < 8; ++j) x[j] *= ew[j];
+          parts_of<T::NW>(x, wf[nt]);
+        }
 #pragma unroll
-          for (int q = NS - 1; q >= 0; --q) {
-            const Frag<T> pf = row_frag(prow + (q * C + i * 16) * PR + 32 * sb);
+        for (int kt = 0; kt < KT; ++kt) {
+          const Frag<T> yf = col_frag<KP>(ycol + 32 * sb * KR + 32 * (kt >> 1) + 4 * (kt & 1));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
-          }
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
+        }
       }
 
-      // this lane: rows i * 16 + r of the pass, columns vc .. vc + 4 NT - 1
-      const int vc = v0 + vb + 4 * NT * g;
-      const E* ap = nullptr;
-      if (MODE == GRAD)
-        ap = (const E*)job.A.p + b * job.A.sb + pl.first * job.A.sl + h / job.adiv * job.A.sh + vc;
-      const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh + vc;
+      if (XS) {
+        __syncthreads();  // P is whole
 #pragma unroll
-      for (int i = 0; i < TT; ++i) {
-        const int row = i * 16 + r;
-        const bool live = row < cnt && vc < a.VV;
-        const int64_t t = tfirst + tstep * row;
-        float y[4 * NT];
+        for (int sb = 0; sb < SB; ++sb) {
+          Frag<T> zf[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 4 * nt);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y[4 * nt + j] = O[i][nt][j];
-        if constexpr (MODE == GRAD) {
-          float d = 0.0f;
+          for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
+#pragma unroll
+            for (int q = NS - 1; q >= 0; --q) {
+              const Frag<T> pf = row_frag(prow + (q * C + i * 16) * PR + 32 * sb);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
+            }
+        }
+
+        // this lane: rows i * 16 + r of the chunk, columns vc .. vc + 4 NT - 1
+        int vc = v0 + vb + 4 * NT * g, r0 = r;
+        asm volatile("" : "+v"(vc), "+v"(r0));
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+          const int row = i * 16 + r0;
+          const bool live = row < cnt && vc < a.VV;
+          const int64_t t = tfirst + tstep * row;
+          float y[4 * NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[4 * nt + j] = O[i][nt][j];
+          if constexpr (MODE == GRAD) {
+            float d = 0.0f;
+            if (live) {
+              const E* p = ap + t * job.A.sl + vc;
+              if (job.avec) {
+                E e[4 * NT];
+                __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * NT * sizeof(E) < 16 ? 8 : 16),
+                                 sizeof(e));
+#pragma unroll
+                for (int j = 0; j < 4 * NT; ++j) d = __builtin_fmaf(y[j], widen1(e[j]), d);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4 * NT; ++j)
+                  if (vc + j < a.VV) d = __builtin_fmaf(y[j], widen1(p[j]), d);
+              }
+            }
+            d += __shfl_xor(d, 16);
+            d += __shfl_xor(d, 32);
+            if (g == 0) sh.dots[wave * C + row] = d;
+          }
           if (live) {
-            const E* p = ap + t * job.A.sl;
-            if (job.avec) {
-              E e[4 * NT];
-              __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * NT * sizeof(E) < 16 ? 8 : 16),
-                               sizeof(e));
+            const int64_t off = ob + t * job.ol + vc;
+            if (T::SPLIT && !job.out_f32) {
+              uint16_t* op = (uint16_t*)job.out + off;
+              uint32_t u[2 * NT];
 #pragma unroll
-              for (int j = 0; j < 4 * NT; ++j) d = __builtin_fmaf(y[j], widen1(e[j]), d);
+              for (int j = 0; j < 2 * NT; ++j) u[j] = bf16x2_rne(y[2 * j], y[2 * j + 1]);
+              if (job.ovec) {
+                __builtin_memcpy(__builtin_assume_aligned(op, 8 * NT), u, 8 * NT);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4 * NT; ++j)
+                  if (vc + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
+              }
             } else {
+              float* op = (float*)job.out + off;
+              if (job.ovec) {
+                __builtin_memcpy(__builtin_assume_aligned(op, 16), y, 16 * NT);
+              } else {
 #pragma unroll
-              for (int j = 0; j < 4 * NT; ++j)
-                if (vc + j < a.VV) d = __builtin_fmaf(y[j], widen1(p[j]), d);
-            }
-          }
-          d += __shfl_xor(d, 16);
-          d += __shfl_xor(d, 32);
-          if (g == 0) sh.dots[wave * C + row] = d;
-        }
-        if (live) {
-          const int64_t off = ob + t * job.ol;
-          if (T::SPLIT && !job.out_f32) {
-            uint16_t* op = (uint16_t*)job.out + off;
-            uint32_t u[2 * NT];
-#pragma unroll
-            for (int j = 0; j < 2 * NT; ++j) u[j] = bf16x2_rne(y[2 * j], y[2 * j + 1]);
-            if (job.ovec) {
-              __builtin_memcpy(__builtin_assume_aligned(op, 8 * NT), u, 8 * NT);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4 * NT; ++j)
-                if (vc + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
-            }
-          } else {
-            float* op = (float*)job.out + off;
-            if (job.ovec) {
-              __builtin_memcpy(__builtin_assume_aligned(op, 16), y, 16 * NT);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4 * NT; ++j)
-                if (vc + j < a.VV) op[j] = y[j];
+                for (int j = 0; j < 4 * NT; ++j)
+                  if (vc + j < a.VV) op[j] = y[j];
+              }
             }
           }
         }
       }
-      if constexpr (MODE == GRAD) {
-        if (job.anchors && ends && reached > 0 && reached < len && reached % ANCHOR == 0)
-          store_state(anchor_at(reached / ANCHOR - 1), 1.0f);
-      }
+    }
+    if constexpr (MODE == GRAD) {
+      if (job.anchors && reached > 0 && reached < len && reached % ANCHOR == 0)
+        store_state(anchor_at(reached / ANCHOR - 1), 1.0f);
     }
     __syncthreads();  // the tiles are free
     if constexpr (MODE == GRAD) {
@@ -749,32 +783,41 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   }
 }
 
-template <class T, int KP, int NT>
+template <class T, int KP, int NT, bool VEC>
 int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
   const dim3 grid((unsigned)wgs), block(256);
   if (m == CARRY)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY, VEC>), grid, block, 0, st, a);
   else if (m == GRAD)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD, VEC>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
   return check_launch("walk_kernel");
 }
 
 // The instance: X's and Y's columns rounded up to 32, 64, 128 or 256; tiles of
 // 64 nt of Z's columns (nt = 1 above 128 columns of Y: the state's registers).
+template <class T, bool VEC>
+int launch_walk_vec(const WalkArgs& a, Mode m, int nt, int64_t wgs, hipStream_t st) {
+#define SW_WALK(KP)                                             \
+  return nt == 1 ? launch_walk_at<T, KP, 1, VEC>(a, m, wgs, st) \
+                 : launch_walk_at<T, KP, 2, VEC>(a, m, wgs, st)
+  if (a.KK <= 32) SW_WALK(32);
+  if (a.KK <= 64) SW_WALK(64);
+  if (a.KK <= 128) SW_WALK(128);
+  return launch_walk_at<T, 256, 1, VEC>(a, m, wgs, st);
+#undef SW_WALK
+}
+
 template <class T>
 int launch_walk(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
   const int64_t wgs = a.slots * a.H * a.tiles * a.njobs;
   if (wgs == 0) return SW_OK;
-#define SW_WALK(KP)                                      \
-  return nt == 1 ? launch_walk_at<T, KP, 1>(a, m, wgs, st) \
-                 : launch_walk_at<T, KP, 2>(a, m, wgs, st)
-  if (a.KK <= 32) SW_WALK(32);
-  if (a.KK <= 64) SW_WALK(64);
-  if (a.KK <= 128) SW_WALK(128);
-  return launch_walk_at<T, 256, 1>(a, m, wgs, st);
-#undef SW_WALK
+  bool vec = true;
+  for (int i = 0; i < a.njobs; ++i)
+    vec = vec && (m == CARRY || a.job[i].xvec) && a.job[i].yvec && a.job[i].zvec;
+  return vec ? launch_walk_vec<T, true>(a, m, nt, wgs, st)
+             : launch_walk_vec<T, false>(a, m, nt, wgs, st);
 }
 
 int launch_walk_bf16(const WalkArgs& a, Mode m, int nt, hipStream_t st);
