@@ -13,8 +13,8 @@
 // C steps at a time (G_i: the decays' running sum inside the chunk):
 //     P_ts = (X_t . Y_s) e^{G_t - G_s}  for s <= t, else 0
 //     out  = P Z + e^G X S        S <- e^{G_C} S + (e^{G_C - G} Z)^T-weighted Y^T
-// All four products run on the matrix cores.  A workgroup of four waves walks
-// one (sequence, segment, head, tile of Z's columns); a wave owns 16 NT
+// All four products run on the matrix cores.  A workgroup of 4 or 8 waves walks
+// one (sequence, segment, head, tile of Z's columns); a wave owns 16
 // columns and keeps its part of S in accumulators, fp32, from the first step
 // to the last.  The lane that holds an accumulator's column is the lane that
 // the next product wants as an operand's row, and the contraction order is
@@ -36,7 +36,7 @@ namespace lin {
 
 constexpr int CHUNK = 64;      // steps between the places where walks may start or stop
 constexpr int ANCHOR = 256;    // steps between the states kept for dg
-constexpr float G_MIN = -1.0e4f;  // e^g is zero in fp32 far above this
+constexpr float G_MIN = -104.0f;  // e^g is zero in fp32 here: the lowest that counts
 
 struct Job {
   HeadRows X, Y, Z, A;   // A: the input whose products with out are summed (dots)
@@ -182,6 +182,17 @@ __device__ __forceinline__ Frag<F32> row_frag(const float* t) {
   return f;
 }
 
+// Places of P's row: from granule c, swizzled by the row's m = t % 8.
+__device__ __forceinline__ Frag<Bf16> p_frag(const uint16_t* row, int c, int m) {
+  return {*reinterpret_cast<const s8*>(row + (c ^ m) * 8)};
+}
+__device__ __forceinline__ Frag<F32> p_frag(const float* row, int c, int m) {
+  Frag<F32> f;
+  *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(row + (c ^ m) * 4);
+  *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(row + ((c + 1) ^ m) * 4);
+  return f;
+}
+
 // The transposed fragment of 32 steps: lane (g, r) holds column
 // STEP * (r / 4) + r % 4 at the steps 4 j + g, j = 0 .. 7.  col_base gives the
 // lane's address for the block's first step and the columns' first.
@@ -279,10 +290,10 @@ __device__ __forceinline__ float check_finite(u4 u, float acc, F32*) {
 // the granules are stored.  What lies outside the tile has an offset past the
 // buffer's end (rows from n do since a row is no longer than a step; backwards
 // their offsets are negative) and reads zero.
-template <class T, int W, bool VEC>
+template <class T, int W, int THREADS, bool VEC>
 struct Tile {
-  static constexpr int NG = W / T::G, PER = T::C * NG / 256, RPG = 256 / NG;
-  static_assert(PER >= 1 && T::C * NG % 256 == 0, "whole granules per thread");
+  static constexpr int NG = W / T::G, RPG = THREADS / NG, PER = RPG < T::C ? T::C / RPG : 1;
+  static_assert(THREADS % NG == 0 && (RPG >= T::C || T::C % RPG == 0), "whole rows at a time");
   typedef typename T::E E;
   u4 u[PER];
   __device__ __forceinline__ void load(const E* rows, int64_t step, int n, bool rev, int width,
@@ -313,12 +324,14 @@ struct Tile {
       }
     }
   }
-  __device__ __forceinline__ float store(E* lds, int tid, float acc) const {
+  template <bool CHECK>
+  __device__ __forceinline__ float store(E* lds, int tid) const {
+    float acc = 0.0f;
     E* p = lds + tid / NG * ROW<T, W> + tid % NG * T::G;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      *reinterpret_cast<u4*>(p + i * RPG * ROW<T, W>) = u[i];
-      acc = check_finite(u[i], acc, (T*)nullptr);
+      if (RPG <= T::C || tid / NG < T::C) *reinterpret_cast<u4*>(p + i * RPG * ROW<T, W>) = u[i];
+      if (CHECK) acc = check_finite(u[i], acc, (T*)nullptr);
     }
     return acc;
   }
@@ -328,44 +341,57 @@ struct Tile {
 // products with an input are summed by step (with the states kept for dg).
 enum Mode { CARRY, OUT, GRAD };
 
-template <class T, int KP, int NT, Mode MODE>
+template <class T, int KP, int NWV, Mode MODE>
 struct Shared {
-  static constexpr int VT = 64 * NT, C = T::C;
+  static constexpr int VT = 16 * NWV, C = T::C;
   static constexpr int NS = MODE == GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
   static constexpr bool XS = MODE != CARRY;
+  // fp32 results take the decays between steps to fp32: their running sums in two parts
+  static constexpr bool FINE = MODE == GRAD || !T::SPLIT;
   typename T::E y[C * ROW<T, KP>];
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
-  typename T::E p[XS ? NS * C * ROW<T, C> : 8];
-  float gh[C], gl[C];  // by step: the running log2 decay, high and low parts
-  float er[C];         // by step: rscale 2^G
-  float ph[C], pl[C];  // by place: gh and gl
-  float ew[C];         // by place: wscale 2^(G_C - G)
-  float dots[MODE == GRAD ? 4 * C : 4];
-  float g1[C];         // by step: its own log2 decay
-  float ec;            // 2^G_C
-  uint32_t bad[2];     // the chunk (of odd or even number) holds what is not finite
+  typename T::E p[XS ? NS * C * C : 8];  // granule c of row t at c ^ (t % 8)
+  float gh[C], gl[FINE ? C : 4];  // by step: the running log2 decay, high and low parts
+  float er[C];                    // by step: rscale 2^G
+  float g1[C];                    // by step: its own decay
+  float ph[C], pl[FINE ? C : 4];  // by place: gh and gl
+  float ew[C];                    // by place: wscale 2^(G_C - G)
+  float dots[MODE == GRAD ? NWV * C : 4];
+  float ec;                       // 2^G_C
+  uint32_t bad[2];                // the chunk (of odd or even number) holds what is not finite
 };
 
-// Waves per SIMD: what the accumulators of S, out and the loads in flight leave
-// room for (KP = 128, NT = 2: 64 + 32 + 48 registers of 256).
-constexpr int walk_waves(int KP, int NT, Mode m) {
-  return KP >= 256 ? 1 : KP <= 64 && NT == 1 && m != GRAD ? 3 : 2;
+// The lane's place in a fragment, worked out anew: what is derived from it (each
+// phase's addresses in LDS) is not kept in registers across the walk.
+struct LanePlace {
+  int g, r;
+};
+__device__ __forceinline__ LanePlace lane_place(int tid) {
+  asm volatile("" : "+v"(tid));
+  return {(tid >> 4) & 3, tid & 15};
 }
 
-template <class T, int KP, int NT, Mode MODE, bool VEC>
-__global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(WalkArgs a) {
+// Waves per SIMD.  Eight waves share the tiles of X and Y and keep 16 columns of S
+// each, so that two such workgroups (four waves per SIMD, 128 registers) fit a
+// compute unit at KP = 128: with two waves of 32 columns each, half of the time
+// went in waiting (B=1 L=65536 H=40 K=V=128, the walk: 686 us).
+constexpr int walk_waves(int KP, int NWV, Mode m) { return KP >= 256 ? 2 : 4; }
+
+template <class T, int KP, int NWV, Mode MODE, bool VEC>
+__global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kernel(WalkArgs a) {
   typedef typename T::E E;
-  typedef Shared<T, KP, NT, MODE> Sh;
+  typedef Shared<T, KP, NWV, MODE> Sh;
   constexpr bool XS = MODE != CARRY;
-  constexpr int C = T::C, KT = KP / 16, VT = 64 * NT, SB = C / 32, TT = C / 16, NS = Sh::NS;
-  // P: a wave's 16 steps t, and ST tiles of 16 steps s (all of them at C = 64,
-  // one of two at C = 32)
-  constexpr int ST = C * C / 1024;
-  constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, PR = ROW<T, C>;
+  constexpr int C = T::C, KT = KP / 16, VT = 16 * NWV, SB = C / 32, TT = C / 16, NS = Sh::NS;
+  constexpr int THREADS = 64 * NWV;
+  // P: each wave a tile of 16 steps t and ST tiles of 16 steps s
+  constexpr int ST = C == 32 ? 1 : 16 / NWV;
+  constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, G = T::G;
   __shared__ __align__(16) Sh sh;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t w = xcd_contiguous(blockIdx.x, gridDim.x);
   const int tile = w % (uint32_t)a.tiles;
   w /= (uint32_t)a.tiles;
@@ -380,7 +406,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   const bool final_seg = rev ? pl.part == 0 : pl.part == pl.parts - 1;
   if (MODE == CARRY && final_seg) return;
   const int64_t b = a.cu ? 0 : pl.n;
-  const int v0 = tile * VT, vb = wave * 16 * NT;  // the tile's first column; the wave's in it
+  const int v0 = tile * VT, vb = wave * 16;  // the tile's first column; the wave's in it
 
   // steps [lo, hi) of the sequence, in chunks of at most C
   const int len = (int)pl.len, lo = (int)(pl.part * a.lseg);
@@ -394,46 +420,41 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   const E* Z = (const E*)job.Z.p + b * job.Z.sb + pl.first * job.Z.sl + h / job.zdiv * job.Z.sh + v0;
   const float* gp = a.g + b * a.g_sb + pl.first * a.g_sl + h * a.g_sh;
 
-  f4 S[KT][NT];
-  // state element of accumulator (kt, nt, i): Y's column 32 (kt / 2) + 8 g + 4 (kt % 2) + i,
-  // Z's column v0 + vb + 4 NT (r / 4) + 4 nt + r % 4
+  f4 S[KT];
+  // state element of accumulator (kt, i): Y's column 32 (kt / 2) + 8 g + 4 (kt % 2) + i,
+  // Z's column v0 + vb + r
   auto each_state = [&](auto fn) __attribute__((always_inline)) {
-    int kk = 8 * g, vv = v0 + vb + 4 * NT * (r >> 2) + (r & 3);
+    int kk = 8 * g, vv = v0 + vb + r;
     asm volatile("" : "+v"(kk), "+v"(vv));  // worked out here, not kept across the walk
+    if (vv < a.VV) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if (vv + 4 * nt < a.VV) {
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = kk + 32 * (kt >> 1) + 4 * (kt & 1) + i;
-            if (k < a.KK) fn(kt, nt, i, k * job.skk + (vv + 4 * nt) * job.svv);
-          }
-      }
+        for (int i = 0; i < 4; ++i) {
+          const int k = kk + 32 * (kt >> 1) + 4 * (kt & 1) + i;
+          if (k < a.KK) fn(kt, i, k * job.skk + vv * job.svv);
+        }
     }
   };
   auto store_state = [&](float* p, float f) __attribute__((always_inline)) {
-    each_state([&](int kt, int nt, int i, int64_t at) __attribute__((always_inline)) { p[at] = S[kt][nt][i] * f; });
+    each_state([&](int kt, int i, int64_t at) __attribute__((always_inline)) { p[at] = S[kt][i] * f; });
   };
   auto anchor_at = [&](int64_t i) {  // the sequence's i-th
     const int64_t per = (a.L + ANCHOR - 1) / ANCHOR;
     return job.anchors + ((first_slot(pl, a.cu, ANCHOR, per) + i) * a.H + h) * a.KV;
   };
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) S[kt][nt] = f4{0.f, 0.f, 0.f, 0.f};
+  for (int kt = 0; kt < KT; ++kt) S[kt] = f4{0.f, 0.f, 0.f, 0.f};
   if (XS) {
     const float* p = job.carry ? job.carry + (slot * a.H + h) * a.KV
                      : job.init ? job.init + (pl.n * a.H + h) * a.KV
                                 : nullptr;
-    if (p) each_state([&](int kt, int nt, int i, int64_t at) __attribute__((always_inline)) { S[kt][nt][i] = p[at]; });
+    if (p) each_state([&](int kt, int i, int64_t at) __attribute__((always_inline)) { S[kt][i] = p[at]; });
   }
   float seg_decay = 1.0f;
 
-  Tile<T, KP, VEC> tx, ty;
-  Tile<T, VT, VEC> tz;
+  Tile<T, KP, THREADS, VEC> tx, ty;
+  Tile<T, VT, THREADS, VEC> tz;
   float tg = 0.0f;
   int t0 = 0, n = 0;  // a chunk's steps: t0 .. t0 + n - 1; its row i is the walk's i-th of them
   auto load_chunk = [&](int c) __attribute__((always_inline)) {  // c = nch: nothing
@@ -450,11 +471,6 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     }
   };
 
-  // this lane's first address in each tile
-  const E* const xrow = sh.x + r * KR + 8 * g;               // steps 16 i + r
-  const E* const ycol = col_base<KP, 8>(sh.y, g, r);
-  const E* const zcol = col_base<VT, 4 * NT>(sh.z, g, r) + vb;
-  const E* const prow = sh.p + r * PR + 8 * g;
   const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh;
   const E* ap = nullptr;
   if (MODE == GRAD)
@@ -466,8 +482,11 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     __syncthreads();
   }
   for (int c = 0; c < nch; ++c) {
-    float fin = ty.store(sh.y, tid, tz.store(sh.z, tid, 0.0f));
-    if (XS) fin = tx.store(sh.x, tid, fin);
+    // what is not finite in X and Y meets its own steps and columns only; in Z, zero
+    // weights too
+    const float fin = tz.template store<true>(sh.z, tid);
+    ty.template store<false>(sh.y, tid);
+    if (XS) tx.template store<false>(sh.x, tid);
     if (fin != fin) sh.bad[c & 1] = 1;
     if (wave == 0) {
       const double g1 = (double)clamp_g(tg) * 1.4426950408889634;
@@ -482,9 +501,11 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         const int q = place_in(lane);
         const float hi_ = (float)G, lo_ = (float)(G - (double)hi_);
         sh.gh[lane] = hi_;
-        sh.gl[lane] = lo_;
         sh.ph[q] = hi_;
-        sh.pl[q] = lo_;
+        if (Sh::FINE) {
+          sh.gl[lane] = lo_;
+          sh.pl[q] = lo_;
+        }
         sh.er[lane] = exp2_of(G) * job.rscale;
         sh.ew[q] = exp2_of(GC - G) * job.wscale;
         sh.g1[lane] = exp2_of(g1);
@@ -505,14 +526,10 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 #pragma unroll 1
       for (int i = 0; i < cnt; ++i) {
         const float a1 = sh.g1[i];
-        int vc = v0 + vb + 4 * NT * (r >> 2) + (r & 3), kg = 8 * g;
+        int vc = v0 + vb + r, kg = 8 * g;
         asm volatile("" : "+v"(vc), "+v"(kg));  // worked out here, not kept across the walk
-        float xy = 0.0f, acc[NT], z[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          acc[nt] = 0.0f;
-          z[nt] = widen1(sh.z[i * VR + vc - v0 + 4 * nt]);
-        }
+        const float z = widen1(sh.z[i * VR + vc - v0]);
+        float xy = 0.0f, acc = 0.0f;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -522,11 +539,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
               const float y = widen1(sh.y[i * KR + kk]);
               const float x = XS ? widen1(sh.x[i * KR + kk]) : 0.0f;
               xy = __builtin_fmaf(x, y, xy);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                acc[nt] = __builtin_fmaf(x, S[kt][nt][j], acc[nt]);
-                S[kt][nt][j] = __builtin_fmaf(y, job.wscale * z[nt], a1 * S[kt][nt][j]);
-              }
+              acc = __builtin_fmaf(x, S[kt][j], acc);
+              S[kt][j] = __builtin_fmaf(y, job.wscale * z, a1 * S[kt][j]);
             }
           }
         if (MODE == CARRY) seg_decay *= a1;
@@ -534,20 +548,17 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
           const int64_t t = tfirst + tstep * i;
           xy += __shfl_xor(xy, 16);
           xy += __shfl_xor(xy, 32);
+          acc += __shfl_xor(acc, 16);
+          acc += __shfl_xor(acc, 32);
+          const float y = a1 * job.rscale * acc + job.pscale * xy * z;
           float d = 0.0f;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            acc[nt] += __shfl_xor(acc[nt], 16);
-            acc[nt] += __shfl_xor(acc[nt], 32);
-            const float y = a1 * job.rscale * acc[nt] + job.pscale * xy * z[nt];
-            if (g == 0 && vc + 4 * nt < a.VV) {
-              const int64_t off = ob + t * job.ol + vc + 4 * nt;
-              if (T::SPLIT && !job.out_f32)
-                ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
-              else
-                ((float*)job.out)[off] = y;
-              if (MODE == GRAD) d += y * widen1(ap[t * job.A.sl + vc + 4 * nt]);
-            }
+          if (g == 0 && vc < a.VV) {
+            const int64_t off = ob + t * job.ol + vc;
+            if (T::SPLIT && !job.out_f32)
+              ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
+            else
+              ((float*)job.out)[off] = y;
+            if (MODE == GRAD) d = y * widen1(ap[t * job.A.sl + vc]);
           }
           if (MODE == GRAD) {
 #pragma unroll
@@ -558,89 +569,85 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       }
       load_chunk(c + 1);
     } else {
-      f4 O[TT][NT];
+      f4 O[TT];
       if (XS) {
         // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
-        const int tt = ST == 4 ? wave : wave & 1, q0 = ST == 4 ? 0 : 16 * (wave >> 1);
-        const int t = tt * 16 + r;
-        f4 acc[ST];
+        const int tt = wave & (TT - 1), q0 = 16 * ST * (wave / TT);
+        // a wave beyond the tiles, or above the diagonal where nothing is read
+        if (q0 < C && 16 * tt + 15 >= (q0 & ~31)) {
+          const auto [g, r] = lane_place(tid);
+          const int t = tt * 16 + r;
+          f4 acc[ST];
 #pragma unroll
-        for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
-        // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; step_of's terms in st are
-        // constants: 16 (st % 2) + st / 2
-        const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
-        const E* const xr = sh.x + t * KR + 8 * g;
+          for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
+          // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; what step_of adds for
+          // st is constant
+          auto more = [](int st) { return ST == 4 ? 16 * (st & 1) + (st >> 1) : 16 * st; };
+          const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
+          const E* const xr = sh.x + t * KR + 8 * g;
 #pragma unroll
-        for (int p = 0; p < KP / 32; ++p) {
-          const Frag<T> xf = row_frag(xr + 32 * p);
+          for (int p = 0; p < KP / 32; ++p) {
+            const Frag<T> xf = row_frag(xr + 32 * p);
 #pragma unroll
-          for (int st = 0; st < ST; ++st)
-            acc[st] = mma(row_frag(yr + (16 * (st & 1) + (st >> 1)) * KR + 32 * p), xf, acc[st]);
-        }
-        // this lane: step t, places qf .. qf + 4 ST - 1
-        const int qf = q0 + 4 * ST * g;
-        const float ght = sh.gh[t], glt = sh.gl[t];
-        int ahead = t - step_of(qf);  // steps from the first place's to t
-        asm volatile("" : "+v"(ahead));  // compared here: sixteen masks are not kept
-        float pv[4 * ST];
-#pragma unroll
-        for (int st = 0; st < ST; ++st) {
-          const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
-          const f4 gl = *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float d = (ght - gh[i]) + (glt - gl[i]);
-            const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d) * job.pscale);
-            pv[4 * st + i] = 16 * (st & 1) + (st >> 1) + 4 * i <= ahead ? e : 0.0f;
+            for (int st = 0; st < ST; ++st)
+              acc[st] = mma(row_frag(yr + more(st) * KR + 32 * p), xf, acc[st]);
           }
-        }
-        E* const pw = sh.p + t * PR + qf;
-        if constexpr (T::SPLIT) {
+          // this lane: step t, places qf .. qf + 4 ST - 1
+          const int qf = q0 + 4 * ST * g;
+          const float ght = sh.gh[t], glt = Sh::FINE ? sh.gl[t] : 0.0f;
+          int ahead = t - step_of(qf);  // steps from the first place's to t
+          asm volatile("" : "+v"(ahead));  // compared here: the masks are not kept
+          float pv[4 * ST];
 #pragma unroll
-          for (int half = 0; half < ST / 2; ++half) {
-            Frag<T> f[NS];
-            parts_of<NS>(pv + 8 * half, f);
+          for (int st = 0; st < ST; ++st) {
+            const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
+            f4 d = ght - gh;
+            if (Sh::FINE) d += glt - *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
 #pragma unroll
-            for (int i = 0; i < NS; ++i)
-              *reinterpret_cast<s8*>(pw + i * C * PR + 8 * half) = f[i].v;
+            for (int i = 0; i < 4; ++i) {
+              const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d[i]) * job.pscale);
+              pv[4 * st + i] = more(st) + 4 * i <= ahead ? e : 0.0f;
+            }
           }
-        } else {
-          *reinterpret_cast<f4*>(pw) = f4{pv[0], pv[1], pv[2], pv[3]};
+          E* const pw = sh.p + t * C;
+          if constexpr (T::SPLIT) {
+#pragma unroll
+            for (int half = 0; half < ST / 2; ++half) {
+              Frag<T> f[NS];
+              parts_of<NS>(pv + 8 * half, f);
+#pragma unroll
+              for (int i = 0; i < NS; ++i)
+                *reinterpret_cast<s8*>(pw + i * C * C + ((qf / 8 + half) ^ (t & 7)) * 8) = f[i].v;
+            }
+          } else {
+            *reinterpret_cast<f4*>(pw + ((qf / 4) ^ (t & 7)) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
+          }
         }
 
         // X S
+        const auto [g, r] = lane_place(tid);
+        const E* const xrow = sh.x + r * KR + 8 * g;
 #pragma unroll
-        for (int i = 0; i < TT; ++i)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < TT; ++i) O[i] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < KP / 32; ++p) {
-          Frag<T> sfr[NT][NS];
+          Frag<T> sf[NS];
+          float x[8];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[i] = S[2 * p][nt][i];
-              x[4 + i] = S[2 * p + 1][nt][i];
-            }
-            parts_of<NS>(x, sfr[nt]);
+          for (int i = 0; i < 4; ++i) {
+            x[i] = S[2 * p][i];
+            x[4 + i] = S[2 * p + 1][i];
           }
+          parts_of<NS>(x, sf);
 #pragma unroll
           for (int i = 0; i < TT; ++i) {
             const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sfr[nt][q], xf, O[i][nt]);
+            for (int q = NS - 1; q >= 0; --q) O[i] = mma(sf[q], xf, O[i]);
           }
         }
 #pragma unroll
-        for (int i = 0; i < TT; ++i) {
-          const float er = sh.er[i * 16 + r];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
-        }
+        for (int i = 0; i < TT; ++i) O[i] *= sh.er[i * 16 + r];
       }
 
       load_chunk(c + 1);  // in flight while the state moves on; earlier, its registers would spill
@@ -648,78 +655,65 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       // S <- e^{G_C} S + Y^T (weighted Z)
       const float ec = sh.ec;
       if (MODE == CARRY) seg_decay *= ec;
+      const auto [g, r] = lane_place(tid);
+      const E* const ycol = col_base<KP, 8>(sh.y, g, r);
+      const E* const zcol = col_base<VT, 4>(sh.z, g, r) + vb;
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
+      for (int kt = 0; kt < KT; ++kt) S[kt] *= ec;
 #pragma unroll
       for (int sb = 0; sb < SB; ++sb) {
-        Frag<T> wf[NT][T::NW];
-        float ew[8];
+        Frag<T> wf[T::NW];
+        float ew[8], x[8];
         *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
         *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
+        widen(col_frag<VT>(zcol + 32 * sb * VR), x);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float x[8];
-          widen(col_frag<VT>(zcol + 32 * sb * VR + 4 * nt), x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] *= ew[j];
-          parts_of<T::NW>(x, wf[nt]);
-        }
+        for (int j = 0; j < 8; ++j) x[j] *= ew[j];
+        parts_of<T::NW>(x, wf);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           const Frag<T> yf = col_frag<KP>(ycol + 32 * sb * KR + 32 * (kt >> 1) + 4 * (kt & 1));
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
+          for (int q = T::NW - 1; q >= 0; --q) S[kt] = mma(yf, wf[q], S[kt]);
         }
       }
 
       if (XS) {
         __syncthreads();  // P is whole
+        const auto [g, r] = lane_place(tid);
+        const E* const zcol = col_base<VT, 4>(sh.z, g, r) + vb;
+        const E* const prow = sh.p + r * C;
+        const int pg = 8 / G * g;  // a lane's eight places: whole granules of P's row 16 i + r
 #pragma unroll
         for (int sb = 0; sb < SB; ++sb) {
-          Frag<T> zf[NT];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 4 * nt);
+          const Frag<T> zf = col_frag<VT>(zcol + 32 * sb * VR);
 #pragma unroll
           for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
 #pragma unroll
-            for (int q = NS - 1; q >= 0; --q) {
-              const Frag<T> pf = row_frag(prow + (q * C + i * 16) * PR + 32 * sb);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
-            }
+            for (int q = NS - 1; q >= 0; --q)
+              O[i] = mma(zf, p_frag(prow + (q * C + i * 16) * C, 32 / G * sb + pg, r & 7), O[i]);
         }
 
-        // this lane: rows i * 16 + r of the chunk, columns vc .. vc + 4 NT - 1
-        int vc = v0 + vb + 4 * NT * g, r0 = r;
-        asm volatile("" : "+v"(vc), "+v"(r0));
+        // this lane: rows i * 16 + r of the chunk, columns vc .. vc + 3
+        const int vc = v0 + vb + 4 * g;
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
-          const int row = i * 16 + r0;
+          const int row = i * 16 + r;
           const bool live = row < cnt && vc < a.VV;
           const int64_t t = tfirst + tstep * row;
-          float y[4 * NT];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[4 * nt + j] = O[i][nt][j];
           if constexpr (MODE == GRAD) {
             float d = 0.0f;
             if (live) {
               const E* p = ap + t * job.A.sl + vc;
               if (job.avec) {
-                E e[4 * NT];
-                __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * NT * sizeof(E) < 16 ? 8 : 16),
-                                 sizeof(e));
+                E e[4];
+                __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * sizeof(E)), sizeof(e));
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j) d = __builtin_fmaf(y[j], widen1(e[j]), d);
+                for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][j], widen1(e[j]), d);
               } else {
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j)
-                  if (vc + j < a.VV) d = __builtin_fmaf(y[j], widen1(p[j]), d);
+                for (int j = 0; j < 4; ++j)
+                  if (vc + j < a.VV) d = __builtin_fmaf(O[i][j], widen1(p[j]), d);
               }
             }
             d += __shfl_xor(d, 16);
@@ -730,24 +724,22 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
             const int64_t off = ob + t * job.ol + vc;
             if (T::SPLIT && !job.out_f32) {
               uint16_t* op = (uint16_t*)job.out + off;
-              uint32_t u[2 * NT];
-#pragma unroll
-              for (int j = 0; j < 2 * NT; ++j) u[j] = bf16x2_rne(y[2 * j], y[2 * j + 1]);
+              const uint32_t u[2] = {bf16x2_rne(O[i][0], O[i][1]), bf16x2_rne(O[i][2], O[i][3])};
               if (job.ovec) {
-                __builtin_memcpy(__builtin_assume_aligned(op, 8 * NT), u, 8 * NT);
+                *reinterpret_cast<uint2*>(op) = make_uint2(u[0], u[1]);
               } else {
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j)
+                for (int j = 0; j < 4; ++j)
                   if (vc + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
               }
             } else {
               float* op = (float*)job.out + off;
               if (job.ovec) {
-                __builtin_memcpy(__builtin_assume_aligned(op, 16), y, 16 * NT);
+                *reinterpret_cast<f4*>(op) = O[i];
               } else {
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j)
-                  if (vc + j < a.VV) op[j] = y[j];
+                for (int j = 0; j < 4; ++j)
+                  if (vc + j < a.VV) op[j] = O[i][j];
               }
             }
           }
@@ -763,7 +755,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       if (wave == 0 && lane < cnt) {
         float d = 0.0f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) d += sh.dots[q * C + lane];
+        for (int q = 0; q < NWV; ++q) d += sh.dots[q * C + lane];
         job.dots[((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst +
                  tstep * lane] = d;
       }
@@ -783,45 +775,45 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   }
 }
 
-template <class T, int KP, int NT, bool VEC>
+template <class T, int KP, int NWV, bool VEC>
 int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
-  const dim3 grid((unsigned)wgs), block(256);
+  const dim3 grid((unsigned)wgs), block(64 * NWV);
   if (m == CARRY)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, CARRY, VEC>), grid, block, 0, st, a);
   else if (m == GRAD)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, GRAD, VEC>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, OUT, VEC>), grid, block, 0, st, a);
   return check_launch("walk_kernel");
 }
 
 // The instance: X's and Y's columns rounded up to 32, 64, 128 or 256; tiles of
-// 64 nt of Z's columns (nt = 1 above 128 columns of Y: the state's registers).
+// 16 columns of Z for each of 4 or 8 waves.
 template <class T, bool VEC>
-int launch_walk_vec(const WalkArgs& a, Mode m, int nt, int64_t wgs, hipStream_t st) {
-#define SW_WALK(KP)                                             \
-  return nt == 1 ? launch_walk_at<T, KP, 1, VEC>(a, m, wgs, st) \
-                 : launch_walk_at<T, KP, 2, VEC>(a, m, wgs, st)
+int launch_walk_vec(const WalkArgs& a, Mode m, int waves, int64_t wgs, hipStream_t st) {
+#define SW_WALK(KP)                                                \
+  return waves == 4 ? launch_walk_at<T, KP, 4, VEC>(a, m, wgs, st) \
+                    : launch_walk_at<T, KP, 8, VEC>(a, m, wgs, st)
   if (a.KK <= 32) SW_WALK(32);
   if (a.KK <= 64) SW_WALK(64);
   if (a.KK <= 128) SW_WALK(128);
-  return launch_walk_at<T, 256, 1, VEC>(a, m, wgs, st);
+  SW_WALK(256);
 #undef SW_WALK
 }
 
 template <class T>
-int launch_walk(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
+int launch_walk(const WalkArgs& a, Mode m, int waves, hipStream_t st) {
   const int64_t wgs = a.slots * a.H * a.tiles * a.njobs;
   if (wgs == 0) return SW_OK;
   bool vec = true;
   for (int i = 0; i < a.njobs; ++i)
     vec = vec && (m == CARRY || a.job[i].xvec) && a.job[i].yvec && a.job[i].zvec;
-  return vec ? launch_walk_vec<T, true>(a, m, nt, wgs, st)
-             : launch_walk_vec<T, false>(a, m, nt, wgs, st);
+  return vec ? launch_walk_vec<T, true>(a, m, waves, wgs, st)
+             : launch_walk_vec<T, false>(a, m, waves, wgs, st);
 }
 
-int launch_walk_bf16(const WalkArgs& a, Mode m, int nt, hipStream_t st);
-int launch_walk_f32(const WalkArgs& a, Mode m, int nt, hipStream_t st);
+int launch_walk_bf16(const WalkArgs& a, Mode m, int waves, hipStream_t st);
+int launch_walk_f32(const WalkArgs& a, Mode m, int waves, hipStream_t st);
 
 }  // namespace lin
 }  // namespace sw
