@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void share_kernel(const float* __restrict__ pa
 // -------------------------------------------------------------- planning
 
 struct Plan {
-  int waves_v = 4, waves_k = 4;    // tiles of 16 columns a wave: of V (fwd, dv), of K (dq, dk)
+  int nt_v = 1, nt_k = 1;          // tiles of 64 nt columns: of V (fwd, dv), of K (dq, dk)
   int64_t tiles_v = 1, tiles_k = 1;
   int64_t lseg = CHUNK, per_seq = 1, slots = 0;  // segments
   bool cut = false;                // some sequence may have several
@@ -213,10 +213,10 @@ struct Plan {
 // a walk of the keys and values alone before the walk itself.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
-  p.waves_v = a.V <= 64 ? 4 : 8;
-  p.waves_k = a.K <= 64 ? 4 : 8;
-  p.tiles_v = (a.V + 16 * p.waves_v - 1) / (16 * p.waves_v);
-  p.tiles_k = (a.K + 16 * p.waves_k - 1) / (16 * p.waves_k);
+  p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
+  p.nt_k = a.K <= 64 || a.V > 128 ? 1 : 2;
+  p.tiles_v = (a.V + 64 * p.nt_v - 1) / (64 * p.nt_v);
+  p.tiles_k = (a.K + 64 * p.nt_k - 1) / (64 * p.nt_k);
   const int64_t per_seq_wgs = a.H * (bwd ? 2 * p.tiles_k : p.tiles_v);
   const int64_t longest = a.L, chunks = (longest + CHUNK - 1) / CHUNK;
   const int64_t want = 2 * (int64_t)cus, whole = a.B * per_seq_wgs;
@@ -333,14 +333,15 @@ void set_out(Job& j, const LinAttnArgs& a, void* out, int64_t heads, int64_t wid
   j.ob = a.L * j.ol;
   j.out_f32 = f32;
   j.ovec = (uintptr_t)out % 16 == 0 && width % 4 == 0;  // a lane's four columns
+  j.orows = (uintptr_t)out % 16 == 0 && width % 8 == 0 && a.bf16 && !f32;
 }
 
 int launch_walk_any(const LinAttnArgs& a, WalkArgs& w, Mode m, int64_t KK, int64_t VV,
-                    int waves, int64_t tiles, hipStream_t st) {
+                    int nt, int64_t tiles, hipStream_t st) {
   w.KK = (int)KK;
   w.VV = (int)VV;
   w.tiles = (int)tiles;
-  return a.bf16 ? launch_walk_bf16(w, m, waves, st) : launch_walk_f32(w, m, waves, st);
+  return a.bf16 ? launch_walk_bf16(w, m, nt, st) : launch_walk_f32(w, m, nt, st);
 }
 
 int launch_fold(const LinAttnArgs& a, const Plan& p, FoldArgs& f, int njobs, hipStream_t s) {
@@ -434,13 +435,13 @@ int linear_attn_fwd(const LinAttnArgs& a) {
     j.carry = (float*)(ws.p + l.carry[0]);
     j.decay = (float*)(ws.p + l.decay[0]);
     w.job[0] = j;
-    if ((st = launch_walk_any(a, w, CARRY, a.K, a.V, p.waves_v, p.tiles_v, s)) != SW_OK) return st;
+    if ((st = launch_walk_any(a, w, CARRY, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
     FoldArgs f{};
     f.job[0] = {j.carry, j.decay, a.h0, false};
     if ((st = launch_fold(a, p, f, 1, s)) != SW_OK) return st;
   }
   w.job[0] = j;
-  return launch_walk_any(a, w, OUT, a.K, a.V, p.waves_v, p.tiles_v, s);
+  return launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s);
 }
 
 int linear_attn_bwd(const LinAttnArgs& a) {
@@ -481,7 +482,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
     w.job[0] = jq;
     w.job[1] = jk;
     w.njobs = 2;
-    if ((st = launch_walk_any(a, w, CARRY, a.V, a.K, p.waves_k, p.tiles_k, s)) != SW_OK) return st;
+    if ((st = launch_walk_any(a, w, CARRY, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
     FoldArgs f{};
     f.job[0] = {jq.carry, jq.decay, a.h0, false};
     f.job[1] = {jk.carry, jk.decay, a.dh_last, true};
@@ -502,10 +503,10 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   w.job[0] = jq;
   w.job[1] = jk;
   w.njobs = 2;
-  if ((st = launch_walk_any(a, w, GRAD, a.V, a.K, p.waves_k, p.tiles_k, s)) != SW_OK) return st;
+  if ((st = launch_walk_any(a, w, GRAD, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
   w.job[0] = jv;
   w.njobs = 1;
-  if ((st = launch_walk_any(a, w, OUT, a.K, a.V, p.waves_v, p.tiles_v, s)) != SW_OK) return st;
+  if ((st = launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
 
   DgArgs d{};
   d.rdots = at(l.rdots);

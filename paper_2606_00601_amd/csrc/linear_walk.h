@@ -13,8 +13,8 @@
 // C steps at a time (G_i: the decays' running sum inside the chunk):
 //     P_ts = (X_t . Y_s) e^{G_t - G_s}  for s <= t, else 0
 //     out  = P Z + e^G X S        S <- e^{G_C} S + (e^{G_C - G} Z)^T-weighted Y^T
-// All four products run on the matrix cores.  A workgroup of 4 or 8 waves walks
-// one (sequence, segment, head, tile of Z's columns); a wave owns 16
+// All four products run on the matrix cores.  A workgroup of four waves walks
+// one (sequence, segment, head, tile of Z's columns); a wave owns 16 NT
 // columns and keeps its part of S in accumulators, fp32, from the first step
 // to the last.  The lane that holds an accumulator's column is the lane that
 // the next product wants as an operand's row, and the contraction order is
@@ -41,7 +41,8 @@ constexpr float G_MIN = -104.0f;  // e^g is zero in fp32 here: the lowest that c
 struct Job {
   HeadRows X, Y, Z, A;   // A: the input whose products with out are summed (dots)
   int xdiv, ydiv, zdiv, adiv;  // head h reads head h / div
-  bool xvec, yvec, zvec, avec, ovec;  // rows are 16-byte aligned whole vectors
+  bool xvec, yvec, zvec, avec;  // rows are 16-byte aligned whole vectors
+  bool ovec, orows;             // out's rows: whole fours of columns; and 16-byte granules
   void* out;
   int64_t ob, ol, oh;
   bool out_f32;
@@ -116,6 +117,32 @@ __device__ __forceinline__ int64_t first_slot(const Place& p, const int32_t* cu,
 // e^g of a decay as the walks use it.
 __device__ __forceinline__ float clamp_g(float g) { return g < G_MIN ? G_MIN : g; }
 
+// One step of an inclusive sum over a wave's lanes: v plus that of the lane the
+// control names, where it has one.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double add_from(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo =
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROW_MASK, 0xf, false);
+  const uint32_t hi =
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROW_MASK, 0xf, false);
+  return v + __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+// Inclusive sums over the 64 lanes; all: the last lane's, on every lane.
+__device__ __forceinline__ double wave_running_sum(double v, double* all) {
+  v = add_from<DPP_ROW_SHR1, 0xf>(v);
+  v = add_from<DPP_ROW_SHR2, 0xf>(v);
+  v = add_from<DPP_ROW_SHR4, 0xf>(v);
+  v = add_from<DPP_ROW_SHR8, 0xf>(v);
+  v = add_from<DPP_ROW_BCAST15, 0xa>(v);
+  v = add_from<DPP_ROW_BCAST31, 0xc>(v);
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
+  *all = __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+  return v;
+}
+
 // 2^x of a double, to fp32 rounding.
 __device__ __forceinline__ float exp2_of(double x) {
   const double n = rint(x);
@@ -160,18 +187,28 @@ __device__ __forceinline__ f4 mma(const Frag<F32>& a, const Frag<F32>& b, f4 c) 
   return c;
 }
 
-// LDS tiles are rows of W elements and 16 bytes of padding, so that one
-// granule of 16 bytes of eight neighbouring rows, and four granules of rows
-// four apart, lie in different banks, and every fragment of a lane is at a
-// constant offset from its first.
+// Tiles in LDS.  The contraction over steps runs in blocks of 32, whose place
+// (lane group g, element j) is step 4 g + j (j < 4) or 16 + 4 g + j - 4; that over
+// columns in blocks of 32, whose (g, j) is column 8 g + j.  An accumulator's rows
+// then are an operand's places, X's fragments are one read, and transposed reads
+// take four neighbouring rows a group.
+// Rows have 32 bytes of padding: 32 bytes of each of eight neighbouring rows lie
+// in different banks.  In Y (bf16), 16-byte granules of odd pairs have their halves
+// exchanged: a transposed read takes the same half of four granules, and so meets
+// all of those 32 bytes.  Counted, the reads of X's, Y's and Z's fragments take the
+// cycles that their bytes need.
 template <class T, int W>
-constexpr int ROW = W + T::G;
+constexpr int ROW = W + 2 * T::G;
 
-// The contraction over a chunk's steps runs in blocks of 32; in each, place q
-// of an operand (lane group q / 8, element q % 8) is step 4 (q % 8) + q / 8.
-__device__ __forceinline__ int step_of(int q) { return (q & ~31) + 4 * (q & 7) + ((q >> 3) & 3); }
-__device__ __forceinline__ int place_in(int s) { return (s & ~31) + 8 * (s & 3) + ((s >> 2) & 7); }
+// Place q of a chunk is this step; and the other way round.
+__device__ __forceinline__ int step_of(int q) {
+  return (q & ~31) + 16 * ((q >> 2) & 1) + 4 * ((q >> 3) & 3) + (q & 3);
+}
+__device__ __forceinline__ int place_in(int s) {
+  return (s & ~31) + 8 * ((s >> 2) & 3) + 4 * ((s >> 4) & 1) + (s & 3);
+}
 
+// Eight columns of a row of X or Y.
 __device__ __forceinline__ Frag<Bf16> row_frag(const uint16_t* t) {
   return {*reinterpret_cast<const s8*>(t)};
 }
@@ -181,28 +218,58 @@ __device__ __forceinline__ Frag<F32> row_frag(const float* t) {
   *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(t + 4);
   return f;
 }
-
-// Places of P's row: from granule c, swizzled by the row's m = t % 8.
-__device__ __forceinline__ Frag<Bf16> p_frag(const uint16_t* row, int c, int m) {
-  return {*reinterpret_cast<const s8*>(row + (c ^ m) * 8)};
+// X's fragment in the order of Y's.
+__device__ __forceinline__ Frag<Bf16> as_y(const Frag<Bf16>& f, int g) {
+  const u4 u = __builtin_bit_cast(u4, f.v);
+  return {__builtin_bit_cast(s8, g & 2 ? u4{u[2], u[3], u[0], u[1]} : u)};
 }
-__device__ __forceinline__ Frag<F32> p_frag(const float* row, int c, int m) {
+__device__ __forceinline__ Frag<F32> as_y(const Frag<F32>& f, int) { return f; }
+
+// P's rows hold what lies on and below the diagonal's blocks: of 64 steps, the
+// first 32 rows one block of 32 places and the others two.  16-byte granule c of
+// row t is at c ^ pswz(t) of its row.
+template <class T>
+__device__ __forceinline__ int p_row(int t) {  // the row's first element
+  return T::C == 32 || t >= 32 ? t * T::C - (T::C == 64 ? 32 * 32 : 0) : t * 32;
+}
+template <class T>
+__device__ __forceinline__ int pswz(int t) {
+  return T::C == 32 || t >= 32 ? t & 7 : 2 * ((t >> 2) & 1);
+}
+template <class T>
+constexpr int P_SIZE = T::C == 64 ? 64 * 64 - 32 * 32 : 32 * 32;
+// A lane's eight places 8 g .. + 7 of block sb.
+__device__ __forceinline__ Frag<Bf16> p_frag(const uint16_t* p, int t, int sb, int g) {
+  return {*reinterpret_cast<const s8*>(p + p_row<Bf16>(t) + ((4 * sb + g) ^ pswz<Bf16>(t)) * 8)};
+}
+__device__ __forceinline__ Frag<F32> p_frag(const float* p, int t, int, int g) {
   Frag<F32> f;
-  *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(row + (c ^ m) * 4);
-  *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(row + ((c + 1) ^ m) * 4);
+  const int m = pswz<F32>(t);
+  const float* row = p + p_row<F32>(t);
+  *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(row + ((2 * g) ^ m) * 4);
+  *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(row + ((2 * g + 1) ^ m) * 4);
   return f;
 }
 
-// The transposed fragment of 32 steps: lane (g, r) holds column
-// STEP * (r / 4) + r % 4 at the steps 4 j + g, j = 0 .. 7.  col_base gives the
-// lane's address for the block's first step and the columns' first.
-template <int W, int STEP>
-__device__ __forceinline__ const uint16_t* col_base(const uint16_t* t, int g, int r) {
-  return t + (4 * (r >> 2) + g) * ROW<Bf16, W> + STEP * (r & 3);
+// The transposed fragment of 32 steps: lane (g, r) holds a column at its group's
+// places: of Z, column r of 16 (z_base); of Y, column 8 (r / 4) + 4 half + r % 4 of
+// 32 (y_base; half: 0 or 1).  Both give the lane's address for the block's first
+// step and the columns' first.
+template <int W>
+__device__ __forceinline__ const uint16_t* z_base(const uint16_t* t, int g, int r) {
+  return t + (4 * g + (r >> 2)) * ROW<Bf16, W> + 4 * (r & 3);
 }
-template <int W, int STEP>
-__device__ __forceinline__ const float* col_base(const float* t, int g, int r) {
-  return t + g * ROW<F32, W> + STEP * (r >> 2) + (r & 3);
+template <int W>
+__device__ __forceinline__ const float* z_base(const float* t, int g, int r) {
+  return t + 4 * g * ROW<F32, W> + r;
+}
+template <int W>
+__device__ __forceinline__ const uint16_t* y_base(const uint16_t* t, int g, int r, int half) {
+  return t + (4 * g + (r >> 2)) * ROW<Bf16, W> + 8 * (r & 3) + 4 * (half ^ ((r >> 1) & 1));
+}
+template <int W>
+__device__ __forceinline__ const float* y_base(const float* t, int g, int r, int half) {
+  return t + 4 * g * ROW<F32, W> + 8 * (r >> 2) + 4 * half + (r & 3);
 }
 template <int W>
 __device__ __forceinline__ Frag<Bf16> col_frag(const uint16_t* t) {
@@ -215,7 +282,7 @@ template <int W>
 __device__ __forceinline__ Frag<F32> col_frag(const float* t) {
   Frag<F32> f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f.v[j] = t[4 * j * ROW<F32, W>];
+  for (int j = 0; j < 8; ++j) f.v[j] = t[(j + (j < 4 ? 0 : 12)) * ROW<F32, W>];
   return f;
 }
 
@@ -324,15 +391,22 @@ struct Tile {
       }
     }
   }
-  template <bool CHECK>
-  __device__ __forceinline__ float store(E* lds, int tid) const {
-    float acc = 0.0f;
+  // To the tile's rows (SWAP: as Y's).
+  template <bool SWAP>
+  __device__ __forceinline__ void store(E* lds, int tid) const {
     E* p = lds + tid / NG * ROW<T, W> + tid % NG * T::G;
+    const bool swap = SWAP && T::SPLIT && (tid & 2);  // NG is a multiple of 4
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      if (RPG <= T::C || tid / NG < T::C) *reinterpret_cast<u4*>(p + i * RPG * ROW<T, W>) = u[i];
-      if (CHECK) acc = check_finite(u[i], acc, (T*)nullptr);
-    }
+    for (int i = 0; i < PER; ++i)
+      if (RPG <= T::C || tid / NG < T::C)
+        *reinterpret_cast<u4*>(p + i * RPG * ROW<T, W>) =
+            swap ? u4{u[i][2], u[i][3], u[i][0], u[i][1]} : u[i];
+  }
+  // Zero, or NaN if an element is not finite.
+  __device__ __forceinline__ float finite() const {
+    float acc = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc = check_finite(u[i], acc, (T*)nullptr);
     return acc;
   }
 };
@@ -341,9 +415,9 @@ struct Tile {
 // products with an input are summed by step (with the states kept for dg).
 enum Mode { CARRY, OUT, GRAD };
 
-template <class T, int KP, int NWV, Mode MODE>
+template <class T, int KP, int NT, Mode MODE>
 struct Shared {
-  static constexpr int VT = 16 * NWV, C = T::C;
+  static constexpr int VT = 64 * NT, C = T::C;
   static constexpr int NS = MODE == GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
   static constexpr bool XS = MODE != CARRY;
   // fp32 results take the decays between steps to fp32: their running sums in two parts
@@ -351,16 +425,24 @@ struct Shared {
   typename T::E y[C * ROW<T, KP>];
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
-  typename T::E p[XS ? NS * C * C : 8];  // granule c of row t at c ^ (t % 8)
+  typename T::E p[XS ? NS * P_SIZE<T> : 8];
   float gh[C], gl[FINE ? C : 4];  // by step: the running log2 decay, high and low parts
   float er[C];                    // by step: rscale 2^G
   float g1[C];                    // by step: its own decay
   float ph[C], pl[FINE ? C : 4];  // by place: gh and gl
   float ew[C];                    // by place: wscale 2^(G_C - G)
-  float dots[MODE == GRAD ? NWV * C : 4];
+  // bf16 outputs leave as whole rows: a wave's columns are 32 or 64 bytes of each step's
+  static constexpr bool ROWS = MODE == OUT && T::SPLIT;
+  typename T::E o[ROWS ? C * VT : 8];  // granule c of row t at c ^ oswz(t)
+  float dots[MODE == GRAD ? 4 * C : 4];
   float ec;                       // 2^G_C
   uint32_t bad[2];                // the chunk (of odd or even number) holds what is not finite
 };
+
+template <int VT>
+__device__ __forceinline__ int oswz(int t) {
+  return VT == 128 ? t & 15 : (t >> 1) & 7;
+}
 
 // The lane's place in a fragment, worked out anew: what is derived from it (each
 // phase's addresses in LDS) is not kept in registers across the walk.
@@ -372,21 +454,23 @@ __device__ __forceinline__ LanePlace lane_place(int tid) {
   return {(tid >> 4) & 3, tid & 15};
 }
 
-// Waves per SIMD.  Eight waves share the tiles of X and Y and keep 16 columns of S
-// each, so that two such workgroups (four waves per SIMD, 128 registers) fit a
-// compute unit at KP = 128: with two waves of 32 columns each, half of the time
-// went in waiting (B=1 L=65536 H=40 K=V=128, the walk: 686 us).
-constexpr int walk_waves(int KP, int NWV, Mode m) { return KP >= 256 ? 2 : 4; }
+// Waves per SIMD, as the accumulators of S and out (16 NT + KP NT / 2 registers) and
+// the loads in flight leave room for.  Wider tiles a wave (NT = 2) read each
+// fragment of X, Y and P for twice the products: with eight waves of 16 columns
+// instead, LDS reads doubled and set the pace.
+constexpr int walk_waves(int KP, int NT, Mode m) {
+  return KP >= 256 ? 1 : NT == 2 ? 2 : KP == 128 || m == GRAD ? 2 : 4;
+}
 
-template <class T, int KP, int NWV, Mode MODE, bool VEC>
-__global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kernel(WalkArgs a) {
+template <class T, int KP, int NT, Mode MODE, bool VEC>
+__global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(WalkArgs a) {
   typedef typename T::E E;
-  typedef Shared<T, KP, NWV, MODE> Sh;
+  typedef Shared<T, KP, NT, MODE> Sh;
   constexpr bool XS = MODE != CARRY;
-  constexpr int C = T::C, KT = KP / 16, VT = 16 * NWV, SB = C / 32, TT = C / 16, NS = Sh::NS;
-  constexpr int THREADS = 64 * NWV;
+  constexpr int C = T::C, KT = KP / 16, VT = 64 * NT, SB = C / 32, TT = C / 16, NS = Sh::NS;
+  constexpr int THREADS = 256;
   // P: each wave a tile of 16 steps t and ST tiles of 16 steps s
-  constexpr int ST = C == 32 ? 1 : 16 / NWV;
+  constexpr int ST = C == 32 ? 1 : 4;
   constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, G = T::G;
   __shared__ __align__(16) Sh sh;
 
@@ -406,7 +490,7 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
   const bool final_seg = rev ? pl.part == 0 : pl.part == pl.parts - 1;
   if (MODE == CARRY && final_seg) return;
   const int64_t b = a.cu ? 0 : pl.n;
-  const int v0 = tile * VT, vb = wave * 16;  // the tile's first column; the wave's in it
+  const int v0 = tile * VT, vb = wave * 16 * NT;  // the tile's first column; the wave's in it
 
   // steps [lo, hi) of the sequence, in chunks of at most C
   const int len = (int)pl.len, lo = (int)(pl.part * a.lseg);
@@ -420,36 +504,43 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
   const E* Z = (const E*)job.Z.p + b * job.Z.sb + pl.first * job.Z.sl + h / job.zdiv * job.Z.sh + v0;
   const float* gp = a.g + b * a.g_sb + pl.first * a.g_sl + h * a.g_sh;
 
-  f4 S[KT];
-  // state element of accumulator (kt, i): Y's column 32 (kt / 2) + 8 g + 4 (kt % 2) + i,
-  // Z's column v0 + vb + r
+  f4 S[KT][NT];
+  // state element of accumulator (kt, nt, i): Y's column 32 (kt / 2) + 8 g + 4 (kt % 2) + i,
+  // Z's v0 + vb + 16 nt + r
   auto each_state = [&](auto fn) __attribute__((always_inline)) {
     int kk = 8 * g, vv = v0 + vb + r;
     asm volatile("" : "+v"(kk), "+v"(vv));  // worked out here, not kept across the walk
-    if (vv < a.VV) {
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
+    for (int nt = 0; nt < NT; ++nt)
+      if (vv + 16 * nt < a.VV) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int k = kk + 32 * (kt >> 1) + 4 * (kt & 1) + i;
-          if (k < a.KK) fn(kt, i, k * job.skk + vv * job.svv);
-        }
-    }
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = kk + 32 * (kt >> 1) + 4 * (kt & 1) + i;
+            if (k < a.KK) fn(kt, nt, i, k * job.skk + (vv + 16 * nt) * job.svv);
+          }
+      }
   };
   auto store_state = [&](float* p, float f) __attribute__((always_inline)) {
-    each_state([&](int kt, int i, int64_t at) __attribute__((always_inline)) { p[at] = S[kt][i] * f; });
+    each_state([&](int kt, int nt, int i, int64_t at)
+                   __attribute__((always_inline)) { p[at] = S[kt][nt][i] * f; });
   };
   auto anchor_at = [&](int64_t i) {  // the sequence's i-th
     const int64_t per = (a.L + ANCHOR - 1) / ANCHOR;
     return job.anchors + ((first_slot(pl, a.cu, ANCHOR, per) + i) * a.H + h) * a.KV;
   };
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt) S[kt] = f4{0.f, 0.f, 0.f, 0.f};
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) S[kt][nt] = f4{0.f, 0.f, 0.f, 0.f};
   if (XS) {
     const float* p = job.carry ? job.carry + (slot * a.H + h) * a.KV
                      : job.init ? job.init + (pl.n * a.H + h) * a.KV
                                 : nullptr;
-    if (p) each_state([&](int kt, int i, int64_t at) __attribute__((always_inline)) { S[kt][i] = p[at]; });
+    if (p)
+      each_state([&](int kt, int nt, int i, int64_t at)
+                     __attribute__((always_inline)) { S[kt][nt][i] = p[at]; });
   }
   float seg_decay = 1.0f;
 
@@ -484,19 +575,15 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
   for (int c = 0; c < nch; ++c) {
     // what is not finite in X and Y meets its own steps and columns only; in Z, zero
     // weights too
-    const float fin = tz.template store<true>(sh.z, tid);
-    ty.template store<false>(sh.y, tid);
+    const float fin = tz.finite();
+    tz.template store<false>(sh.z, tid);
+    ty.template store<true>(sh.y, tid);
     if (XS) tx.template store<false>(sh.x, tid);
     if (fin != fin) sh.bad[c & 1] = 1;
     if (wave == 0) {
       const double g1 = (double)clamp_g(tg) * 1.4426950408889634;
-      double G = lane < n ? g1 : 0.0;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const double up = __shfl_up(G, d);
-        if (lane >= d) G += up;
-      }
-      const double GC = __shfl(G, 63);
+      double GC;
+      const double G = wave_running_sum(lane < n ? g1 : 0.0, &GC);
       if (lane < C) {
         const int q = place_in(lane);
         const float hi_ = (float)G, lo_ = (float)(G - (double)hi_);
@@ -528,19 +615,26 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
         const float a1 = sh.g1[i];
         int vc = v0 + vb + r, kg = 8 * g;
         asm volatile("" : "+v"(vc), "+v"(kg));  // worked out here, not kept across the walk
-        const float z = widen1(sh.z[i * VR + vc - v0]);
-        float xy = 0.0f, acc = 0.0f;
+        float xy = 0.0f, d = 0.0f, acc[NT], z[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          acc[nt] = 0.0f;
+          z[nt] = widen1(sh.z[i * VR + vc - v0 + 16 * nt]);
+        }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int kk = kg + 32 * (kt >> 1) + 4 * (kt & 1) + j;
             if (kk < a.KK) {
-              const float y = widen1(sh.y[i * KR + kk]);
+              const float y = widen1(sh.y[i * KR + (T::SPLIT && (kk & 16) ? kk ^ 4 : kk)]);
               const float x = XS ? widen1(sh.x[i * KR + kk]) : 0.0f;
               xy = __builtin_fmaf(x, y, xy);
-              acc = __builtin_fmaf(x, S[kt][j], acc);
-              S[kt][j] = __builtin_fmaf(y, job.wscale * z, a1 * S[kt][j]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                acc[nt] = __builtin_fmaf(x, S[kt][nt][j], acc[nt]);
+                S[kt][nt][j] = __builtin_fmaf(y, job.wscale * z[nt], a1 * S[kt][nt][j]);
+              }
             }
           }
         if (MODE == CARRY) seg_decay *= a1;
@@ -548,17 +642,19 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
           const int64_t t = tfirst + tstep * i;
           xy += __shfl_xor(xy, 16);
           xy += __shfl_xor(xy, 32);
-          acc += __shfl_xor(acc, 16);
-          acc += __shfl_xor(acc, 32);
-          const float y = a1 * job.rscale * acc + job.pscale * xy * z;
-          float d = 0.0f;
-          if (g == 0 && vc < a.VV) {
-            const int64_t off = ob + t * job.ol + vc;
-            if (T::SPLIT && !job.out_f32)
-              ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
-            else
-              ((float*)job.out)[off] = y;
-            if (MODE == GRAD) d = y * widen1(ap[t * job.A.sl + vc]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            acc[nt] += __shfl_xor(acc[nt], 16);
+            acc[nt] += __shfl_xor(acc[nt], 32);
+            const float y = a1 * job.rscale * acc[nt] + job.pscale * xy * z[nt];
+            if (g == 0 && vc + 16 * nt < a.VV) {
+              const int64_t off = ob + t * job.ol + vc + 16 * nt;
+              if (T::SPLIT && !job.out_f32)
+                ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
+              else
+                ((float*)job.out)[off] = y;
+              if (MODE == GRAD) d += y * widen1(ap[t * job.A.sl + vc + 16 * nt]);
+            }
           }
           if (MODE == GRAD) {
 #pragma unroll
@@ -569,7 +665,7 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
       }
       load_chunk(c + 1);
     } else {
-      f4 O[TT];
+      f4 O[TT][NT];
       if (XS) {
         // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
         const int tt = wave & (TT - 1), q0 = 16 * ST * (wave / TT);
@@ -582,12 +678,12 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
           for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
           // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; what step_of adds for
           // st is constant
-          auto more = [](int st) { return ST == 4 ? 16 * (st & 1) + (st >> 1) : 16 * st; };
+          auto more = [](int st) { return ST == 4 ? 16 * (st & 1) + 4 * (st >> 1) : 16 * st; };
           const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
           const E* const xr = sh.x + t * KR + 8 * g;
 #pragma unroll
           for (int p = 0; p < KP / 32; ++p) {
-            const Frag<T> xf = row_frag(xr + 32 * p);
+            const Frag<T> xf = as_y(row_frag(xr + 32 * p), g);
 #pragma unroll
             for (int st = 0; st < ST; ++st)
               acc[st] = mma(row_frag(yr + more(st) * KR + 32 * p), xf, acc[st]);
@@ -606,21 +702,24 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d[i]) * job.pscale);
-              pv[4 * st + i] = more(st) + 4 * i <= ahead ? e : 0.0f;
+              pv[4 * st + i] = more(st) + i <= ahead ? e : 0.0f;
             }
           }
-          E* const pw = sh.p + t * C;
+          E* const pw = sh.p + p_row<T>(t);
+          const int m = pswz<T>(t);
           if constexpr (T::SPLIT) {
+            if (t >= 32 || qf < 32) {
 #pragma unroll
-            for (int half = 0; half < ST / 2; ++half) {
-              Frag<T> f[NS];
-              parts_of<NS>(pv + 8 * half, f);
+              for (int half = 0; half < ST / 2; ++half) {
+                Frag<T> f[NS];
+                parts_of<NS>(pv + 8 * half, f);
 #pragma unroll
-              for (int i = 0; i < NS; ++i)
-                *reinterpret_cast<s8*>(pw + i * C * C + ((qf / 8 + half) ^ (t & 7)) * 8) = f[i].v;
+                for (int i = 0; i < NS; ++i)
+                  *reinterpret_cast<s8*>(pw + i * P_SIZE<T> + ((qf / 8 + half) ^ m) * 8) = f[i].v;
+              }
             }
           } else {
-            *reinterpret_cast<f4*>(pw + ((qf / 4) ^ (t & 7)) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
+            *reinterpret_cast<f4*>(pw + ((qf / 4) ^ m) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
           }
         }
 
@@ -628,26 +727,37 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
         const auto [g, r] = lane_place(tid);
         const E* const xrow = sh.x + r * KR + 8 * g;
 #pragma unroll
-        for (int i = 0; i < TT; ++i) O[i] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < TT; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < KP / 32; ++p) {
-          Frag<T> sf[NS];
-          float x[8];
+          Frag<T> sf[NT][NS];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[i] = S[2 * p][i];
-            x[4 + i] = S[2 * p + 1][i];
+          for (int nt = 0; nt < NT; ++nt) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[i] = S[2 * p][nt][i];
+              x[4 + i] = S[2 * p + 1][nt][i];
+            }
+            parts_of<NS>(x, sf[nt]);
           }
-          parts_of<NS>(x, sf);
 #pragma unroll
           for (int i = 0; i < TT; ++i) {
             const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
 #pragma unroll
-            for (int q = NS - 1; q >= 0; --q) O[i] = mma(sf[q], xf, O[i]);
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sf[nt][q], xf, O[i][nt]);
           }
         }
 #pragma unroll
-        for (int i = 0; i < TT; ++i) O[i] *= sh.er[i * 16 + r];
+        for (int i = 0; i < TT; ++i) {
+          const float er = sh.er[i * 16 + r];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
+        }
       }
 
       load_chunk(c + 1);  // in flight while the state moves on; earlier, its registers would spill
@@ -656,92 +766,119 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
       const float ec = sh.ec;
       if (MODE == CARRY) seg_decay *= ec;
       const auto [g, r] = lane_place(tid);
-      const E* const ycol = col_base<KP, 8>(sh.y, g, r);
-      const E* const zcol = col_base<VT, 4>(sh.z, g, r) + vb;
+      const E* const ycol[2] = {y_base<KP>(sh.y, g, r, 0), y_base<KP>(sh.y, g, r, 1)};
+      const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) S[kt] *= ec;
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
 #pragma unroll
       for (int sb = 0; sb < SB; ++sb) {
-        Frag<T> wf[T::NW];
-        float ew[8], x[8];
+        Frag<T> wf[NT][T::NW];
+        float ew[8];
         *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
         *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
-        widen(col_frag<VT>(zcol + 32 * sb * VR), x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= ew[j];
-        parts_of<T::NW>(x, wf);
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[8];
+          widen(col_frag<VT>(zcol + 32 * sb * VR + 16 * nt), x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] *= ew[j];
+          parts_of<T::NW>(x, wf[nt]);
+        }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-          const Frag<T> yf = col_frag<KP>(ycol + 32 * sb * KR + 32 * (kt >> 1) + 4 * (kt & 1));
+          const Frag<T> yf = col_frag<KP>(ycol[kt & 1] + 32 * sb * KR + 32 * (kt >> 1));
 #pragma unroll
-          for (int q = T::NW - 1; q >= 0; --q) S[kt] = mma(yf, wf[q], S[kt]);
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
         }
       }
 
       if (XS) {
         __syncthreads();  // P is whole
         const auto [g, r] = lane_place(tid);
-        const E* const zcol = col_base<VT, 4>(sh.z, g, r) + vb;
-        const E* const prow = sh.p + r * C;
-        const int pg = 8 / G * g;  // a lane's eight places: whole granules of P's row 16 i + r
+        const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
 #pragma unroll
         for (int sb = 0; sb < SB; ++sb) {
-          const Frag<T> zf = col_frag<VT>(zcol + 32 * sb * VR);
+          Frag<T> zf[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 16 * nt);
 #pragma unroll
           for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
 #pragma unroll
-            for (int q = NS - 1; q >= 0; --q)
-              O[i] = mma(zf, p_frag(prow + (q * C + i * 16) * C, 32 / G * sb + pg, r & 7), O[i]);
+            for (int q = NS - 1; q >= 0; --q) {
+              const Frag<T> pf = p_frag(sh.p + q * P_SIZE<T>, i * 16 + r, sb, g);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
+            }
         }
 
-        // this lane: rows i * 16 + r of the chunk, columns vc .. vc + 3
+        // this lane: rows i * 16 + r of the chunk, columns vc + 16 nt .. + 3
         const int vc = v0 + vb + 4 * g;
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
           const int row = i * 16 + r;
-          const bool live = row < cnt && vc < a.VV;
           const int64_t t = tfirst + tstep * row;
-          if constexpr (MODE == GRAD) {
-            float d = 0.0f;
-            if (live) {
-              const E* p = ap + t * job.A.sl + vc;
-              if (job.avec) {
-                E e[4];
-                __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * sizeof(E)), sizeof(e));
+          float d = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][j], widen1(e[j]), d);
-              } else {
+          for (int nt = 0; nt < NT; ++nt) {
+            const int v = vc + 16 * nt;
+            const bool live = row < cnt && v < a.VV;
+            if constexpr (MODE == GRAD) {
+              if (live) {
+                const E* p = ap + t * job.A.sl + v;
+                if (job.avec) {
+                  E e[4];
+                  __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * sizeof(E)), sizeof(e));
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (vc + j < a.VV) d = __builtin_fmaf(O[i][j], widen1(p[j]), d);
+                  for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][nt][j], widen1(e[j]), d);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    if (v + j < a.VV) d = __builtin_fmaf(O[i][nt][j], widen1(p[j]), d);
+                }
               }
             }
+            if constexpr (Sh::ROWS) {
+              if (job.orows) {
+                const int c = 2 * (NT * wave + nt) + (g >> 1);  // its granule
+                *reinterpret_cast<uint2*>(sh.o + row * VT + (c ^ oswz<VT>(row)) * 8 + 4 * (g & 1)) =
+                    make_uint2(bf16x2_rne(O[i][nt][0], O[i][nt][1]),
+                               bf16x2_rne(O[i][nt][2], O[i][nt][3]));
+                continue;
+              }
+            }
+            if (live) {
+              const int64_t off = ob + t * job.ol + v;
+              if (T::SPLIT && !job.out_f32) {
+                uint16_t* op = (uint16_t*)job.out + off;
+                const uint32_t u[2] = {bf16x2_rne(O[i][nt][0], O[i][nt][1]),
+                                       bf16x2_rne(O[i][nt][2], O[i][nt][3])};
+                if (job.ovec) {
+                  *reinterpret_cast<uint2*>(op) = make_uint2(u[0], u[1]);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    if (v + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
+                }
+              } else {
+                float* op = (float*)job.out + off;
+                if (job.ovec) {
+                  *reinterpret_cast<f4*>(op) = O[i][nt];
+                } else {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    if (v + j < a.VV) op[j] = O[i][nt][j];
+                }
+              }
+            }
+          }
+          if constexpr (MODE == GRAD) {
             d += __shfl_xor(d, 16);
             d += __shfl_xor(d, 32);
             if (g == 0) sh.dots[wave * C + row] = d;
-          }
-          if (live) {
-            const int64_t off = ob + t * job.ol + vc;
-            if (T::SPLIT && !job.out_f32) {
-              uint16_t* op = (uint16_t*)job.out + off;
-              const uint32_t u[2] = {bf16x2_rne(O[i][0], O[i][1]), bf16x2_rne(O[i][2], O[i][3])};
-              if (job.ovec) {
-                *reinterpret_cast<uint2*>(op) = make_uint2(u[0], u[1]);
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (vc + j < a.VV) op[j] = (uint16_t)(u[j / 2] >> (16 * (j & 1)));
-              }
-            } else {
-              float* op = (float*)job.out + off;
-              if (job.ovec) {
-                *reinterpret_cast<f4*>(op) = O[i];
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (vc + j < a.VV) op[j] = O[i][j];
-              }
-            }
           }
         }
       }
@@ -751,11 +888,26 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
         store_state(anchor_at(reached / ANCHOR - 1), 1.0f);
     }
     __syncthreads();  // the tiles are free
+    if constexpr (Sh::ROWS) {
+      if (job.orows && !bad) {
+        constexpr int NG = VT / G;
+        int id = tid;
+        asm volatile("" : "+v"(id));
+        const int col = id % NG * G;
+#pragma unroll
+        for (int i = 0; i < C * NG / THREADS; ++i) {
+          const int row = id / NG + i * (THREADS / NG);
+          if (row < cnt && v0 + col < a.VV)
+            *reinterpret_cast<u4*>((E*)job.out + ob + (tfirst + tstep * row) * job.ol + v0 + col) =
+                *reinterpret_cast<const u4*>(sh.o + row * VT + (col / G ^ oswz<VT>(row)) * G);
+        }
+      }
+    }
     if constexpr (MODE == GRAD) {
       if (wave == 0 && lane < cnt) {
         float d = 0.0f;
 #pragma unroll
-        for (int q = 0; q < NWV; ++q) d += sh.dots[q * C + lane];
+        for (int q = 0; q < 4; ++q) d += sh.dots[q * C + lane];
         job.dots[((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst +
                  tstep * lane] = d;
       }
@@ -775,45 +927,45 @@ __global__ __launch_bounds__(64 * NWV, walk_waves(KP, NWV, MODE)) void walk_kern
   }
 }
 
-template <class T, int KP, int NWV, bool VEC>
+template <class T, int KP, int NT, bool VEC>
 int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
-  const dim3 grid((unsigned)wgs), block(64 * NWV);
+  const dim3 grid((unsigned)wgs), block(256);
   if (m == CARRY)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, CARRY, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY, VEC>), grid, block, 0, st, a);
   else if (m == GRAD)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, GRAD, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD, VEC>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((walk_kernel<T, KP, NWV, OUT, VEC>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
   return check_launch("walk_kernel");
 }
 
 // The instance: X's and Y's columns rounded up to 32, 64, 128 or 256; tiles of
-// 16 columns of Z for each of 4 or 8 waves.
+// 64 nt of Z's columns (nt = 1 above 128 columns of Y: the state's registers).
 template <class T, bool VEC>
-int launch_walk_vec(const WalkArgs& a, Mode m, int waves, int64_t wgs, hipStream_t st) {
-#define SW_WALK(KP)                                                \
-  return waves == 4 ? launch_walk_at<T, KP, 4, VEC>(a, m, wgs, st) \
-                    : launch_walk_at<T, KP, 8, VEC>(a, m, wgs, st)
+int launch_walk_vec(const WalkArgs& a, Mode m, int nt, int64_t wgs, hipStream_t st) {
+#define SW_WALK(KP)                                             \
+  return nt == 1 ? launch_walk_at<T, KP, 1, VEC>(a, m, wgs, st) \
+                 : launch_walk_at<T, KP, 2, VEC>(a, m, wgs, st)
   if (a.KK <= 32) SW_WALK(32);
   if (a.KK <= 64) SW_WALK(64);
   if (a.KK <= 128) SW_WALK(128);
-  SW_WALK(256);
+  return launch_walk_at<T, 256, 1, VEC>(a, m, wgs, st);
 #undef SW_WALK
 }
 
 template <class T>
-int launch_walk(const WalkArgs& a, Mode m, int waves, hipStream_t st) {
+int launch_walk(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
   const int64_t wgs = a.slots * a.H * a.tiles * a.njobs;
   if (wgs == 0) return SW_OK;
   bool vec = true;
   for (int i = 0; i < a.njobs; ++i)
     vec = vec && (m == CARRY || a.job[i].xvec) && a.job[i].yvec && a.job[i].zvec;
-  return vec ? launch_walk_vec<T, true>(a, m, waves, wgs, st)
-             : launch_walk_vec<T, false>(a, m, waves, wgs, st);
+  return vec ? launch_walk_vec<T, true>(a, m, nt, wgs, st)
+             : launch_walk_vec<T, false>(a, m, nt, wgs, st);
 }
 
-int launch_walk_bf16(const WalkArgs& a, Mode m, int waves, hipStream_t st);
-int launch_walk_f32(const WalkArgs& a, Mode m, int waves, hipStream_t st);
+int launch_walk_bf16(const WalkArgs& a, Mode m, int nt, hipStream_t st);
+int launch_walk_f32(const WalkArgs& a, Mode m, int nt, hipStream_t st);
 
 }  // namespace lin
 }  // namespace sw

@@ -3,8 +3,8 @@
 
 namespace sw {
 namespace lin {
-int launch_walk_bf16(const WalkArgs& a, Mode m, int waves, hipStream_t st) {
-  return launch_walk<Bf16>(a, m, waves, st);
+int launch_walk_bf16(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
+  return launch_walk<Bf16>(a, m, nt, st);
 }
 }  // namespace lin
 }  // namespace sw
