@@ -1,6 +1,8 @@
 // linear_attn.hip -- linear attention with a log decay for each head: plans
 // the chunked walks of linear_walk.h, composes their segments, forms the
 // decays' gradient and the sums over shared heads; and the one-step form.
+#include <math.h>
+
 #include "linear_walk.h"
 
 namespace sw {
@@ -320,7 +322,9 @@ Job make_job(const LinAttnArgs& a, const Role& X, const Role& Y, const Role& Z, 
   j.zvec = rows_vec(j.Z, zw, a.bf16);
   j.skk = swapped ? 1 : a.V;
   j.svv = swapped ? a.V : 1;
-  j.pscale = a.scale;
+  j.pabs = fabsf(a.scale);
+  j.plog = log2((double)j.pabs);
+  j.neg = a.scale < 0.0f;
   j.wscale = 1.0f;
   j.rscale = 1.0f;
   return j;
@@ -427,7 +431,7 @@ int linear_attn_fwd(const LinAttnArgs& a) {
   const int r = (int)(a.H / a.Hk);
   WalkArgs w = walk_args(a, p);
   Job j = make_job(a, {a.q, r}, {a.k, r}, {a.v, 1}, false);
-  j.rscale = a.scale;
+  j.rscale = fabsf(a.scale);
   j.init = a.h0;
   j.last = a.h_last;
   set_out(j, a, a.o, a.H, a.V, !a.bf16);
@@ -460,15 +464,17 @@ int linear_attn_bwd(const LinAttnArgs& a) {
 
   WalkArgs w = walk_args(a, p);
   Job jq = make_job(a, dout, v, k, true);
-  jq.rscale = a.scale;
+  jq.rscale = fabsf(a.scale);
   jq.init = a.h0;
   Job jk = make_job(a, v, dout, q, true);
   jk.reverse = true;
-  jk.wscale = a.scale;
+  jk.wscale = a.scale;  // the state holds the scale with its sign
+  jk.rscale = jk.neg ? -1.0f : 1.0f;
   jk.init = a.dh_last;
   Job jv = make_job(a, k, q, dout, false);
   jv.reverse = true;
   jv.wscale = a.scale;
+  jv.rscale = jv.neg ? -1.0f : 1.0f;
   jv.init = a.dh_last;
   jv.last = a.dh0;
   set_out(jv, a, a.dv, a.H, a.V, !a.bf16);

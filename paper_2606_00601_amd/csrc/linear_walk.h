@@ -55,7 +55,11 @@ struct Job {
   float* anchors;        // (anchor slots, H, K, V) or NULL
   bool last_anchor;      // the state after the last step is an anchor too
   int64_t skk, svv;      // where state element (Y's column, Z's column) lies in (K, V)
-  float pscale, wscale, rscale;
+  // scales of P (its absolute value and log2), of the state's increments and of the
+  // read-out; neg: out changes its sign
+  float pabs, wscale, rscale;
+  double plog;
+  bool neg;
 };
 
 struct WalkArgs {
@@ -200,10 +204,7 @@ __device__ __forceinline__ f4 mma(const Frag<F32>& a, const Frag<F32>& b, f4 c) 
 template <class T, int W>
 constexpr int ROW = W + 2 * T::G;
 
-// Place q of a chunk is this step; and the other way round.
-__device__ __forceinline__ int step_of(int q) {
-  return (q & ~31) + 16 * ((q >> 2) & 1) + 4 * ((q >> 3) & 3) + (q & 3);
-}
+// Step s's place in its chunk.
 __device__ __forceinline__ int place_in(int s) {
   return (s & ~31) + 8 * ((s >> 2) & 3) + 4 * ((s >> 4) & 1) + (s & 3);
 }
@@ -426,16 +427,19 @@ struct Shared {
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
   typename T::E p[XS ? NS * P_SIZE<T> : 8];
-  float gh[C], gl[FINE ? C : 4];  // by step: the running log2 decay, high and low parts
-  float er[C];                    // by step: rscale 2^G
-  float g1[C];                    // by step: its own decay
-  float ph[C], pl[FINE ? C : 4];  // by place: gh and gl
-  float ew[C];                    // by place: wscale 2^(G_C - G)
+  // A chunk's decays, of this chunk and the next.
+  struct Decays {
+    float gs[C], gsl[FINE ? C : 4];  // by step s: the running log2 decay, high and low parts
+    float gt[C], gtl[FINE ? C : 4];  // by step t: the same with log2 |pscale|
+    float er[C];                     // by step: rscale 2^G
+    float g1[C];                     // by step: its own decay
+    float ew[C];                     // by place: wscale 2^(G_C - G)
+    float ec;                        // 2^G_C
+  } dec[2];
   // bf16 outputs leave as whole rows: a wave's columns are 32 or 64 bytes of each step's
   static constexpr bool ROWS = MODE == OUT && T::SPLIT;
   typename T::E o[ROWS ? C * VT : 8];  // granule c of row t at c ^ oswz(t)
   float dots[MODE == GRAD ? 4 * C : 4];
-  float ec;                       // 2^G_C
   uint32_t bad[2];                // the chunk (of odd or even number) holds what is not finite
 };
 
@@ -443,6 +447,11 @@ template <int VT>
 __device__ __forceinline__ int oswz(int t) {
   return VT == 128 ? t & 15 : (t >> 1) & 7;
 }
+
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
 
 // The lane's place in a fragment, worked out anew: what is derived from it (each
 // phase's addresses in LDS) is not kept in registers across the walk.
@@ -469,8 +478,6 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   constexpr bool XS = MODE != CARRY;
   constexpr int C = T::C, KT = KP / 16, VT = 64 * NT, SB = C / 32, TT = C / 16, NS = Sh::NS;
   constexpr int THREADS = 256;
-  // P: each wave a tile of 16 steps t and ST tiles of 16 steps s
-  constexpr int ST = C == 32 ? 1 : 4;
   constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, G = T::G;
   __shared__ __align__(16) Sh sh;
 
@@ -555,11 +562,41 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     if (XS) tx.load(X + t * job.X.sl, job.X.sl, n, rev, a.KK, tid);
     ty.load(Y + t * job.Y.sl, job.Y.sl, n, rev, a.KK, tid);
     tz.load(Z + t * job.Z.sl, job.Z.sl, n, rev, a.VV - v0, tid);
-    if (wave == 0) {
-      // backwards, a step's decay is that of the step after it in time; none at the end
-      const int64_t s = rev ? t + n - lane : t + lane;
-      tg = lane < n && s < len ? gp[s * a.g_sl] : 0.0f;
+  };
+  // The first wave works out a chunk's decays while the others still multiply for
+  // the chunk before (it has the least to do above P's diagonal); their g is on its
+  // way a chunk earlier still.
+  auto cnt_of = [&](int c) {
+    const int c0 = lo + (rev ? nch - 1 - c : c) * C;
+    return c >= nch ? 0 : hi - c0 < C ? hi - c0 : C;
+  };
+  auto load_decays = [&](int c) __attribute__((always_inline)) {
+    const int c0 = lo + (rev ? nch - 1 - c : c) * C, cn = cnt_of(c);
+    // backwards, a step's decay is that of the step after it in time; none at the end
+    const int s = rev ? c0 + cn - lane : c0 + lane;
+    tg = lane < cn && s < len ? gp[s * a.g_sl] : 0.0f;
+  };
+  auto put_decays = [&](int c) __attribute__((always_inline)) {
+    typename Sh::Decays& d = sh.dec[c & 1];
+    const double g1 = (double)clamp_g(tg) * 1.4426950408889634;
+    double GC;
+    const double G = wave_running_sum(lane < cnt_of(c) ? g1 : 0.0, &GC);
+    if (lane < C) {
+      if (XS) {
+        const double Gt = G + job.plog;
+        const float s_ = (float)G, t_ = (float)Gt;
+        d.gs[lane] = s_;
+        d.gt[lane] = t_;
+        if (Sh::FINE) {
+          d.gsl[lane] = (float)(G - (double)s_);
+          d.gtl[lane] = job.plog > -1.0e30 ? (float)(Gt - (double)t_) : 0.0f;
+        }
+        d.er[lane] = exp2_of(G) * job.rscale;
+      }
+      d.ew[place_in(lane)] = exp2_of(GC - G) * job.wscale;
+      d.g1[lane] = exp2_of(g1);
     }
+    if (lane == 0) d.ec = exp2_of(GC);
   };
 
   const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh;
@@ -570,6 +607,11 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   if (tid < 2) sh.bad[tid] = 0;
   if (nch > 0) {
     load_chunk(0);
+    if (wave == 0) {
+      load_decays(0);
+      put_decays(0);
+      load_decays(1);
+    }
     __syncthreads();
   }
   for (int c = 0; c < nch; ++c) {
@@ -580,27 +622,9 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     ty.template store<true>(sh.y, tid);
     if (XS) tx.template store<false>(sh.x, tid);
     if (fin != fin) sh.bad[c & 1] = 1;
-    if (wave == 0) {
-      const double g1 = (double)clamp_g(tg) * 1.4426950408889634;
-      double GC;
-      const double G = wave_running_sum(lane < n ? g1 : 0.0, &GC);
-      if (lane < C) {
-        const int q = place_in(lane);
-        const float hi_ = (float)G, lo_ = (float)(G - (double)hi_);
-        sh.gh[lane] = hi_;
-        sh.ph[q] = hi_;
-        if (Sh::FINE) {
-          sh.gl[lane] = lo_;
-          sh.pl[q] = lo_;
-        }
-        sh.er[lane] = exp2_of(G) * job.rscale;
-        sh.ew[q] = exp2_of(GC - G) * job.wscale;
-        sh.g1[lane] = exp2_of(g1);
-      }
-      if (lane == 0) sh.ec = exp2_of(GC);
-    }
     __syncthreads();
     const bool bad = sh.bad[c & 1];
+    const typename Sh::Decays& dec = sh.dec[c & 1];
     if (tid == 0) sh.bad[(c + 1) & 1] = 0;
 
     // rows of this chunk: cnt, the first of them step tfirst, the next tstep on
@@ -612,7 +636,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       // chunk goes step by step, as the recurrence says, on plain arithmetic.
 #pragma unroll 1
       for (int i = 0; i < cnt; ++i) {
-        const float a1 = sh.g1[i];
+        const float a1 = dec.g1[i];
         int vc = v0 + vb + r, kg = 8 * g;
         asm volatile("" : "+v"(vc), "+v"(kg));  // worked out here, not kept across the walk
         float xy = 0.0f, d = 0.0f, acc[NT], z[NT];
@@ -646,7 +670,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
           for (int nt = 0; nt < NT; ++nt) {
             acc[nt] += __shfl_xor(acc[nt], 16);
             acc[nt] += __shfl_xor(acc[nt], 32);
-            const float y = a1 * job.rscale * acc[nt] + job.pscale * xy * z[nt];
+            float y = a1 * job.rscale * acc[nt] + job.pabs * xy * z[nt];
+            if (job.neg) y = -y;
             if (g == 0 && vc + 16 * nt < a.VV) {
               const int64_t off = ob + t * job.ol + vc + 16 * nt;
               if (T::SPLIT && !job.out_f32)
@@ -664,63 +689,80 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         }
       }
       load_chunk(c + 1);
+      if (wave == 0) {
+        put_decays(c + 1);
+        load_decays(c + 2);
+      }
     } else {
       f4 O[TT][NT];
       if (XS) {
-        // P^T = Y X^T (rows s by place, columns t), weighted and handed to the other waves
-        const int tt = wave & (TT - 1), q0 = 16 * ST * (wave / TT);
-        // a wave beyond the tiles, or above the diagonal where nothing is read
-        if (q0 < C && 16 * tt + 15 >= (q0 & ~31)) {
+        // P^T = Y X^T: a wave has 16 steps t (columns) and of the tiles of 16 steps s
+        // (rows) those up to the diagonal's; the pair that holds it is filled with zeros
+        {
           const auto [g, r] = lane_place(tid);
-          const int t = tt * 16 + r;
-          f4 acc[ST];
-#pragma unroll
-          for (int st = 0; st < ST; ++st) acc[st] = f4{0.f, 0.f, 0.f, 0.f};
-          // tile st's row 4 g' + i is place q0 + 4 ST g' + 4 st + i; what step_of adds for
-          // st is constant
-          auto more = [](int st) { return ST == 4 ? 16 * (st & 1) + 4 * (st >> 1) : 16 * st; };
-          const E* const yr = sh.y + step_of(q0 + 4 * ST * (r >> 2) + (r & 3)) * KR + 8 * g;
+          const int tt = wave & (TT - 1), t = tt * 16 + r;
+          const int first = C == 32 ? wave >> 1 : 0;  // its first tile of steps s
+          Frag<T> xf[KP / 32];
           const E* const xr = sh.x + t * KR + 8 * g;
 #pragma unroll
-          for (int p = 0; p < KP / 32; ++p) {
-            const Frag<T> xf = as_y(row_frag(xr + 32 * p), g);
-#pragma unroll
-            for (int st = 0; st < ST; ++st)
-              acc[st] = mma(row_frag(yr + more(st) * KR + 32 * p), xf, acc[st]);
-          }
-          // this lane: step t, places qf .. qf + 4 ST - 1
-          const int qf = q0 + 4 * ST * g;
-          const float ght = sh.gh[t], glt = Sh::FINE ? sh.gl[t] : 0.0f;
-          int ahead = t - step_of(qf);  // steps from the first place's to t
-          asm volatile("" : "+v"(ahead));  // compared here: the masks are not kept
-          float pv[4 * ST];
-#pragma unroll
-          for (int st = 0; st < ST; ++st) {
-            const f4 gh = *reinterpret_cast<const f4*>(sh.ph + qf + 4 * st);
-            f4 d = ght - gh;
-            if (Sh::FINE) d += glt - *reinterpret_cast<const f4*>(sh.pl + qf + 4 * st);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float e = acc[st][i] * (__builtin_amdgcn_exp2f(d[i]) * job.pscale);
-              pv[4 * st + i] = more(st) + i <= ahead ? e : 0.0f;
-            }
-          }
+          for (int p = 0; p < KP / 32; ++p) xf[p] = as_y(row_frag(xr + 32 * p), g);
+          const float gt = dec.gt[t], gtl = Sh::FINE ? dec.gtl[t] : 0.0f;
           E* const pw = sh.p + p_row<T>(t);
           const int m = pswz<T>(t);
-          if constexpr (T::SPLIT) {
-            if (t >= 32 || qf < 32) {
+          // N tiles from `first`, the last of them the diagonal's if `diag`
+          auto weigh = [&](auto count, bool diag) __attribute__((always_inline)) {
+            constexpr int N = decltype(count)::value;
+            f4 acc[N];
 #pragma unroll
-              for (int half = 0; half < ST / 2; ++half) {
-                Frag<T> f[NS];
-                parts_of<NS>(pv + 8 * half, f);
+            for (int i = 0; i < N; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+            const E* const yr = sh.y + (16 * first + r) * KR + 8 * g;
 #pragma unroll
-                for (int i = 0; i < NS; ++i)
-                  *reinterpret_cast<s8*>(pw + i * P_SIZE<T> + ((qf / 8 + half) ^ m) * 8) = f[i].v;
+            for (int p = 0; p < KP / 32; ++p)
+#pragma unroll
+              for (int i = 0; i < N; ++i)
+                acc[i] = mma(row_frag(yr + 16 * i * KR + 32 * p), xf[p], acc[i]);
+            float pv[4 * (N + (N & 1))];
+#pragma unroll
+            for (int i = 0; i < N + (N & 1); ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) pv[4 * i + j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              f4 d = gt - *reinterpret_cast<const f4*>(dec.gs + 16 * (first + i) + 4 * g);
+              if (Sh::FINE) d += gtl - *reinterpret_cast<const f4*>(dec.gsl + 16 * (first + i) + 4 * g);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float e = acc[i][j] * __builtin_amdgcn_exp2f(d[j]);
+                pv[4 * i + j] = i == N - 1 && diag && 4 * g + j > r ? 0.0f : e;
               }
             }
+            if constexpr (T::SPLIT) {
+#pragma unroll
+              for (int i = 0; i < (N + 1) / 2; ++i) {  // places 32 i + 8 g .. + 7
+                Frag<T> f[NS];
+                parts_of<NS>(pv + 8 * i, f);
+#pragma unroll
+                for (int q = 0; q < NS; ++q)
+                  *reinterpret_cast<s8*>(pw + q * P_SIZE<T> + ((4 * i + g) ^ m) * 8) = f[q].v;
+              }
+            } else {  // places 8 g + 4 first .. + 3
+              *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
+            }
+          };
+          if constexpr (C == 64) {
+            if (tt == 0) weigh(Count<1>(), true);
+            else if (tt == 1) weigh(Count<2>(), true);
+            else if (tt == 2) weigh(Count<3>(), true);
+            else weigh(Count<4>(), true);
+          } else if (first <= tt) {
+            weigh(Count<1>(), first == tt);
           } else {
-            *reinterpret_cast<f4*>(pw + ((qf / 4) ^ m) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
+            *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{0.f, 0.f, 0.f, 0.f};
           }
+        }
+        if (wave == 0) {
+          put_decays(c + 1);
+          load_decays(c + 2);
         }
 
         // X S
@@ -754,7 +796,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         }
 #pragma unroll
         for (int i = 0; i < TT; ++i) {
-          const float er = sh.er[i * 16 + r];
+          const float er = dec.er[i * 16 + r];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
         }
@@ -763,7 +805,11 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       load_chunk(c + 1);  // in flight while the state moves on; earlier, its registers would spill
 
       // S <- e^{G_C} S + Y^T (weighted Z)
-      const float ec = sh.ec;
+      if (MODE == CARRY && wave == 0) {
+        put_decays(c + 1);
+        load_decays(c + 2);
+      }
+      const float ec = dec.ec;
       if (MODE == CARRY) seg_decay *= ec;
       const auto [g, r] = lane_place(tid);
       const E* const ycol[2] = {y_base<KP>(sh.y, g, r, 0), y_base<KP>(sh.y, g, r, 1)};
@@ -776,8 +822,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       for (int sb = 0; sb < SB; ++sb) {
         Frag<T> wf[NT][T::NW];
         float ew[8];
-        *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g);
-        *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(sh.ew + 32 * sb + 8 * g + 4);
+        *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g);
+        *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g + 4);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float x[8];
@@ -815,6 +861,12 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
             }
         }
 
+        if (job.neg) {
+#pragma unroll
+          for (int i = 0; i < TT; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O[i][nt] = -O[i][nt];
+        }
         // this lane: rows i * 16 + r of the chunk, columns vc + 16 nt .. + 3
         const int vc = v0 + vb + 4 * g;
 #pragma unroll

@@ -160,6 +160,20 @@ def test_resets_and_lowest_decays(sw, dtype):
     assert (r["dh0"][0, 0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.7, 1e-3])
+def test_scales(sw, scale, dtype):
+    t, x = _inputs(1, 140, 1, 2, 32, 64, 33, dtype, h0=True, dh=True)
+    _check(sw, t, x, scale, dtype)
+    t["v"][0, 70, 0, 5] = float("inf")
+    x["v"][0, 70, 0, 5] = 1.0  # magnitudes alone
+    o = sw.linear_attn_fwd(t["q"], t["k"], t["v"], t["g"], scale=scale, h0=t["h0"])[0]
+    w = ref.attn(x["q"], x["k"], x["v"], x["g"], scale, x["h0"])["o"]
+    m = ref.magnitudes(x["q"], x["k"], x["v"], x["g"], scale, x["h0"])["o"]
+    for part in (np.s_[:, :70], np.s_[:, 70:, 0, :5], np.s_[:, 70:, 1]):
+        _near(o[part], w[part], m[part], BF16 if dtype == "bf16" else F32, "o")
+
+
 def test_strong_and_growing_decays(sw):
     """Decays that underflow within a chunk, and states that grow."""
     t, x = _inputs(1, 200, 1, 2, 32, 32, 31, "f32", rate=40.0)
