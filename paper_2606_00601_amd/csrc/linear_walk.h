@@ -367,10 +367,10 @@ struct Tile {
   __device__ __forceinline__ void load(const E* rows, int64_t step, int n, bool rev, int width,
                                        int tid) {
     asm volatile("" : "+v"(tid));  // offsets worked out here, not kept across the walk
-    const int row = tid / NG, col = tid % NG * T::G;
+    const int row = (unsigned)tid / NG, col = (unsigned)tid % NG * T::G;
     if constexpr (VEC) {
       const int st = (int)step * (int)sizeof(E);
-      const int end = n > 0 ? (n - 1) * st + (width < W ? width : W) * (int)sizeof(E) : 0;
+      const int end = max((n - 1) * st + min(width, W) * (int)sizeof(E), 0);  // none: n = 0
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)rows, 0, end, 0x00020000);
       uint32_t off = (uint32_t)((rev ? n - 1 - row : row) * st) +
                      (col < width ? col * (uint32_t)sizeof(E) : 0x40000000u);
@@ -451,6 +451,38 @@ __device__ __forceinline__ int oswz(int t) {
 template <int N>
 struct Count {
   static constexpr int value = N;
+};
+
+// Keeps what follows from moving before what precedes: a product, a few vector
+// instructions that run beside it, the next product.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// Two values of an operand fragment on their way into N bf16 parts, a few
+// instructions at a time: step 0 .. N - 1 (or N, after a step that weighs them).
+struct Pair {
+  float a, b;
+  __device__ __forceinline__ uint32_t part(bool last) {
+    const uint32_t u = bf16x2_rne(a, b);
+    if (!last) {
+      a -= bf16_lo(u);
+      b -= bf16_hi(u);
+    }
+    return u;
+  }
+};
+template <int N>
+struct Parts {  // of one fragment: its pairs' N parts
+  Pair x[4];
+  u4 u[N];
+  // STEPS steps for each pair; done(i): step i of all
+  static constexpr int STEPS = 4 * N;
+  __device__ __forceinline__ void step(int i) {
+    const int j = i / N, q = i % N;
+    u[q][j] = x[j].part(q == N - 1);
+  }
+  __device__ __forceinline__ Frag<Bf16> frag(int q) const {
+    return {__builtin_bit_cast(s8, u[q])};
+  }
 };
 
 // The lane's place in a fragment, worked out anew: what is derived from it (each
@@ -760,85 +792,195 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
             *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{0.f, 0.f, 0.f, 0.f};
           }
         }
-        if (wave == 0) {
-          put_decays(c + 1);
-          load_decays(c + 2);
-        }
+      }
+      if (wave == 0) {
+        put_decays(c + 1);
+        load_decays(c + 2);
+      }
+      // the next chunk's loads fly during the products (after X S where its operands' parts
+      // leave no room for them)
+      constexpr bool LATE = MODE == GRAD && NT == 2;
+      if (!LATE) load_chunk(c + 1);
 
-        // X S
-        const auto [g, r] = lane_place(tid);
-        const E* const xrow = sh.x + r * KR + 8 * g;
+      // From here to the barrier the products and the vector instructions that make
+      // their operands alternate, so that both units work: while the products of
+      // one block run, the next one's parts are worked out.
+      const auto [g, r] = lane_place(tid);
+      const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
+      const E* const ycol[2] = {y_base<KP>(sh.y, g, r, 0), y_base<KP>(sh.y, g, r, 1)};
+      const E* const xrow = sh.x + r * KR + 8 * g;
+      const float ec = dec.ec;
+      if (MODE == CARRY) seg_decay *= ec;
+      if (XS) {
 #pragma unroll
         for (int i = 0; i < TT; ++i)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) O[i][nt] = f4{0.f, 0.f, 0.f, 0.f};
+      }
+      if constexpr (T::SPLIT) {
+        constexpr int NP = KP / 32, NW = T::NW;
+        // the weighted Z of block sb: NT fragments of four pairs, each weighed (a step) and
+        // split (NW steps)
+        Parts<NW> wz[NT];
+        Frag<T> zf[NT];
+        f4 ew[2];
+        constexpr int WSTEPS = NT * 4 * (NW + 1);
+        auto begin_z = [&](int sb) __attribute__((always_inline)) {
+          ew[0] = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g);
+          ew[1] = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g + 4);
 #pragma unroll
-        for (int p = 0; p < KP / 32; ++p) {
-          Frag<T> sf[NT][NS];
+          for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 16 * nt);
+        };
+        auto z_steps = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[i] = S[2 * p][nt][i];
-              x[4 + i] = S[2 * p + 1][nt][i];
+          for (int i = from; i < to; ++i) {
+            const int nt = i / (4 * (NW + 1)), j = i / (NW + 1) % 4, q = i % (NW + 1);
+            if (q == 0) {
+              const u4 u = __builtin_bit_cast(u4, zf[nt].v);
+              wz[nt].x[j] = {bf16_lo(u[j]) * ew[j / 2][2 * (j & 1)],
+                             bf16_hi(u[j]) * ew[j / 2][2 * (j & 1) + 1]};
+            } else {
+              wz[nt].u[q - 1][j] = wz[nt].x[j].part(q == NW);
             }
-            parts_of<NS>(x, sf[nt]);
           }
+        };
+        begin_z(0);
+        if constexpr (XS) {  // X S
+          Parts<NS> sp[2][NT];  // S's rows of this block of columns and the next
+          constexpr int SSTEPS = NT * 4 * NS;
+          auto s_steps = [&](int p, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-          for (int i = 0; i < TT; ++i) {
-            const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
+            for (int i = from; i < to; ++i) {
+              const int nt = i / (4 * NS), j = i / NS % 4, q = i % NS;
+              Parts<NS>& t = sp[p & 1][nt];
+              if (q == 0) t.x[j] = {S[2 * p + j / 2][nt][2 * (j & 1)], S[2 * p + j / 2][nt][2 * (j & 1) + 1]};
+              t.u[q][j] = t.x[j].part(q == NS - 1);
+            }
+          };
+          Frag<T> xf[2][TT];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+          for (int i = 0; i < TT; ++i) xf[0][i] = row_frag(xrow + i * 16 * KR);
+          s_steps(0, 0, SSTEPS);
+          in_order();
+          constexpr int M = NS * TT * NT;  // products of a block of columns
 #pragma unroll
-              for (int q = NS - 1; q >= 0; --q) O[i][nt] = mma(sf[nt][q], xf, O[i][nt]);
+          for (int p = 0; p < NP; ++p) {
+            if (p + 1 < NP)
+#pragma unroll
+              for (int i = 0; i < TT; ++i) xf[(p + 1) & 1][i] = row_frag(xrow + i * 16 * KR + 32 * (p + 1));
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+              const int q = NS - 1 - m / (TT * NT), i = m / NT % TT, nt = m % NT;
+              O[i][nt] = mma(sp[p & 1][nt].frag(q), xf[p & 1][i], O[i][nt]);
+              if (p + 1 < NP) s_steps(p + 1, m * SSTEPS / M, (m + 1) * SSTEPS / M);
+              z_steps((p * M + m) * WSTEPS / (NP * M), (p * M + m + 1) * WSTEPS / (NP * M));
+              in_order();
+            }
           }
+        } else {
+          z_steps(0, WSTEPS);
         }
-#pragma unroll
-        for (int i = 0; i < TT; ++i) {
-          const float er = dec.er[i * 16 + r];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
-        }
-      }
 
-      load_chunk(c + 1);  // in flight while the state moves on; earlier, its registers would spill
-
-      // S <- e^{G_C} S + Y^T (weighted Z)
-      if (MODE == CARRY && wave == 0) {
-        put_decays(c + 1);
-        load_decays(c + 2);
-      }
-      const float ec = dec.ec;
-      if (MODE == CARRY) seg_decay *= ec;
-      const auto [g, r] = lane_place(tid);
-      const E* const ycol[2] = {y_base<KP>(sh.y, g, r, 0), y_base<KP>(sh.y, g, r, 1)};
-      const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
-#pragma unroll
-      for (int sb = 0; sb < SB; ++sb) {
-        Frag<T> wf[NT][T::NW];
-        float ew[8];
-        *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g);
-        *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(dec.ew + 32 * sb + 8 * g + 4);
+        if (LATE) load_chunk(c + 1);
+        // S <- e^{G_C} S + Y^T (weighted Z)
+        constexpr int M = KT * NT * NW;  // products of a block of steps
+        auto scale = [&](int k, int nt) __attribute__((always_inline)) { S[k][nt] *= ec; };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float x[8];
-          widen(col_frag<VT>(zcol + 32 * sb * VR + 16 * nt), x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] *= ew[j];
-          parts_of<T::NW>(x, wf[nt]);
+          scale(0, nt);
+          scale(1, nt);
         }
+        Frag<T> yf[2][2];
+        auto load_y = [&](int at) __attribute__((always_inline)) {  // at: sb * KT / 2 + k / 2
+          const int sb = at / (KT / 2), k2 = at % (KT / 2);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          const Frag<T> yf = col_frag<KP>(ycol[kt & 1] + 32 * sb * KR + 32 * (kt >> 1));
+          for (int k = 0; k < 2; ++k) yf[at & 1][k] = col_frag<KP>(ycol[k] + 32 * sb * KR + 32 * k2);
+        };
+        load_y(0);
+#pragma unroll
+        for (int sb = 0; sb < SB; ++sb) {
+          Frag<T> wf[NT][NW];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int q = T::NW - 1; q >= 0; --q) S[kt][nt] = mma(yf, wf[nt][q], S[kt][nt]);
+            for (int q = 0; q < NW; ++q) wf[nt][q] = wz[nt].frag(q);
+          if (sb + 1 < SB) begin_z(sb + 1);
+          float er[TT];
+          if (XS && sb + 1 == SB)
+#pragma unroll
+            for (int i = 0; i < TT; ++i) er[i] = dec.er[i * 16 + r];
+          in_order();
+#pragma unroll
+          for (int k2 = 0; k2 < KT / 2; ++k2) {
+            const int at = sb * (KT / 2) + k2;
+            if (at + 1 < SB * (KT / 2)) load_y(at + 1);
+            constexpr int MK = 2 * NT * NW;
+#pragma unroll
+            for (int m = 0; m < MK; ++m) {
+              const int q = NW - 1 - m / (2 * NT), k = m / NT % 2, nt = m % NT;
+              S[2 * k2 + k][nt] = mma(yf[at & 1][k], wf[nt][q], S[2 * k2 + k][nt]);
+              const int done = k2 * MK + m;
+              if (sb + 1 < SB) z_steps(done * WSTEPS / M, (done + 1) * WSTEPS / M);
+              // the next rows of S, before their first product
+              if (sb == 0 && k2 + 1 < KT / 2)
+#pragma unroll
+                for (int i = m * 2 * NT / MK; i < (m + 1) * 2 * NT / MK; ++i)
+                  scale(2 * (k2 + 1) + i / NT, i % NT);
+              if (XS && sb + 1 == SB)
+#pragma unroll
+                for (int i = done * TT * NT / M; i < (done + 1) * TT * NT / M; ++i)
+                  O[i / NT][i % NT] *= er[i / NT];
+              in_order();
+            }
+          }
+        }
+      } else {
+        if (XS) {  // X S
+#pragma unroll
+          for (int p = 0; p < KP / 32; ++p) {
+            Frag<T> sf[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                sf[nt].v[i] = S[2 * p][nt][i];
+                sf[nt].v[4 + i] = S[2 * p + 1][nt][i];
+              }
+#pragma unroll
+            for (int i = 0; i < TT; ++i) {
+              const Frag<T> xf = row_frag(xrow + i * 16 * KR + 32 * p);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(sf[nt], xf, O[i][nt]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < TT; ++i) {
+            const float er = dec.er[i * 16 + r];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) O[i][nt] *= er;
+          }
+        }
+        if (LATE) load_chunk(c + 1);
+        // S <- e^{G_C} S + Y^T (weighted Z)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) S[kt][nt] *= ec;
+        Frag<T> wf[NT];
+        float ew[8];
+        *reinterpret_cast<f4*>(ew) = *reinterpret_cast<const f4*>(dec.ew + 8 * g);
+        *reinterpret_cast<f4*>(ew + 4) = *reinterpret_cast<const f4*>(dec.ew + 8 * g + 4);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          wf[nt] = col_frag<VT>(zcol + 16 * nt);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) wf[nt].v[j] *= ew[j];
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          const Frag<T> yf = col_frag<KP>(ycol[kt & 1] + 32 * (kt >> 1));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) S[kt][nt] = mma(yf, wf[nt], S[kt][nt]);
         }
       }
 
@@ -852,9 +994,9 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 16 * nt);
 #pragma unroll
-          for (int i = 2 * sb; i < TT; ++i)  // steps t before the block have no weight in it
+          for (int q = NS - 1; q >= 0; --q)
 #pragma unroll
-            for (int q = NS - 1; q >= 0; --q) {
+            for (int i = 2 * sb; i < TT; ++i) {  // steps t before the block have no weight in it
               const Frag<T> pf = p_frag(sh.p + q * P_SIZE<T>, i * 16 + r, sb, g);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) O[i][nt] = mma(zf[nt], pf, O[i][nt]);
