@@ -120,8 +120,17 @@ __global__ __launch_bounds__(256) void dg_kernel(DgArgs a) {
     d = a.dh_last + (pl.n * a.H + h) * a.KV;
   }
   double dot = 0.0;
-  if (s)
-    for (int64_t e = tid; e < a.KV; e += 256) dot += (double)s[e] * d[e];
+  if (s) {
+    int64_t e = 4 * tid;
+    if (a.KV % 4 == 0 && ((uintptr_t)s | (uintptr_t)d) % 16 == 0)
+#pragma unroll 4
+      for (; e < a.KV; e += 1024) {
+        const f4 x = *reinterpret_cast<const f4*>(s + e), y = *reinterpret_cast<const f4*>(d + e);
+        dot += ((double)x[0] * y[0] + (double)x[1] * y[1]) + ((double)x[2] * y[2] + (double)x[3] * y[3]);
+      }
+    else
+      for (e = tid; e < a.KV; e += 256) dot += (double)s[e] * d[e];
+  }
   dot = wave_sum(dot);
   if (lane == 0) part[wave] = dot;
 
@@ -210,22 +219,48 @@ struct Plan {
   int64_t aper = 1, aslots = 0;    // intervals of ANCHOR steps
 };
 
-// Segments: whole sequences where their heads and tiles fill the GPU, else
-// rows cut so that about two workgroups reach every compute unit.  A cut costs
-// a walk of the keys and values alone before the walk itself.
+// Workgroups of a walk that share a compute unit (registers and LDS), and what a
+// chunk then takes, in units of one alone: two side by side finish in 1.5 of it.
+int resident(int64_t contracted, int nt) {
+  return contracted > 128 ? 1 : contracted <= 64 && nt == 1 ? 3 : 2;
+}
+double pace(int64_t wgs, int cus, int res) {
+  const int64_t load = (wgs + cus - 1) / cus;  // of the fullest compute unit
+  const int64_t rounds = load / res, rest = load % res;
+  return rounds * (1.0 + 0.5 * (res - 1)) + (rest ? 1.0 + 0.5 * (rest - 1) : 0.0);
+}
+
+// Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
+// alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, gradient
+// with its row sums 9.5; a workgroup's start and end are worth a chunk, the
+// composition's launch 12 us.  At B=8 L=2048 H=12: one walk of whole sequences 175
+// us against 117 in five parts; forward and backward 680 against 560 in four.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
   p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
   p.nt_k = a.K <= 64 || a.V > 128 ? 1 : 2;
   p.tiles_v = (a.V + 64 * p.nt_v - 1) / (64 * p.nt_v);
   p.tiles_k = (a.K + 64 * p.nt_k - 1) / (64 * p.nt_k);
-  const int64_t per_seq_wgs = a.H * (bwd ? 2 * p.tiles_k : p.tiles_v);
   const int64_t longest = a.L, chunks = (longest + CHUNK - 1) / CHUNK;
-  const int64_t want = 2 * (int64_t)cus, whole = a.B * per_seq_wgs;
-  // the most parts that still run side by side: one more would wait for a whole round
-  int64_t parts = whole > 0 ? want / whole : 1;
-  if (parts > chunks / 4) parts = chunks / 4;
-  if (parts < 3) parts = 1;  // a cut into two does not pay: the first walk costs about half the second
+  const int64_t rows = a.B * a.H;
+  int64_t parts = 1;
+  double best = 0.0;
+  for (int64_t n = 1; n <= 256 && (n == 1 || 2 * n <= chunks); ++n) {
+    const double len = (double)((chunks + n - 1) / n + 1);
+    double us;
+    if (bwd) {
+      const double two = pace(rows * n * 2 * p.tiles_k, cus, resident(a.V, p.nt_k));
+      us = len * (two * (9.5 + (n > 1 ? 3.0 : 0.0)) +
+                  5.5 * pace(rows * n * p.tiles_v, cus, resident(a.K, p.nt_v)));
+    } else {
+      us = len * pace(rows * n * p.tiles_v, cus, resident(a.K, p.nt_v)) * (n > 1 ? 8.5 : 5.5);
+    }
+    if (n > 1) us += 12.0;
+    if (n == 1 || us < best) {
+      best = us;
+      parts = n;
+    }
+  }
   int64_t lseg = (chunks + parts - 1) / parts * CHUNK;
   if (lseg < CHUNK) lseg = CHUNK;
   p.lseg = lseg;
