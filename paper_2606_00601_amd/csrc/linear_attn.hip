@@ -232,9 +232,9 @@ double pace(int64_t wgs, int cus, int res) {
 
 // Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
 // alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, gradient
-// with its row sums 9.5; a workgroup's start and end are worth a chunk, the
-// composition's launch 12 us.  At B=8 L=2048 H=12: one walk of whole sequences 175
-// us against 117 in five parts; forward and backward 680 against 560 in four.
+// with its row sums 9.5; a workgroup's start and end are worth two chunks, the
+// composition's launch 12 us.  At B=8 L=2048 H=12 forward and backward took 680 us
+// with the backward's sequences whole and 552 in the parts chosen.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
   p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
@@ -246,7 +246,7 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   int64_t parts = 1;
   double best = 0.0;
   for (int64_t n = 1; n <= 256 && (n == 1 || 2 * n <= chunks); ++n) {
-    const double len = (double)((chunks + n - 1) / n + 1);
+    const double len = (double)((chunks + n - 1) / n) + 2.0;
     double us;
     if (bwd) {
       const double two = pace(rows * n * 2 * p.tiles_k, cus, resident(a.V, p.nt_k));

@@ -79,7 +79,7 @@ __device__ __forceinline__ float as_stored(float x, const uint16_t*) {
 }
 __device__ __forceinline__ float as_stored(float x, const float*) { return x; }
 
-constexpr int threads_of(int lpr) { return lpr > 256 ? lpr : 256; }
+constexpr int threads_of(int lpr) { return lpr > 64 ? lpr : 256; }  // whole rows
 
 // N sums over the LPR lanes of a row; `par` alternates from call to call, so
 // that one barrier each suffices where a row spans waves.
@@ -150,16 +150,32 @@ inline bool vec_rows(const void* p, int64_t st, int64_t width, bool bf16) {
 }
 
 // Row blocks of a backward: the workgroups' partial sums are this many rows.
-// Two workgroups for each compute unit hold enough rows in flight (their
-// accumulators leave room for no more); fewer rows, fewer blocks.
+// Four workgroups for each compute unit run side by side.
 inline int64_t bwd_blocks(int64_t M, int64_t D, int64_t width, int cus) {
   const int64_t groups = D / width;
-  int64_t n = (2 * (int64_t)cus + groups - 1) / groups;
+  int64_t n = (4 * (int64_t)cus + groups - 1) / groups;
   if (n > M) n = M;
   return n < 1 ? 1 : n;
 }
 
-// CALL(LPR, NV) for the smallest that holds a row of `width`.
+// CALL(LPR, NV) for the smallest that holds a row of `width`; a wave for each row
+// of up to 1536 columns needs no barrier.  A backward's registers hold more of each column, so a row takes more lanes: at
+// 16384 rows of 1536 (residual norm, fp32 stream) 64 lanes of three vectors ran two
+// waves per SIMD and 121 us, 192 lanes of one four waves and 102.  Rows over 8192
+// spill some of theirs.
+#define SW_NORM_PICK_BWD(width, CALL)           \
+  do {                                          \
+    if ((width) <= 64) { CALL(8, 1); }          \
+    else if ((width) <= 128) { CALL(16, 1); }   \
+    else if ((width) <= 256) { CALL(32, 1); }   \
+    else if ((width) <= 512) { CALL(64, 1); }   \
+    else if ((width) <= 1024) { CALL(128, 1); } \
+    else if ((width) <= 1536) { CALL(192, 1); } \
+    else if ((width) <= 2048) { CALL(256, 1); } \
+    else if ((width) <= 4096) { CALL(512, 1); } \
+    else if ((width) <= 8192) { CALL(1024, 1); } \
+    else { CALL(1024, 2); }                     \
+  } while (0)
 #define SW_NORM_PICK(width, CALL)              \
   do {                                         \
     if ((width) <= 64) { CALL(8, 1); }         \
