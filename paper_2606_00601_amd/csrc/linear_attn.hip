@@ -74,53 +74,73 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a) {
   }
 }
 
-// dg of up to ANCHOR steps of one head: with r = q . dq and c = k . dk,
-//   dg_t = sum_{t <= i < e} (r_i - c_i) + dg_e,
-//   dg_e = e^{g_e} <dS_e, S_{e-1}> from the states kept at the interval's end e
-// (<dh_last, h_last> at the sequence's).  The difference telescopes: sums that
-// cancel never run over more than ANCHOR steps, in fp64.
-struct DgArgs {
-  const float *rdots, *cdots;  // [tile][H][B * L]
-  int tiles;
-  const float* g;
-  int64_t g_sb, g_sl, g_sh;
-  const int32_t* cu;
-  const float *S, *dS, *dh_last;
-  float* dg;        // (B, L, H), or NULL
-  double* by_slot;  // (slots, H): sums over the interval, or NULL
-  int64_t B, L, nseq, H, KV, per_seq;
-};
-
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
 
-__global__ __launch_bounds__(256) void dg_kernel(DgArgs a) {
-  __shared__ double part[4], whole[4], sums[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  const Place pl = place_of(a.cu, slot, ANCHOR, a.per_seq, a.nseq, a.L);
-  if (!pl.valid || pl.len == 0) {
-    if (a.by_slot && tid == 0) a.by_slot[slot * a.H + h] = 0.0;
-    return;
-  }
-  const int64_t b = a.cu ? 0 : pl.n;
-  const int64_t t0 = pl.part * ANCHOR, t1 = t0 + ANCHOR < pl.len ? t0 + ANCHOR : pl.len;
-  const float* gp = a.g + b * a.g_sb + pl.first * a.g_sl + h * a.g_sh;
+// Steps of an interval of dg.  A head's gradient is the sum over its steps, which
+// may cancel where theirs do not, so its intervals are shorter: in 256 steps its error
+// came to 2.7e-6 of it where fp32 sums have 6e-7 (2 x 1501 steps of 4 heads,
+// K = V = 64), in 64 to 5.1e-7, for 15 us more of 275 (B=4 L=1501 H=32 K=V=64).
+constexpr int STEP_ANCHOR = 256, HEAD_ANCHOR = 64;
 
-  // the state product at the interval's end
+// dg, in intervals of `anchor` steps s .. e-1 of one head: with r = q . dq and
+// c = k . dk,
+//   dg_t = dg_e + sum_{t <= i < e} (r_i - c_i),   dg_t = e^{g_t} <dS_t, S_{t-1}>,
+// the products of the states taken at the intervals' ends only (at a sequence's
+// <dh_last, h_last> and <dh0, h0>).  The difference telescopes, but r and c are
+// rounded apart, so the sum walks away from dg_s by the time it gets there: what it
+// misses there is spread evenly over the interval.  That halves the error of the
+// interval's sum (of independent ones, 1/12 of the variance's A^3 and not 1/3).  fp64
+// throughout.
+struct DgArgs {
+  const float *rdots, *cdots;  // [tile][H][B * L]
+  int tiles;
+  const float* g;
+  int64_t g_sb, g_sl, g_sh;
+  const int32_t* cu;
+  const float *S, *dS, *h0, *dh0, *dh_last;
+  double *ends, *starts;  // (slots, H), (nseq, H): dg_e, dg_s; NULL: all zero
+  float* dg;              // (B, L, H), or NULL
+  double* by_slot;        // (slots, H): sums over the interval, or NULL
+  int64_t B, L, nseq, H, KV, per_seq, slots;
+  int anchor;
+};
+
+// The states' products: workgroups (slot, h), then (sequence, h).
+__global__ __launch_bounds__(256) void ends_kernel(DgArgs a) {
+  __shared__ double part[4];
+  const int tid = threadIdx.x;
+  const int64_t h = blockIdx.x % a.H;
+  int64_t slot = blockIdx.x / a.H;
   const float *s = nullptr, *d = nullptr;
-  if (t1 < pl.len) {
+  double* out;
+  double mul = 1.0;
+  if (slot < a.slots) {
+    const Place pl = place_of(a.cu, slot, a.anchor, a.per_seq, a.nseq, a.L);
+    if (!pl.valid) return;
+    const int64_t t1 = (pl.part + 1) * a.anchor;
     s = a.S + (slot * a.H + h) * a.KV;
-    d = a.dS + (slot * a.H + h) * a.KV;
-  } else if (a.dh_last) {
-    s = a.S + (slot * a.H + h) * a.KV;
-    d = a.dh_last + (pl.n * a.H + h) * a.KV;
+    if (t1 < pl.len) {
+      d = a.dS + (slot * a.H + h) * a.KV;
+      const int64_t b = a.cu ? 0 : pl.n;
+      mul = exp((double)clamp_g(a.g[b * a.g_sb + (pl.first + t1) * a.g_sl + h * a.g_sh]));
+    } else if (a.dh_last && pl.len > 0) {
+      d = a.dh_last + (pl.n * a.H + h) * a.KV;
+    }
+    out = a.ends + slot * a.H + h;
+  } else {
+    slot -= a.slots;
+    if (a.h0) {
+      s = a.h0 + (slot * a.H + h) * a.KV;
+      d = a.dh0 + (slot * a.H + h) * a.KV;
+    }
+    out = a.starts + slot * a.H + h;
   }
   double dot = 0.0;
-  if (s) {
+  if (d) {
     int64_t e = 4 * tid;
     if (a.KV % 4 == 0 && ((uintptr_t)s | (uintptr_t)d) % 16 == 0)
 #pragma unroll 4
@@ -132,51 +152,78 @@ __global__ __launch_bounds__(256) void dg_kernel(DgArgs a) {
       for (e = tid; e < a.KV; e += 256) dot += (double)s[e] * d[e];
   }
   dot = wave_sum(dot);
-  if (lane == 0) part[wave] = dot;
+  if ((tid & 63) == 0) part[tid >> 6] = dot;
+  __syncthreads();
+  if (tid == 0) *out = mul * (part[0] + part[1] + part[2] + part[3]);
+}
 
-  // a thread's steps, summed from the end
-  constexpr int U = ANCHOR / 256;
-  double v[U];
-  const int64_t at = b * a.L + pl.first;
-#pragma unroll
-  for (int u = U - 1; u >= 0; --u) {
-    const int64_t t = t0 + U * tid + u;
-    double x = 0.0;
-    if (t < t1)
-      for (int q = 0; q < a.tiles; ++q) {
-        const int64_t i = ((int64_t)q * a.H + h) * (a.B * a.L) + at + t;
-        x += (double)a.rdots[i] - a.cdots[i];
-      }
-    v[u] = u + 1 < U ? v[u + 1] + x : x;
-  }
-  double suf = v[0];  // this thread's and later lanes'
+// v summed over this lane and the later (LATER) or the earlier ones; whole: over the wave.
+template <bool LATER>
+__device__ __forceinline__ double wave_scan(double v, int lane) {
 #pragma unroll
   for (int k = 1; k < 64; k <<= 1) {
-    const double o = __shfl_down(suf, k);
-    if (lane + k < 64) suf += o;
+    const double o = LATER ? __shfl_down(v, k) : __shfl_up(v, k);
+    if (LATER ? lane + k < 64 : lane >= k) v += o;
   }
+  return v;
+}
+
+// A workgroup of `anchor` threads for each interval and head.
+__global__ __launch_bounds__(STEP_ANCHOR) void dg_kernel(DgArgs a) {
+  __shared__ double whole[STEP_ANCHOR / 64], sums[STEP_ANCHOR / 64];
+  const int waves = a.anchor / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  const Place pl = place_of(a.cu, slot, a.anchor, a.per_seq, a.nseq, a.L);
+  if (!pl.valid || pl.len == 0) {
+    if (a.by_slot && tid == 0) a.by_slot[slot * a.H + h] = 0.0;
+    return;
+  }
+  const int64_t b = a.cu ? 0 : pl.n;
+  const int64_t t0 = pl.part * a.anchor, n = pl.len - t0 < a.anchor ? pl.len - t0 : a.anchor;
+  const int64_t at = b * a.L + pl.first + t0 + tid;
+  double x = 0.0, end = 0.0, start = 0.0, g = 0.0;
+  if (tid < n) {
+    for (int q = 0; q < a.tiles; ++q) {
+      const int64_t i = ((int64_t)q * a.H + h) * (a.B * a.L) + at;
+      x += (double)a.rdots[i] - a.cdots[i];
+    }
+    g = a.g[b * a.g_sb + (pl.first + t0 + tid) * a.g_sl + h * a.g_sh];
+  }
+  if (a.ends) {
+    end = a.ends[slot * a.H + h];
+    start = pl.part ? a.ends[(slot - 1) * a.H + h] : a.starts[pl.n * a.H + h];
+  }
+  const double suf = wave_scan<true>(x, lane);
   if (lane == 0) whole[wave] = suf;
   __syncthreads();
-  double base = part[0] + part[1] + part[2] + part[3];
-  if (t1 < pl.len) base *= exp((double)clamp_g(gp[t1 * a.g_sl]));
-  base += suf - v[0];
-  for (int q = wave + 1; q < 4; ++q) base += whole[q];
-  double sum = 0.0;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t t = t0 + U * tid + u;
-    if (t < t1) {
-      // where e^g is held at zero its derivative is zero too
-      const double x = gp[t * a.g_sl] < G_MIN ? 0.0 : v[u] + base;
-      sum += x;
-      if (a.dg) a.dg[(at + t) * a.H + h] = (float)x;
-    }
+  double all = 0.0, v = suf + end;
+  for (int q = 0; q < waves; ++q) {
+    all += whole[q];
+    if (q > wave) v += whole[q];
   }
+  const double miss = start - (end + all);
+  if (miss - miss == 0.0) {
+    v += miss * ((double)(n - tid) / (double)n);
+  } else {
+    // A value that is not finite: from the end down to it, and from the start up to
+    // it, so that it reaches the steps it reaches in the recurrence.
+    double pre = start - (wave_scan<false>(x, lane) - x);
+    for (int q = 0; q < wave; ++q) pre -= whole[q];
+    if (!(v - v == 0.0)) v = pre;
+  }
+  // where e^g is held at zero its derivative is zero too
+  if (tid >= n || g < G_MIN) v = 0.0;
+  if (a.dg && tid < n) a.dg[at * a.H + h] = (float)v;
   if (a.by_slot) {
-    sum = wave_sum(sum);
-    if (lane == 0) sums[wave] = sum;
+    v = wave_sum(v);
+    if (lane == 0) sums[wave] = v;
     __syncthreads();
-    if (tid == 0) a.by_slot[slot * a.H + h] = sums[0] + sums[1] + sums[2] + sums[3];
+    if (tid == 0) {
+      double t = 0.0;
+      for (int q = 0; q < waves; ++q) t += sums[q];
+      a.by_slot[slot * a.H + h] = t;
+    }
   }
 }
 
@@ -191,21 +238,33 @@ __global__ __launch_bounds__(64) void dg_head_kernel(const double* by_slot, floa
 }
 
 // Gradients of shared heads: rows of r * W fp32 values, summed over the r heads
-// of a group in order and rounded once.
-template <bool BF16>
-__global__ __launch_bounds__(256) void share_kernel(const float* __restrict__ part,
-                                                    void* __restrict__ out, int64_t groups, int r,
-                                                    int W) {
-  const int64_t n = groups * W;
+// of a group in order and rounded once; dq and dk in one launch.  N columns of a
+// thread: 4 where W allows (98 MB of rows: 19 us, a copy's rate; a column each 39).
+struct ShareArgs {
+  const float* part[2];
+  void* out[2];
+  int64_t groups;
+  int r, W;
+};
+template <bool BF16, int N>
+__global__ __launch_bounds__(256) void share_kernel(ShareArgs a) {
+  typedef float fn __attribute__((ext_vector_type(N)));
+  const float* __restrict__ part = a.part[blockIdx.y];
+  const uint32_t per = (uint32_t)(a.W / N);
+  const int64_t n = a.groups * per;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-    const int64_t gi = i / W;
-    const float* p = part + gi * r * W + (i - gi * W);
-    float s = 0.0f;
-    for (int j = 0; j < r; ++j) s += p[(int64_t)j * W];
-    if (BF16)
-      ((uint16_t*)out)[i] = (uint16_t)bf16_rne(s);
-    else
-      ((float*)out)[i] = s;
+    const int64_t gi = n <= 0xffffffffll ? (int64_t)((uint32_t)i / per) : i / per;
+    const int64_t c = (i - gi * per) * N;
+    const float* p = part + gi * a.r * a.W + c;
+    fn s = 0.0f;
+    for (int j = 0; j < a.r; ++j) s += *reinterpret_cast<const fn*>(p + (int64_t)j * a.W);
+    if constexpr (BF16) {
+      uint16_t* o = (uint16_t*)a.out[blockIdx.y] + gi * a.W + c;
+#pragma unroll
+      for (int j = 0; j < N; ++j) o[j] = (uint16_t)bf16_rne(s[j]);
+    } else {
+      *reinterpret_cast<fn*>((float*)a.out[blockIdx.y] + gi * a.W + c) = s;
+    }
   }
 }
 
@@ -216,7 +275,8 @@ struct Plan {
   int64_t tiles_v = 1, tiles_k = 1;
   int64_t lseg = CHUNK, per_seq = 1, slots = 0;  // segments
   bool cut = false;                // some sequence may have several
-  int64_t aper = 1, aslots = 0;    // intervals of ANCHOR steps
+  int anchor = STEP_ANCHOR;        // dg's intervals
+  int64_t aper = 1, aslots = 0;
 };
 
 // Workgroups of a walk that share a compute unit (registers and LDS), and what a
@@ -267,18 +327,20 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   p.cut = lseg < longest;
   p.per_seq = longest > 0 ? (longest + lseg - 1) / lseg : 1;
   p.slots = a.cu ? a.L / lseg + a.nseq : a.B * p.per_seq;
-  p.aper = longest > 0 ? (longest + ANCHOR - 1) / ANCHOR : 1;
-  p.aslots = a.cu ? a.L / ANCHOR + a.nseq : a.B * p.aper;
+  p.anchor = a.g_head ? HEAD_ANCHOR : STEP_ANCHOR;
+  p.aper = longest > 0 ? (longest + p.anchor - 1) / p.anchor : 1;
+  p.aslots = a.cu ? a.L / p.anchor + a.nseq : a.B * p.aper;
   return p;
 }
 
 // The workspace's parts, in bytes from its start; every one 256-byte aligned.
 struct Layout {
   size_t carry[2] = {0, 0}, decay[2] = {0, 0}, S = 0, dS = 0, rdots = 0, cdots = 0, dq = 0, dk = 0,
-         by_slot = 0, bytes = 0;
+         dh0 = 0, ends = 0, starts = 0, by_slot = 0, bytes = 0;
 };
 
-Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool dh_last) {
+// What a call of these sizes may need with every optional operand (`all`), or does.
+Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool all) {
   Layout l;
   auto take = [&](size_t n) {
     const size_t at = l.bytes;
@@ -292,8 +354,11 @@ Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool dh_last) 
       l.decay[i] = take((size_t)(p.slots * a.H) * 4);
     }
   if (bwd) {
-    if (a.L > ANCHOR || dh_last) l.S = take((size_t)p.aslots * HKV * 4);
-    if (a.L > ANCHOR) l.dS = take((size_t)p.aslots * HKV * 4);
+    if (a.L > p.anchor || a.dh_last || all) l.S = take((size_t)p.aslots * HKV * 4);
+    if (a.L > p.anchor) l.dS = take((size_t)p.aslots * HKV * 4);
+    if ((a.h0 && !a.dh0) || all) l.dh0 = take((size_t)a.nseq * HKV * 4);
+    l.ends = take((size_t)(p.aslots * a.H) * 8);
+    l.starts = take((size_t)(a.nseq * a.H) * 8);
     l.rdots = take((size_t)(p.tiles_k * a.H) * T * 4);
     l.cdots = take((size_t)(p.tiles_k * a.H) * T * 4);
     if (a.H != a.Hk) {
@@ -328,6 +393,7 @@ WalkArgs walk_args(const LinAttnArgs& a, const Plan& p) {
   w.lseg = p.lseg;
   w.per_seq = p.per_seq;
   w.slots = p.slots;
+  w.anchor = p.anchor;
   w.njobs = 1;
   return w;
 }
@@ -488,7 +554,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   if ((st = device_cus(&cus)) != SW_OK) return st;
   const Plan p = make_plan(a, true, cus);
   if ((st = check_grid(a, p, true)) != SW_OK) return st;
-  const Layout l = make_layout(a, p, true, a.dh_last != nullptr);
+  const Layout l = make_layout(a, p, true, false);
   const hipStream_t s = current_stream();
   Workspace ws(s);
   if ((st = ws.get(a, l.bytes, "sw_linear_attn_bwd")) != SW_OK) return st;
@@ -511,7 +577,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   jv.wscale = a.scale;
   jv.rscale = jv.neg ? -1.0f : 1.0f;
   jv.init = a.dh_last;
-  jv.last = a.dh0;
+  jv.last = a.dh0 ? a.dh0 : a.h0 ? at(l.dh0) : nullptr;
   set_out(jv, a, a.dv, a.H, a.V, !a.bf16);
   set_out(jq, a, shared ? at(l.dq) : a.dq, a.H, a.K, shared || !a.bf16);
   set_out(jk, a, shared ? at(l.dk) : a.dk, a.H, a.K, shared || !a.bf16);
@@ -538,9 +604,9 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   jk.adiv = r;
   jk.avec = rows_vec(a.k, a.K, a.bf16);
   jk.dots = at(l.cdots);
-  if (a.L > ANCHOR || a.dh_last) jq.anchors = at(l.S);
+  if (a.L > p.anchor || a.dh_last) jq.anchors = at(l.S);
   jq.last_anchor = a.dh_last != nullptr;
-  if (a.L > ANCHOR) jk.anchors = at(l.dS);
+  if (a.L > p.anchor) jk.anchors = at(l.dS);
   w.job[0] = jq;
   w.job[1] = jk;
   w.njobs = 2;
@@ -560,7 +626,12 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   d.cu = a.cu;
   d.S = at(l.S);
   d.dS = at(l.dS);
+  d.h0 = a.h0;
+  d.dh0 = jv.last;
   d.dh_last = a.dh_last;
+  const bool ends = a.L > p.anchor || a.h0 || a.dh_last;
+  d.ends = ends ? (double*)at(l.ends) : nullptr;
+  d.starts = (double*)at(l.starts);
   d.dg = a.g_head ? nullptr : a.dg;
   d.by_slot = a.g_head ? (double*)at(l.by_slot) : nullptr;
   d.B = a.B;
@@ -569,8 +640,14 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   d.H = a.H;
   d.KV = a.K * a.V;
   d.per_seq = p.aper;
+  d.slots = p.aslots;
+  d.anchor = p.anchor;
+  if (ends) {
+    hipLaunchKernelGGL(ends_kernel, dim3((unsigned)((p.aslots + a.nseq) * a.H)), dim3(256), 0, s, d);
+    if ((st = check_launch("ends_kernel")) != SW_OK) return st;
+  }
   if (p.aslots > 0) {
-    hipLaunchKernelGGL(dg_kernel, dim3((unsigned)(p.aslots * a.H)), dim3(256), 0, s, d);
+    hipLaunchKernelGGL(dg_kernel, dim3((unsigned)(p.aslots * a.H)), dim3((unsigned)p.anchor), 0, s, d);
     if ((st = check_launch("dg_kernel")) != SW_OK) return st;
   }
   if (a.g_head) {
@@ -580,19 +657,27 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   }
   const int64_t groups = a.B * a.L * a.Hk;
   if (shared && groups > 0) {
-    int64_t wgs = (groups * a.K + 255) / 256;
-    if (wgs > 16384) wgs = 16384;
-    for (int i = 0; i < 2; ++i) {
-      const float* part = at(i ? l.dk : l.dq);
-      void* out = i ? a.dk : a.dq;
-      if (a.bf16)
-        hipLaunchKernelGGL(share_kernel<true>, dim3((unsigned)wgs), dim3(256), 0, s, part, out, groups,
-                           r, (int)a.K);
-      else
-        hipLaunchKernelGGL(share_kernel<false>, dim3((unsigned)wgs), dim3(256), 0, s, part, out, groups,
-                           r, (int)a.K);
-      if ((st = check_launch("share_kernel")) != SW_OK) return st;
-    }
+    ShareArgs h{};
+    h.part[0] = at(l.dq);
+    h.part[1] = at(l.dk);
+    h.out[0] = a.dq;
+    h.out[1] = a.dk;
+    h.groups = groups;
+    h.r = r;
+    h.W = (int)a.K;
+    const bool four = a.K % 4 == 0 && ((uintptr_t)a.dq | (uintptr_t)a.dk) % 16 == 0;
+    const int64_t n = groups * a.K / (four ? 4 : 1);
+    const int64_t wgs = (n + 255) / 256 < 16384 ? (n + 255) / 256 : 16384;
+    const dim3 grid((unsigned)wgs, 2), block(256);
+    if (a.bf16 && four)
+      hipLaunchKernelGGL((share_kernel<true, 4>), grid, block, 0, s, h);
+    else if (a.bf16)
+      hipLaunchKernelGGL((share_kernel<true, 1>), grid, block, 0, s, h);
+    else if (four)
+      hipLaunchKernelGGL((share_kernel<false, 4>), grid, block, 0, s, h);
+    else
+      hipLaunchKernelGGL((share_kernel<false, 1>), grid, block, 0, s, h);
+    if ((st = check_launch("share_kernel")) != SW_OK) return st;
   }
   return SW_OK;
 }

@@ -35,7 +35,6 @@ namespace sw {
 namespace lin {
 
 constexpr int CHUNK = 64;      // steps between the places where walks may start or stop
-constexpr int ANCHOR = 256;    // steps between the states kept for dg
 constexpr float G_MIN = -104.0f;  // e^g is zero in fp32 here: the lowest that counts
 
 struct Job {
@@ -74,6 +73,7 @@ struct WalkArgs {
   int64_t per_seq;       // segments of a sequence (cu == NULL)
   int64_t slots;
   int tiles, njobs;
+  int anchor;            // steps between the states kept for dg, a multiple of CHUNK
 };
 
 // Where slot `slot` of width `w` steps lies: packed sequence n's slots start at
@@ -565,9 +565,25 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     each_state([&](int kt, int nt, int i, int64_t at)
                    __attribute__((always_inline)) { p[at] = S[kt][nt][i] * f; });
   };
+  // A kept state: the gradients' walks have Y's columns side by side (skk == 1).
+  auto store_anchor = [&](float* p) __attribute__((always_inline)) {
+    if (a.KK % 4) return store_state(p, 1.0f);
+    int kk = 8 * g, vv = v0 + vb + r;
+    asm volatile("" : "+v"(kk), "+v"(vv));
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      if (vv + 16 * nt < a.VV) {
+        float* row = p + (int64_t)(vv + 16 * nt) * job.svv + kk;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          const int k = 32 * (kt >> 1) + 4 * (kt & 1);
+          if (kk + k < a.KK) *reinterpret_cast<f4*>(row + k) = S[kt][nt];
+        }
+      }
+  };
   auto anchor_at = [&](int64_t i) {  // the sequence's i-th
-    const int64_t per = (a.L + ANCHOR - 1) / ANCHOR;
-    return job.anchors + ((first_slot(pl, a.cu, ANCHOR, per) + i) * a.H + h) * a.KV;
+    const int64_t per = (a.L + a.anchor - 1) / a.anchor;
+    return job.anchors + ((first_slot(pl, a.cu, a.anchor, per) + i) * a.H + h) * a.KV;
   };
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt)
@@ -1078,8 +1094,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       }
     }
     if constexpr (MODE == GRAD) {
-      if (job.anchors && reached > 0 && reached < len && reached % ANCHOR == 0)
-        store_state(anchor_at(reached / ANCHOR - 1), 1.0f);
+      if (job.anchors && reached > 0 && reached < len && reached % a.anchor == 0)
+        store_anchor(anchor_at(reached / a.anchor - 1));
     }
     __syncthreads();  // the tiles are free
     if constexpr (Sh::ROWS) {
@@ -1117,7 +1133,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       store_state(job.last + (pl.n * a.H + h) * a.KV,
                   rev && len > 0 ? exp2_of((double)clamp_g(gp[0]) * 1.4426950408889634) : 1.0f);
     if (MODE == GRAD && job.anchors && job.last_anchor && len > 0)
-      store_state(anchor_at((len + ANCHOR - 1) / ANCHOR - 1), 1.0f);
+      store_anchor(anchor_at((len + a.anchor - 1) / a.anchor - 1));
   }
 }
 
