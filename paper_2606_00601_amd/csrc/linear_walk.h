@@ -25,8 +25,8 @@
 // weighted Z is split in three bf16 parts whose sum is the fp32 value, so S
 // keeps fp32 accuracy whatever the number of chunks.  For an output in bf16
 // (NS = 1), P and S are rounded to bf16 once as operands; for outputs whose
-// products with an input feed an fp32 gradient (NS = 3), both are split in
-// three.  fp32 inputs run on the fp32 matrix instructions throughout.
+// products with an input feed an fp32 gradient, and for outputs of few steps
+// (NS = 3), both are split in three.  fp32 inputs run on the fp32 matrix instructions throughout.
 #pragma once
 
 #include "linear_attn.h"
@@ -413,16 +413,17 @@ struct Tile {
 };
 
 // What a walk is for: the segments' carries; an output; an output whose
-// products with an input are summed by step (with the states kept for dg).
-enum Mode { CARRY, OUT, GRAD };
+// products with an input are summed by step (with the states kept for dg); a
+// bf16 output rounded once, at its end.
+enum Mode { CARRY, OUT, GRAD, OUT_ONCE };
 
 template <class T, int KP, int NT, Mode MODE>
 struct Shared {
   static constexpr int VT = 64 * NT, C = T::C;
-  static constexpr int NS = MODE == GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
+  static constexpr int NS = MODE >= GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
   static constexpr bool XS = MODE != CARRY;
   // fp32 results take the decays between steps to fp32: their running sums in two parts
-  static constexpr bool FINE = MODE == GRAD || !T::SPLIT;
+  static constexpr bool FINE = MODE >= GRAD || !T::SPLIT;
   typename T::E y[C * ROW<T, KP>];
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
@@ -500,7 +501,7 @@ __device__ __forceinline__ LanePlace lane_place(int tid) {
 // fragment of X, Y and P for twice the products: with eight waves of 16 columns
 // instead, LDS reads doubled and set the pace.
 constexpr int walk_waves(int KP, int NT, Mode m) {
-  return KP >= 256 ? 1 : NT == 2 ? 2 : KP == 128 || m == GRAD ? 2 : 4;
+  return KP >= 256 ? 1 : NT == 2 ? 2 : KP == 128 || m >= GRAD ? 2 : 4;
 }
 
 template <class T, int KP, int NT, Mode MODE, bool VEC>
@@ -1144,7 +1145,12 @@ int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY, VEC>), grid, block, 0, st, a);
   else if (m == GRAD)
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD, VEC>), grid, block, 0, st, a);
-  else
+  else if constexpr (T::SPLIT && NT == 1) {  // OUT_ONCE takes tiles of 64 columns
+    if (m == OUT_ONCE)
+      hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT_ONCE, VEC>), grid, block, 0, st, a);
+    else
+      hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
+  } else
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
   return check_launch("walk_kernel");
 }
