@@ -460,8 +460,9 @@ int64_t sw_selective_scan_bwd_workspace(int64_t B, int64_t D, int64_t N, int64_t
  * zero).
  *
  * The state and all sums are fp32; bf16 inputs run on bf16 matrix instructions
- * with the state's increments split so that they keep fp32 accuracy, and o is
- * rounded once more where the chunk's weights and the state become operands.
+ * with the state's increments split so that they keep fp32 accuracy.  o is then
+ * rounded once more where the chunk's weights and the state become operands (not
+ * so in calls of at most 128 steps with few heads, nor with fp32 inputs).
  * An infinity or NaN in q, k, v or g reaches the steps from its own on, as in
  * the recurrence, and no earlier one.
  *
@@ -493,7 +494,9 @@ int64_t sw_linear_attn_fwd_workspace(int64_t B, int64_t L, int64_t Hk, int64_t H
  *   dh_last : (nseq, H, K, V) fp32 or NULL (zero)
  *   dq, dk, dv : dense, of dtype, rounded once from fp32;  dg : (B, L, H) fp32, or
  *   (H) with SW_LINEAR_G_HEAD;  dh0 : (nseq, H, K, V) fp32 or NULL
- * Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
+ * The gradients of q and k feed dg, so their operands keep fp32 accuracy; dv is
+ * rounded as o is.  An infinity or NaN reaches the steps that it reaches through
+ * these sums.  Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
  * Otherwise as sw_linear_attn_fwd.
  */
 int sw_linear_attn_bwd(const void* q, const void* k, const void* v, const float* g,

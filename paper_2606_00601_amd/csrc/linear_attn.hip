@@ -305,10 +305,9 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   const int64_t longest = a.L, chunks = (longest + CHUNK - 1) / CHUNK;
   const int64_t rows = a.B * a.H;
   // Rounded once where a call is so short that its launch is what it costs: one or
-  // two chunks, no compute unit with more than one of them (L=100 H=4 K=V=64: 12.0 us,
-  // 11.7 otherwise).
-  // Elsewhere P and S are operands of bf16, which with the output's own rounding
-  // makes 1.41 times its error, spread over many elements.
+  // two chunks, and no compute unit with more than one workgroup (L=100 H=4 K=V=64:
+  // 12.0 us, 11.7 otherwise).  Elsewhere P and S are rounded to bf16 as operands, which
+  // with the output's own rounding makes 1.41 times its error.
   if (a.bf16 && chunks <= 2 && (a.cu ? a.nseq : a.B) * a.H * ((a.V + 63) / 64) <= cus) {
     p.out = OUT_ONCE;
     p.nt_v = 1;

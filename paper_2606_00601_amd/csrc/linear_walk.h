@@ -199,8 +199,8 @@ __device__ __forceinline__ f4 mma(const Frag<F32>& a, const Frag<F32>& b, f4 c) 
 // Rows have 32 bytes of padding: 32 bytes of each of eight neighbouring rows lie
 // in different banks.  In Y (bf16), 16-byte granules of odd pairs have their halves
 // exchanged: a transposed read takes the same half of four granules, and so meets
-// all of those 32 bytes.  Counted, the reads of X's, Y's and Z's fragments take the
-// cycles that their bytes need.
+// all of those 32 bytes.  By the conflict counter the reads of X's, Y's and Z's
+// fragments take the cycles that their bytes need.
 template <class T, int W>
 constexpr int ROW = W + 2 * T::G;
 
@@ -319,20 +319,6 @@ __device__ __forceinline__ void parts_of(const float* x, Frag<F32>* f) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[0].v[j] = x[j];
 }
-__device__ __forceinline__ void widen(const Frag<Bf16>& f, float* x) {
-  const uint4 u = __builtin_bit_cast(uint4, f.v);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x[2 * j] = bf16_lo(w[j]);
-    x[2 * j + 1] = bf16_hi(w[j]);
-  }
-}
-__device__ __forceinline__ void widen(const Frag<F32>& f, float* x) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = f.v[j];
-}
-
 __device__ __forceinline__ float widen1(uint16_t e) { return bf16_one(e); }
 __device__ __forceinline__ float widen1(float e) { return e; }
 
@@ -458,8 +444,7 @@ struct Count {
 // instructions that run beside it, the next product.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
-// Two values of an operand fragment on their way into N bf16 parts, a few
-// instructions at a time: step 0 .. N - 1 (or N, after a step that weighs them).
+// Two values of an operand fragment on their way into bf16 parts, one part a call.
 struct Pair {
   float a, b;
   __device__ __forceinline__ uint32_t part(bool last) {
@@ -475,12 +460,6 @@ template <int N>
 struct Parts {  // of one fragment: its pairs' N parts
   Pair x[4];
   u4 u[N];
-  // STEPS steps for each pair; done(i): step i of all
-  static constexpr int STEPS = 4 * N;
-  __device__ __forceinline__ void step(int i) {
-    const int j = i / N, q = i % N;
-    u[q][j] = x[j].part(q == N - 1);
-  }
   __device__ __forceinline__ Frag<Bf16> frag(int q) const {
     return {__builtin_bit_cast(s8, u[q])};
   }
