@@ -67,11 +67,11 @@ __global__ __launch_bounds__(threads_of(LPR)) void gated_fwd_kernel(GatedNormArg
 // dz = du x silu'(z), dw = sum dy n.  After: the same with u = x and the gate's
 // share of dy: dn = w dy silu(z), dz = w dy n silu'(z), dw = sum dy n silu(z).  The
 // gate's place is a parameter of the kernel: as a branch it cost 72 us where this
-// takes 65 (16384 rows of 12 groups of 128, bf16, 252 MB at 3.9 TB/s; the issue of
-// its ~25 operations a column bounds it with the loads).
-template <class E, Gate GATE, int LPR, int NV>
+// takes 65, and `vec` as one made each load wait for the one before: 51 us without
+// (16384 rows of 12 groups of 128, bf16, 252 MB at 4.9 TB/s).
+template <class E, Gate GATE, bool vec, int LPR, int NV>
 __global__ __launch_bounds__(threads_of(LPR)) void gated_bwd_kernel(GatedNormArgs a, int groups,
-                                                                    float* part, bool vec) {
+                                                                    float* part) {
   constexpr int RPW = threads_of(LPR) / LPR;
   __shared__ RowSum<LPR, 2> sh;
   __shared__ float lds[partial_lds<LPR, NV>];
@@ -150,15 +150,20 @@ int fwd_gated(const GatedNormArgs& a, int groups, int64_t wgs, bool vec, hipStre
   return check_launch("gated_fwd_kernel");
 }
 
-template <class E, Gate GATE>
-int bwd_gated(const GatedNormArgs& a, int groups, float* part, int64_t blocks, bool vec,
-              hipStream_t s) {
-#define CALL(LPR, NV)                                                                       \
-  hipLaunchKernelGGL((gated_bwd_kernel<E, GATE, LPR, NV>), dim3((unsigned)(blocks * groups)), \
-                     dim3(threads_of(LPR)), 0, s, a, groups, part, vec)
+template <class E, Gate GATE, bool VEC>
+int bwd_vec(const GatedNormArgs& a, int groups, float* part, int64_t blocks, hipStream_t s) {
+#define CALL(LPR, NV)                                                                              \
+  hipLaunchKernelGGL((gated_bwd_kernel<E, GATE, VEC, LPR, NV>), dim3((unsigned)(blocks * groups)), \
+                     dim3(threads_of(LPR)), 0, s, a, groups, part)
   SW_NORM_PICK_BWD(a.group, CALL);
 #undef CALL
   return check_launch("gated_bwd_kernel");
+}
+template <class E, Gate GATE>
+int bwd_gated(const GatedNormArgs& a, int groups, float* part, int64_t blocks, bool vec,
+              hipStream_t s) {
+  return vec ? bwd_vec<E, GATE, true>(a, groups, part, blocks, s)
+             : bwd_vec<E, GATE, false>(a, groups, part, blocks, s);
 }
 
 template <class E>

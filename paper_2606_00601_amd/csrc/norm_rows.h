@@ -161,7 +161,7 @@ inline int64_t bwd_blocks(int64_t M, int64_t D, int64_t width, int cus) {
 // CALL(LPR, NV) for the smallest that holds a row of `width`; a wave for each row
 // of up to 1536 columns needs no barrier.  A backward's registers hold more of each column, so a row takes more lanes: at
 // 16384 rows of 1536 (residual norm, fp32 stream) 64 lanes of three vectors ran two
-// waves per SIMD and 121 us, 192 lanes of one four waves and 102.  Rows over 8192
+// waves per SIMD and 121 us, 192 lanes of one four waves and 96.  Rows over 8192
 // spill some of theirs.
 #define SW_NORM_PICK_BWD(width, CALL)           \
   do {                                          \

@@ -59,11 +59,11 @@ __global__ __launch_bounds__(threads_of(LPR)) void res_fwd_kernel(ResNormArgs a,
 // dR' = dres + inv (w dy - n mean(w dy n)), n = R' inv; dx = s dR', dw = sum dy n,
 // ds = sum x dR'.  Both sums of a row, of R'^2 and of w dy R', are of what the
 // row's lanes hold, so one pass over memory gives everything.  16384 rows of 1536,
-// bf16 with an fp32 stream and a scale: 102 us, 453 MB at 4.4 TB/s; the second
-// round of loads (dres, x) after the sums keeps it from the copy's 5.1.
-template <class E, class R, int LPR, int NV>
-__global__ __launch_bounds__(threads_of(LPR)) void res_bwd_kernel(ResNormArgs a, float* part,
-                                                                  bool vec) {
+// bf16 with an fp32 stream and a scale: 96 us, 453 MB at 4.7 TB/s.  All of a row's
+// loads are issued before its sums; as a branch in the kernel `vec` made each wait for
+// the one before (102 us).
+template <class E, class R, bool vec, int LPR, int NV>
+__global__ __launch_bounds__(threads_of(LPR)) void res_bwd_kernel(ResNormArgs a, float* part) {
   constexpr int RPW = threads_of(LPR) / LPR;
   __shared__ RowSum<LPR, 2> sh;
   __shared__ float lds[partial_lds<LPR, NV>];
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(threads_of(LPR)) void res_bwd_kernel(ResNormArgs a,
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[v][j] = ds[v][j] = 0.0f;
   for (int64_t m = blockIdx.x * (int64_t)RPW + sub; m < a.M; m += gridDim.x * (int64_t)RPW) {
-    float r[NV][8], d[NV][8], w[NV][8];
+    float r[NV][8], d[NV][8], w[NV][8], t[NV][8], x[NV][8];
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -83,6 +83,8 @@ __global__ __launch_bounds__(threads_of(LPR)) void res_bwd_kernel(ResNormArgs a,
       load8((const R*)a.stored + m * a.stored_st + c, r[v], a.D - c, vec);
       load8((const E*)a.dy + m * a.dy_st + c, d[v], a.D - c, vec);
       load8(a.w + c, w[v], a.D - c, vec);
+      if (a.dres) load8((const R*)a.dres + m * a.dres_st + c, t[v], a.D - c, vec);
+      if (a.s) load8((const E*)a.x + m * a.x_st + c, x[v], a.D - c, vec);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         sum[0] = __builtin_fmaf(r[v][j], r[v][j], sum[0]);
@@ -95,23 +97,21 @@ __global__ __launch_bounds__(threads_of(LPR)) void res_bwd_kernel(ResNormArgs a,
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int64_t c = (v * LPR + li) * 8;
-      float dr[8], t[8];
-      if (a.dres) load8((const R*)a.dres + m * a.dres_st + c, t, a.D - c, vec);
+      float dr[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float n = r[v][j] * inv;
         dw[v][j] = __builtin_fmaf(d[v][j], n, dw[v][j]);
         dr[j] = inv * (w[v][j] * d[v][j] - n * mean);
-        if (a.dres) dr[j] += t[j];
+        if (a.dres) dr[j] += t[v][j];
       }
       if (a.dr) store8((R*)a.dr + m * a.D + c, dr, a.D - c, vec);
       if (a.s) {
-        float s[8], x[8];
+        float s[8];
         load8(a.s + c, s, a.D - c, vec);
-        load8((const E*)a.x + m * a.x_st + c, x, a.D - c, vec);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          ds[v][j] = __builtin_fmaf(x[j], dr[j], ds[v][j]);
+          ds[v][j] = __builtin_fmaf(x[v][j], dr[j], ds[v][j]);
           dr[j] *= s[j];
         }
       }
@@ -138,14 +138,18 @@ int fwd_typed(const ResNormArgs& a, int64_t wgs, bool vec, hipStream_t s) {
   return check_launch("res_fwd_kernel");
 }
 
-template <class E, class R>
-int bwd_typed(const ResNormArgs& a, float* part, int64_t blocks, bool vec, hipStream_t s) {
-#define CALL(LPR, NV)                                                                \
-  hipLaunchKernelGGL((res_bwd_kernel<E, R, LPR, NV>), dim3((unsigned)blocks), \
-                     dim3(threads_of(LPR)), 0, s, a, part, vec)
+template <class E, class R, bool VEC>
+int bwd_vec(const ResNormArgs& a, float* part, int64_t blocks, hipStream_t s) {
+#define CALL(LPR, NV)                                                              \
+  hipLaunchKernelGGL((res_bwd_kernel<E, R, VEC, LPR, NV>), dim3((unsigned)blocks), \
+                     dim3(threads_of(LPR)), 0, s, a, part)
   SW_NORM_PICK_BWD(a.D, CALL);
 #undef CALL
   return check_launch("res_bwd_kernel");
+}
+template <class E, class R>
+int bwd_typed(const ResNormArgs& a, float* part, int64_t blocks, bool vec, hipStream_t s) {
+  return vec ? bwd_vec<E, R, true>(a, part, blocks, s) : bwd_vec<E, R, false>(a, part, blocks, s);
 }
 
 // Sums of the partial rows: 16 columns of one gradient, 16 rows at a time, added
