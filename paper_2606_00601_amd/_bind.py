@@ -23,6 +23,11 @@ def _need(t, name, dtype, shape=None):
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
 
 
+def _dense_like(t):
+    """A dense tensor of t's shape and type, not filled."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _get_device = getattr(torch._C, "_cuda_getDevice", None)
 

@@ -10,10 +10,16 @@ from __future__ import annotations
 
 import torch
 
-from ._bind import _need, _on, _ptr
+from ._bind import _dense_like, _need, _on, _ptr
 from ._lib import SW_DTYPE_BF16, SW_DTYPE_F32, SW_LINEAR_G_HEAD, check, fast
 
 _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
+
+
+def _steps(st, shape):
+    """The strides of two or three leading dimensions, 0 along a dimension of one."""
+    a, b = (st[0] if shape[0] > 1 else 0), (st[1] if shape[1] > 1 else 0)
+    return (a, b) if len(shape) == 2 else (a, b, st[2] if shape[2] > 1 else 0)
 
 
 def _need_rows(t, name, dtype, shape):
@@ -30,7 +36,7 @@ def _need_rows(t, name, dtype, shape):
     st = t.stride()
     if shape[-1] > 1 and st[-1] != 1 and t.numel():
         raise ValueError(f"{name} must be contiguous along its last dimension")
-    return tuple(s if n > 1 else 0 for s, n in zip(st[:-1], shape[:-1]))
+    return _steps(st, shape[:-1])
 
 
 def _need_decay(g, lead, H):
@@ -45,7 +51,7 @@ def _need_decay(g, lead, H):
         return (0,) * len(lead) + (g.stride(0) if H > 1 else 0,), SW_LINEAR_G_HEAD
     if g.shape != (*lead, H):
         raise ValueError(f"g must have shape {(*lead, H)} or {(H,)} (got {tuple(g.shape)})")
-    return tuple(s if n > 1 else 0 for s, n in zip(g.stride(), g.shape)), 0
+    return _steps(g.stride(), g.shape), 0
 
 
 def _operands(q, k, v, g, h0, cu_seqlens):
@@ -94,7 +100,7 @@ def linear_attn_fwd(q, k, v, g, *, scale=None, h0=None, cu_seqlens=None, o=None,
     sizes, st, dt, flags = _operands(q, k, v, g, h0, cu_seqlens)
     B, L, Hk, H, K, V, n = sizes
     if o is None:
-        o = torch.empty((B, L, H, V), dtype=q.dtype, device=q.device)
+        o = _dense_like(v)
     else:
         _need(o, "o", q.dtype, (B, L, H, V))
     if not want_h_last:
@@ -209,7 +215,7 @@ def linear_attn_step(q, k, v, g, state, *, scale=None, slots=None, o=None):
     elif pool < B:
         raise ValueError(f"state holds {pool} sequences (got {B})")
     if o is None:
-        o = torch.empty((B, H, V), dtype=dt, device=q.device)
+        o = _dense_like(v)
     else:
         _need(o, "o", dt, (B, H, V))
     with _on(q.device):

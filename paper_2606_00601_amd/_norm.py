@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import torch
 
-from ._bind import _need, _on, _ptr
+from ._bind import _dense_like, _need, _on, _ptr
 from ._lib import SW_DTYPE_BF16, SW_DTYPE_F32, SW_GATE_AFTER, check, fast
 
 _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
@@ -77,8 +77,8 @@ def residual_norm_fwd(x, weight, residual=None, *, res_scale=None, eps=1e-6):
     if residual is not None:
         rt = _res_type(residual, "residual", dt)
         rr, r_st = _rows(residual, "residual", rt, shape)
-        out = torch.empty(shape, dtype=rt, device=x.device)
-    y = torch.empty(shape, dtype=dt, device=x.device)
+        out = _dense_like(residual)
+    y = _dense_like(x)
     with _on(x.device):
         check(fast().sw_residual_norm_fwd(
             _ptr(xr), _ptr(rr), _ptr(weight), _ptr(res_scale), _ptr(y), _ptr(out), M, D, x_st, r_st,
@@ -106,9 +106,9 @@ def residual_norm_bwd(dy, dres, residual_out, weight, *, x=None, res_scale=None,
         xr, x_st = _rows(x, "x", dt, shape)
     f32 = dict(dtype=torch.float32, device=dy.device)
     same = res_scale is None and rt is dt
-    out = {"dresidual": torch.empty(shape, dtype=rt, device=dy.device),
+    out = {"dresidual": _dense_like(residual_out),
            "dweight": torch.empty((D,), **f32)}
-    out["dx"] = out["dresidual"] if same else torch.empty(shape, dtype=dt, device=dy.device)
+    out["dx"] = out["dresidual"] if same else _dense_like(dy)
     if res_scale is not None:
         out["dres_scale"] = torch.empty((D,), **f32)
     with _on(dy.device):
@@ -178,7 +178,7 @@ def gated_norm_fwd(x, z, weight, *, group=None, gate_after=False, eps=1e-6):
     (..., D) fp32 or bf16, z None for no gate; weight (D,) fp32.  Returns y.
     """
     shape, M, D, dt, group, xr, x_st, zr, z_st, flags = _gated(x, z, weight, group, gate_after)
-    y = torch.empty(shape, dtype=dt, device=x.device)
+    y = _dense_like(x)
     with _on(x.device):
         check(fast().sw_gated_norm_fwd(
             _ptr(xr), _ptr(zr), _ptr(weight), _ptr(y), M, D, group, x_st, z_st, _DTYPES[dt], flags,
@@ -191,10 +191,10 @@ def gated_norm_bwd(dy, x, z, weight, *, group=None, gate_after=False, eps=1e-6):
     inputs' type and ``dweight`` (D,) fp32."""
     shape, M, D, dt, group, xr, x_st, zr, z_st, flags = _gated(x, z, weight, group, gate_after)
     d, d_st = _rows(dy, "dy", dt, shape)
-    out = {"dx": torch.empty(shape, dtype=dt, device=x.device),
+    out = {"dx": _dense_like(x),
            "dweight": torch.empty((D,), dtype=torch.float32, device=x.device)}
     if z is not None:
-        out["dz"] = torch.empty(shape, dtype=dt, device=x.device)
+        out["dz"] = _dense_like(z)
     with _on(x.device):
         ws, nws = _workspace(M, D, group, 1, x.device)
         check(fast().sw_gated_norm_bwd(
