@@ -40,38 +40,57 @@ __global__ __launch_bounds__(256) void fold_kernel(FoldArgs a) {
     parts = a.per_seq;
   }
   constexpr int U = 4;  // elements of a thread
-  const int64_t e0 = blk * (256 * U) + threadIdx.x;
+  const int KV = (int)a.KV, e0 = (int)blk * (256 * U) + (int)threadIdx.x;
   float s[U];
-  bool in[U];
+  uint32_t e[U];  // past the state: its last element, read and left alone
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    in[u] = e0 + 256 * u < a.KV;
-    s[u] = in[u] && job.init ? job.init[(n * a.H + h) * a.KV + e0 + 256 * u] : 0.0f;
+    e[u] = e0 + 256 * u < KV ? e0 + 256 * u : KV - 1;
+    s[u] = job.init ? (job.init + (n * a.H + h) * a.KV)[e[u]] : 0.0f;
   }
-  constexpr int D = 4;  // segments whose carries are in flight
-  for (int64_t j0 = 0; j0 < parts; j0 += D) {
-    float c[D][U], dec[D];
+  float* const carry = job.carry;
+  const float* const decay = job.decay;
+  const bool reverse = job.reverse;
+  auto place = [&](int64_t j) { return (first + (reverse ? parts - 1 - j : j)) * a.H + h; };
+  auto put = [&](int64_t j) __attribute__((always_inline)) {  // segment j's initial state
+    float* const p = carry + place(j) * a.KV;
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      const int64_t j = j0 + d, slot = first + (job.reverse ? parts - 1 - j : j);
-      const bool has = j < parts - 1;  // the last one hands nothing on
-      dec[d] = has ? job.decay[slot * a.H + h] : 0.0f;
+    for (int u = 0; u < U; ++u)
+      if (e0 + 256 * u < KV) p[e[u]] = s[u];
+  };
+  // The carries of N segments in flight at once, read without a branch: where few
+  // heads make few workgroups, the reads' latency is what this costs (H=1 L=32996
+  // K=16 V=128, 172 segments: 125 us with 4 of them, 74 with 16).  Where few are
+  // left, four: 64 reads for a sequence of one or two segments took 5 us of 95.
+  auto compose = [&](auto count, int64_t j0) __attribute__((always_inline)) {
+    constexpr int N = decltype(count)::value;
+    float c[N][U], dec[N];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        c[d][u] = has && in[u] ? job.carry[(slot * a.H + h) * a.KV + e0 + 256 * u] : 0.0f;
+    for (int d = 0; d < N; ++d) {
+      const int64_t at = place(j0 + d < parts - 1 ? j0 + d : parts - 2);  // past them: not used
+      dec[d] = decay[at];
+      const float* const p = carry + at * a.KV;
+#pragma unroll
+      for (int u = 0; u < U; ++u) c[d][u] = p[e[u]];
     }
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      const int64_t j = j0 + d, slot = first + (job.reverse ? parts - 1 - j : j);
-      if (j < parts) {
+    for (int d = 0; d < N; ++d) {
+      if (j0 + d >= parts - 1) break;
+      put(j0 + d);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (in[u]) job.carry[(slot * a.H + h) * a.KV + e0 + 256 * u] = s[u];
-          s[u] = __builtin_fmaf(dec[d], s[u], c[d][u]);
-        }
-      }
+      for (int u = 0; u < U; ++u) s[u] = __builtin_fmaf(dec[d], s[u], c[d][u]);
+    }
+  };
+  for (int64_t j = 0; j < parts - 1;) {  // the last segment hands nothing on
+    if (parts - 1 - j > 4) {
+      compose(Count<16>(), j);
+      j += 16;
+    } else {
+      compose(Count<4>(), j);
+      j += 4;
     }
   }
+  put(parts - 1);
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -280,21 +299,23 @@ struct Plan {
   int64_t aper = 1, aslots = 0;
 };
 
-// Workgroups of a walk that share a compute unit (registers and LDS), and what a
-// chunk then takes, in units of one alone: two side by side finish in 1.5 of it.
-int resident(int64_t contracted, int nt) {
-  return contracted > 128 ? 1 : contracted <= 64 && nt == 1 ? 3 : 2;
-}
-double pace(int64_t wgs, int cus, int res) {
+// What a chunk of a walk takes, in units of one alone, where `wgs` workgroups are
+// spread over the compute units: how many share one (registers and LDS), and what
+// each beside the first adds.  Two side by side finish in 1.5; narrow fp32 walks,
+// whose chunks are half as long and wait for one product after another, in 1.3.
+double pace(int64_t wgs, int cus, int64_t contracted, int nt, bool bf16) {
+  const bool narrow = contracted <= 64 && nt == 1;
+  const int res = contracted > 128 ? 1 : !narrow ? 2 : bf16 ? 3 : 4;
+  const double more = narrow && !bf16 ? 0.3 : 0.5;
   const int64_t load = (wgs + cus - 1) / cus;  // of the fullest compute unit
   const int64_t rounds = load / res, rest = load % res;
-  return rounds * (1.0 + 0.5 * (res - 1)) + (rest ? 1.0 + 0.5 * (rest - 1) : 0.0);
+  return rounds * (1.0 + more * (res - 1)) + (rest ? 1.0 + more * (rest - 1) : 0.0);
 }
 
 // Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
 // alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, gradient
-// with its row sums 9.5; a workgroup's start and end are worth two chunks, the
-// composition's launch 12 us.  At B=8 L=2048 H=12 forward and backward took 680 us
+// with its row sums 9.5; a workgroup's start and end are worth two chunks of the
+// kernel's (one of these for fp32), the composition 12 us and 0.1 for each segment.  At B=8 L=2048 H=12 forward and backward took 680 us
 // with the backward's sequences whole and 552 in the parts chosen.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
@@ -316,16 +337,16 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   int64_t parts = 1;
   double best = 0.0;
   for (int64_t n = 1; n <= 256 && (n == 1 || 2 * n <= chunks); ++n) {
-    const double len = (double)((chunks + n - 1) / n) + 2.0;
+    const double len = (double)((chunks + n - 1) / n) + (a.bf16 ? 2.0 : 1.0);
     double us;
     if (bwd) {
-      const double two = pace(rows * n * 2 * p.tiles_k, cus, resident(a.V, p.nt_k));
+      const double two = pace(rows * n * 2 * p.tiles_k, cus, a.V, p.nt_k, a.bf16);
       us = len * (two * (9.5 + (n > 1 ? 3.0 : 0.0)) +
-                  5.5 * pace(rows * n * p.tiles_v, cus, resident(a.K, p.nt_v)));
+                  5.5 * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16));
     } else {
-      us = len * pace(rows * n * p.tiles_v, cus, resident(a.K, p.nt_v)) * (n > 1 ? 8.5 : 5.5);
+      us = len * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16) * (n > 1 ? 8.5 : 5.5);
     }
-    if (n > 1) us += 12.0;
+    if (n > 1) us += 12.0 + 0.1 * (double)n;
     if (n == 1 || us < best) {
       best = us;
       parts = n;
