@@ -315,8 +315,9 @@ double pace(int64_t wgs, int cus, int64_t contracted, int nt, bool bf16) {
 // Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
 // alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, gradient
 // with its row sums 9.5; a workgroup's start and end are worth two chunks of the
-// kernel's (one of these for fp32), the composition 12 us and 0.1 for each segment.  At B=8 L=2048 H=12 forward and backward took 680 us
-// with the backward's sequences whole and 552 in the parts chosen.
+// kernel's (one of these for fp32), the composition 12 us and 0.1 for each segment.
+// At B=8 L=2048 H=12 forward and backward took 680 us with the backward's sequences
+// whole and 552 in the parts chosen.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
   p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
