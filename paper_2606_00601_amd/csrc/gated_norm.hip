@@ -202,6 +202,9 @@ int gated_norm_bwd(const GatedNormArgs& a) {
   if ((st = device_cus(&cus)) != SW_OK) return st;
   const hipStream_t s = current_stream();
   const int groups = (int)(a.D / a.group);
+  float* outs[2] = {a.dw, nullptr};
+  // no rows: a sum of none, and inputs that may be NULL
+  if (a.M == 0) return fold_partials(nullptr, 0, a.D, outs, 1, s);
   const int64_t blocks = bwd_blocks(a.M, a.D, a.group, cus);
   Partials part(s);
   if ((st = part.get(a.ws, a.ws_bytes, (size_t)(blocks * a.D * 4), "sw_gated_norm_bwd")) != SW_OK)
@@ -212,7 +215,6 @@ int gated_norm_bwd(const GatedNormArgs& a) {
   st = a.bf16 ? bwd_typed<uint16_t>(a, groups, part.p, blocks, vec, s)
               : bwd_typed<float>(a, groups, part.p, blocks, vec, s);
   if (st != SW_OK) return st;
-  float* outs[2] = {a.dw, nullptr};
   return fold_partials(part.p, blocks, a.D, outs, 1, s);
 }
 

@@ -153,7 +153,7 @@ int bwd_typed(const ResNormArgs& a, float* part, int64_t blocks, bool vec, hipSt
 }
 
 // Sums of the partial rows: 16 columns of one gradient, 16 rows at a time, added
-// in a fixed order.
+// in a fixed order; of no rows zero.
 struct Outs {
   float* p[2];
 };
@@ -224,6 +224,9 @@ int residual_norm_bwd(const ResNormArgs& a) {
   if ((st = device_cus(&cus)) != SW_OK) return st;
   const hipStream_t s = current_stream();
   const int grads = a.s ? 2 : 1;
+  float* outs[2] = {a.dw, a.ds};
+  // no rows: sums of none, and inputs that may be NULL
+  if (a.M == 0) return fold_partials(nullptr, 0, a.D, outs, grads, s);
   const int64_t blocks = bwd_blocks(a.M, a.D, a.D, cus);
   Partials part(s);
   if ((st = part.get(a.ws, a.ws_bytes, (size_t)(blocks * a.D * 4 * grads),
@@ -241,7 +244,6 @@ int residual_norm_bwd(const ResNormArgs& a) {
   else
     st = bwd_typed<uint16_t, float>(a, part.p, blocks, vec, s);
   if (st != SW_OK) return st;
-  float* outs[2] = {a.dw, a.ds};
   return fold_partials(part.p, blocks, a.D, outs, grads, s);
 }
 
