@@ -453,11 +453,12 @@ int64_t sw_selective_scan_bwd_workspace(int64_t B, int64_t D, int64_t N, int64_t
  * depend on it.
  *
  * cu_seqlens: NULL (then nseq = B), or (nseq + 1) int32 device values, ascending
- * from 0 to L: B = 1 and the row of L steps holds nseq sequences, sequence n the
+ * within [0, L]: B = 1 and the row of L steps holds nseq sequences, sequence n the
  * steps cu_seqlens[n] .. cu_seqlens[n+1] - 1, each with its own state.  They are
- * read by the kernels only and held to [0, L]; o at steps that no sequence
- * covers is not written.  A sequence may be empty: its h_last is its h0 (or
- * zero).
+ * read by the kernels only and held to [0, L].  Steps that no sequence covers (a
+ * row padded to a fixed length) read as zero in o, and in every gradient; what q,
+ * k, v, g and dout hold there is not used.  A sequence may be empty: its h_last is
+ * its h0 (or zero).
  *
  * The state and all sums are fp32; bf16 inputs run on bf16 matrix instructions
  * with the state's increments split so that they keep fp32 accuracy.  o is then

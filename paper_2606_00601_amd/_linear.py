@@ -94,8 +94,9 @@ def linear_attn_fwd(q, k, v, g, *, scale=None, h0=None, cu_seqlens=None, o=None,
     bf16, K and V at most 256; g: (B, L, H), or (H,) for one decay a head, fp32.
     ``scale`` is K ** -0.5 if not given.  ``h0`` (n, H, K, V) fp32 is the initial
     state, e.g. the h_last of an earlier part.  With ``cu_seqlens`` (n + 1,) int32,
-    ascending from 0 to L, B is 1 and the row holds n sequences one after the
-    other (o at steps that none of them covers is not written); else n = B.
+    ascending within [0, L], B is 1 and the row holds n sequences one after the
+    other (o is zero at steps that none of them covers, as are the gradients);
+    else n = B.
     """
     sizes, st, dt, flags = _operands(q, k, v, g, h0, cu_seqlens)
     B, L, Hk, H, K, V, n = sizes

@@ -287,6 +287,39 @@ __global__ __launch_bounds__(256) void share_kernel(ShareArgs a) {
   }
 }
 
+// Zeros at the steps of a packed row that no sequence covers (a row padded to a
+// fixed length): before cu[0] and from cu[nseq] on, `per[i]` units of `unit` bytes a
+// step of each output.  The range is known on the device only, so the launch is made
+// for every packed call; where all steps are covered it ends at once.
+struct ClearArgs {
+  void* out[4];
+  int64_t per[4];
+  int unit[4];
+  const int32_t* cu;
+  int64_t nseq, L;
+};
+template <class U>
+__device__ __forceinline__ void clear_units(void* out, int64_t first, int64_t end) {
+  U* const p = (U*)out;
+  for (int64_t i = first + blockIdx.x * 256ll + threadIdx.x; i < end; i += gridDim.x * 256ll)
+    p[i] = U{};
+}
+__global__ __launch_bounds__(256) void clear_kernel(ClearArgs a) {
+  const int64_t c0 = cu_at(a.cu, 0, a.L), cn = cu_at(a.cu, a.nseq, a.L);
+  const int64_t per = a.per[blockIdx.y];
+  const int unit = a.unit[blockIdx.y];
+  void* const out = a.out[blockIdx.y];
+  const int64_t spans[2][2] = {{0, c0}, {cn > c0 ? cn : c0, a.L}};
+  for (const auto& s : spans) {
+    if (unit == 16)
+      clear_units<u4>(out, s[0] * per, s[1] * per);
+    else if (unit == 4)
+      clear_units<uint32_t>(out, s[0] * per, s[1] * per);
+    else
+      clear_units<uint16_t>(out, s[0] * per, s[1] * per);
+  }
+}
+
 // -------------------------------------------------------------- planning
 
 struct Plan {
@@ -495,6 +528,22 @@ int launch_fold(const LinAttnArgs& a, const Plan& p, FoldArgs& f, int njobs, hip
   return check_launch("fold_kernel");
 }
 
+// An output of rows of `row` bytes a step for the next clearing launch.
+void add_clear(ClearArgs& c, int* n, void* out, int64_t row) {
+  const uintptr_t at = (uintptr_t)out | (uintptr_t)row;
+  c.unit[*n] = at % 16 == 0 ? 16 : at % 4 == 0 ? 4 : 2;
+  c.per[*n] = row / c.unit[*n];
+  c.out[(*n)++] = out;
+}
+
+int launch_clear(const LinAttnArgs& a, ClearArgs& c, int n, hipStream_t s) {
+  c.cu = a.cu;
+  c.nseq = a.nseq;
+  c.L = a.L;
+  hipLaunchKernelGGL(clear_kernel, dim3(256, (unsigned)n), dim3(256), 0, s, c);
+  return check_launch("clear_kernel");
+}
+
 int check_grid(const LinAttnArgs& a, const Plan& p, bool bwd) {
   const int64_t tiles = p.tiles_k > p.tiles_v ? p.tiles_k : p.tiles_v;
   const int64_t blocks = (a.K * a.V + 1023) / 1024;
@@ -578,7 +627,12 @@ int linear_attn_fwd(const LinAttnArgs& a) {
     if ((st = launch_fold(a, p, f, 1, s)) != SW_OK) return st;
   }
   w.job[0] = j;
-  return launch_walk_any(a, w, p.out, a.K, a.V, p.nt_v, p.tiles_v, s);
+  if ((st = launch_walk_any(a, w, p.out, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
+  if (!a.cu || a.L == 0) return SW_OK;
+  ClearArgs c{};
+  int n = 0;
+  add_clear(c, &n, a.o, a.H * a.V * (a.bf16 ? 2 : 4));
+  return launch_clear(a, c, n, s);
 }
 
 int linear_attn_bwd(const LinAttnArgs& a) {
@@ -711,7 +765,15 @@ int linear_attn_bwd(const LinAttnArgs& a) {
       hipLaunchKernelGGL((share_kernel<false, 1>), grid, block, 0, s, h);
     if ((st = check_launch("share_kernel")) != SW_OK) return st;
   }
-  return SW_OK;
+  if (!a.cu || a.L == 0) return SW_OK;
+  ClearArgs c{};
+  int n = 0;
+  const int64_t es = a.bf16 ? 2 : 4;
+  add_clear(c, &n, a.dq, a.Hk * a.K * es);
+  add_clear(c, &n, a.dk, a.Hk * a.K * es);
+  add_clear(c, &n, a.dv, a.H * a.V * es);
+  if (!a.g_head) add_clear(c, &n, a.dg, a.H * 4);
+  return launch_clear(a, c, n, s);
 }
 
 // ---------------------------------------------------------------- one step
