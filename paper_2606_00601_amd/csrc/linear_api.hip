@@ -112,17 +112,17 @@ int bwd_common(const LinAttnArgs& a) {
   int st, dev, nin;
   if ((st = check_sizes(a)) != SW_OK) return st;
   const int64_t T = a.B * a.L;
-  if (a.H == 0) return SW_OK;
-  const bool any = T > 0, states = a.nseq > 0 && a.dh0;
-  if (!any && !states && !a.g_head) return SW_OK;
+  // without heads only dq and dk hold anything: sums over none
+  const bool any = T > 0 && (a.H > 0 || a.Hk > 0), states = a.nseq * a.H > 0 && a.dh0;
+  if (!any && !states && !(a.g_head && a.H > 0)) return SW_OK;
   if ((st = current_device(&dev)) != SW_OK) return st;
   Span ins[8];
   if ((st = check_inputs(a, dev, true, ins, &nin)) != SW_OK) return st;
   const size_t es = a.bf16 ? 2 : 4, nh = (size_t)(a.nseq * a.H * a.K * a.V) * 4;
   if ((st = check_ptr(a.dq, es, "dq", any, dev)) != SW_OK) return st;
   if ((st = check_ptr(a.dk, es, "dk", any, dev)) != SW_OK) return st;
-  if ((st = check_ptr(a.dv, es, "dv", any, dev)) != SW_OK) return st;
-  if ((st = check_ptr(a.dg, 4, "dg", any || a.g_head, dev)) != SW_OK) return st;
+  if ((st = check_ptr(a.dv, es, "dv", any && a.H > 0, dev)) != SW_OK) return st;
+  if ((st = check_ptr(a.dg, 4, "dg", (any || a.g_head) && a.H > 0, dev)) != SW_OK) return st;
   if ((st = check_ptr(a.dh0, 4, "dh0", false, dev)) != SW_OK) return st;
   Span outs[] = {{a.dq, (size_t)(T * a.Hk * a.K) * es, "dq"},
                  {a.dk, (size_t)(T * a.Hk * a.K) * es, "dk"},

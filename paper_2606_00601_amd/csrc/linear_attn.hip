@@ -290,7 +290,8 @@ __global__ __launch_bounds__(256) void share_kernel(ShareArgs a) {
 // Zeros at the steps of a packed row that no sequence covers (a row padded to a
 // fixed length): before cu[0] and from cu[nseq] on, `per[i]` units of `unit` bytes a
 // step of each output.  The range is known on the device only, so the launch is made
-// for every packed call; where all steps are covered it ends at once.
+// for every packed call; where all steps are covered it ends at once.  cu == NULL:
+// all L steps.
 struct ClearArgs {
   void* out[4];
   int64_t per[4];
@@ -305,7 +306,8 @@ __device__ __forceinline__ void clear_units(void* out, int64_t first, int64_t en
     p[i] = U{};
 }
 __global__ __launch_bounds__(256) void clear_kernel(ClearArgs a) {
-  const int64_t c0 = cu_at(a.cu, 0, a.L), cn = cu_at(a.cu, a.nseq, a.L);
+  const int64_t c0 = a.cu ? cu_at(a.cu, 0, a.L) : a.L;
+  const int64_t cn = a.cu ? cu_at(a.cu, a.nseq, a.L) : a.L;
   const int64_t per = a.per[blockIdx.y];
   const int unit = a.unit[blockIdx.y];
   void* const out = a.out[blockIdx.y];
@@ -537,9 +539,9 @@ void add_clear(ClearArgs& c, int* n, void* out, int64_t row) {
 }
 
 int launch_clear(const LinAttnArgs& a, ClearArgs& c, int n, hipStream_t s) {
-  c.cu = a.cu;
+  c.cu = a.H > 0 ? a.cu : nullptr;
   c.nseq = a.nseq;
-  c.L = a.L;
+  c.L = a.H > 0 ? a.L : a.B * a.L;
   hipLaunchKernelGGL(clear_kernel, dim3(256, (unsigned)n), dim3(256), 0, s, c);
   return check_launch("clear_kernel");
 }
@@ -638,6 +640,12 @@ int linear_attn_fwd(const LinAttnArgs& a) {
 int linear_attn_bwd(const LinAttnArgs& a) {
   int cus, st;
   if ((st = device_cus(&cus)) != SW_OK) return st;
+  ClearArgs c{};
+  int n = 0;
+  const int64_t es = a.bf16 ? 2 : 4;
+  add_clear(c, &n, a.dq, a.Hk * a.K * es);
+  add_clear(c, &n, a.dk, a.Hk * a.K * es);
+  if (a.H == 0) return launch_clear(a, c, n, current_stream());
   const Plan p = make_plan(a, true, cus);
   if ((st = check_grid(a, p, true)) != SW_OK) return st;
   const Layout l = make_layout(a, p, true, false);
@@ -766,11 +774,6 @@ int linear_attn_bwd(const LinAttnArgs& a) {
     if ((st = check_launch("share_kernel")) != SW_OK) return st;
   }
   if (!a.cu || a.L == 0) return SW_OK;
-  ClearArgs c{};
-  int n = 0;
-  const int64_t es = a.bf16 ? 2 : 4;
-  add_clear(c, &n, a.dq, a.Hk * a.K * es);
-  add_clear(c, &n, a.dk, a.Hk * a.K * es);
   add_clear(c, &n, a.dv, a.H * a.V * es);
   if (!a.g_head) add_clear(c, &n, a.dg, a.H * 4);
   return launch_clear(a, c, n, s);

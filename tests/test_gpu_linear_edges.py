@@ -1,5 +1,5 @@
 """Linear attention at the edges of its contract: rows of packed sequences padded to a
-fixed length."""
+fixed length; no heads."""
 import numpy as np
 import pytest
 
@@ -95,3 +95,20 @@ def test_padded_row_through_autograd(sw):
     long, short = grad(L), grad(e)
     assert torch.isfinite(long).all()
     assert torch.allclose(long, short, rtol=0, atol=1e-4 * short.abs().max().item())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_no_heads(sw, dtype, packed):
+    """q's and k's are sums over no heads."""
+    B, L, Hk, K = (1, 50, 2, 24) if packed else (3, 50, 2, 24)
+    t = _rand(3, dtype, q=(B, L, Hk, K), k=(B, L, Hk, K))
+    v = t["q"].new_empty(B, L, 0, 16)
+    c = torch.tensor([0, 20, 50], dtype=torch.int32, device="cuda") if packed else None
+    for g in (torch.empty(B, L, 0, device="cuda"), torch.empty(0, device="cuda")):
+        _poison()
+        o, h = sw.linear_attn_fwd(t["q"], t["k"], v, g, cu_seqlens=c)
+        assert o.shape == v.shape and h.numel() == 0
+        r = sw.linear_attn_bwd(t["q"], t["k"], v, g, v, cu_seqlens=c)
+        assert (r["dq"] == 0).all() and (r["dk"] == 0).all() and r["dq"].shape == t["q"].shape
+        assert r["dv"].shape == v.shape and r["dg"].shape == g.shape
