@@ -546,16 +546,21 @@ int launch_clear(const LinAttnArgs& a, ClearArgs& c, int n, hipStream_t s) {
   return check_launch("clear_kernel");
 }
 
+// Every launch of the call keeps within the limit.
 int check_grid(const LinAttnArgs& a, const Plan& p, bool bwd) {
-  const int64_t tiles = p.tiles_k > p.tiles_v ? p.tiles_k : p.tiles_v;
-  const int64_t blocks = (a.K * a.V + 1023) / 1024;
-  int64_t n = p.slots > a.nseq ? p.slots : a.nseq;
-  if (bwd && p.aslots > n) n = p.aslots;
-  int64_t most;
-  if (__builtin_mul_overflow(n, a.H * 2 * (tiles > blocks ? tiles : blocks), &most) ||
-      most > SW_MAX_WGS)
-    return fail(SW_ERR_UNSUPPORTED, "%lld segments of %lld heads exceed the launch limit",
-                (long long)n, (long long)a.H);
+  const int64_t jobs = bwd ? 2 : 1, blocks = (a.K * a.V + 1023) / 1024;
+  const int64_t grids[][2] = {
+      {p.slots * a.H, p.tiles_v},                            // o, or dv
+      {p.slots * a.H, bwd ? jobs * p.tiles_k : 0},           // dq and dk, and their carries
+      {p.cut ? a.nseq * a.H : 0, jobs * blocks},             // the composition
+      {bwd ? (p.aslots + a.nseq) * a.H : 0, 1},              // dg
+  };
+  for (const auto& g : grids) {
+    int64_t n;
+    if (__builtin_mul_overflow(g[0], g[1], &n) || n > SW_MAX_WGS)
+      return fail(SW_ERR_UNSUPPORTED, "%lld segments of %lld heads exceed the launch limit",
+                  (long long)p.slots, (long long)a.H);
+  }
   return SW_OK;
 }
 

@@ -1,5 +1,5 @@
 """Linear attention at the edges of its contract: rows of packed sequences padded to a
-fixed length; no heads."""
+fixed length; no heads; many sequences."""
 import numpy as np
 import pytest
 
@@ -100,7 +100,7 @@ def test_padded_row_through_autograd(sw):
 @pytest.mark.parametrize("packed", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gradients_of_no_heads(sw, dtype, packed):
-    """q's and k's are sums over no heads."""
+    """q's and k's are sums over no heads; many sequences."""
     B, L, Hk, K = (1, 50, 2, 24) if packed else (3, 50, 2, 24)
     t = _rand(3, dtype, q=(B, L, Hk, K), k=(B, L, Hk, K))
     v = t["q"].new_empty(B, L, 0, 16)
@@ -112,3 +112,15 @@ def test_gradients_of_no_heads(sw, dtype, packed):
         r = sw.linear_attn_bwd(t["q"], t["k"], v, g, v, cu_seqlens=c)
         assert (r["dq"] == 0).all() and (r["dk"] == 0).all() and r["dq"].shape == t["q"].shape
         assert r["dv"].shape == v.shape and r["dg"].shape == g.shape
+
+
+def test_many_short_sequences_of_wide_heads(sw):
+    """Each launch is held to the limit by its own workgroups: 2^17 sequences of one step
+    with K = V = 256 take 2^19."""
+    B, K = 2 ** 17, 256
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn(B, 1, 1, K, generator=gen, device="cuda").bfloat16() for _ in range(3))
+    o, _ = sw.linear_attn_fwd(q, k, v, torch.zeros(B, 1, 1, device="cuda"), want_h_last=False)
+    want = (q.float() * k.float()).sum(-1, keepdim=True) * K ** -0.5 * v.float()
+    # q.k and the result are rounded to bf16; the sums of q.k to fp32
+    assert ((o.float() - want).abs() <= 2.0 ** -7 * want.abs() + 1e-6 * v.abs()).all()
