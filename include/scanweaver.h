@@ -495,10 +495,15 @@ int64_t sw_linear_attn_fwd_workspace(int64_t B, int64_t L, int64_t Hk, int64_t H
  *   dh_last : (nseq, H, K, V) fp32 or NULL (zero)
  *   dq, dk, dv : dense, of dtype, rounded once from fp32;  dg : (B, L, H) fp32, or
  *   (H) with SW_LINEAR_G_HEAD;  dh0 : (nseq, H, K, V) fp32 or NULL
- * The gradients of q and k feed dg, so their operands keep fp32 accuracy; dv is
- * rounded as o is.  An infinity or NaN reaches the steps that it reaches through
- * these sums.  Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
- * Otherwise as sw_linear_attn_fwd.
+ * The states in dq, dk and dg keep fp32 accuracy; dv is rounded as o is.  dg is a
+ * sum of products of steps before t with steps from t on, without a difference, so
+ * that it keeps its digits where a step forgets nearly everything; it is zero where
+ * g < -104.  An infinity or NaN reaches the steps that it reaches through these sums.
+ * Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
+ * The workspace holds a state of each head for every 64 steps (32 for fp32 inputs):
+ * 4 H K V / 64 bytes a step, 2.7 GB at L = 65536, H = 40, K = V = 128; and fp32
+ * gradients of q and k for every head where heads share them.  Otherwise as
+ * sw_linear_attn_fwd.
  */
 int sw_linear_attn_bwd(const void* q, const void* k, const void* v, const float* g,
                        const float* h0, const int32_t* cu_seqlens, const void* dout,

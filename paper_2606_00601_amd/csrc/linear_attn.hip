@@ -99,154 +99,20 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// Steps of an interval of dg.  A head's gradient is the sum over its steps, which
-// may cancel where theirs do not, so its intervals are shorter: in 256 steps its error
-// came to 2.7e-6 of it where fp32 sums have 6e-7 (2 x 1501 steps of 4 heads,
-// K = V = 64), in 64 to 5.1e-7, for 15 us more of 275 (B=4 L=1501 H=32 K=V=64).
-constexpr int STEP_ANCHOR = 256, HEAD_ANCHOR = 64;
-
-// dg, in intervals of `anchor` steps s .. e-1 of one head: with r = q . dq and
-// c = k . dk,
-//   dg_t = dg_e + sum_{t <= i < e} (r_i - c_i),   dg_t = e^{g_t} <dS_t, S_{t-1}>,
-// the products of the states taken at the intervals' ends only (at a sequence's
-// <dh_last, h_last> and <dh0, h0>).  The difference telescopes, but r and c are
-// rounded apart, so the sum walks away from dg_s by the time it gets there: what it
-// misses there is spread evenly over the interval.  That halves the error of the
-// interval's sum (of independent ones, 1/12 of the variance's A^3 and not 1/3).  fp64
-// throughout.
-struct DgArgs {
-  const float *rdots, *cdots;  // [tile][H][B * L]
-  int tiles;
-  const float* g;
-  int64_t g_sb, g_sl, g_sh;
-  const int32_t* cu;
-  const float *S, *dS, *h0, *dh0, *dh_last;
-  double *ends, *starts;  // (slots, H), (nseq, H): dg_e, dg_s; NULL: all zero
-  float* dg;              // (B, L, H), or NULL
-  double* by_slot;        // (slots, H): sums over the interval, or NULL
-  int64_t B, L, nseq, H, KV, per_seq, slots;
-  int anchor;
-};
-
-// The states' products: workgroups (slot, h), then (sequence, h).
-__global__ __launch_bounds__(256) void ends_kernel(DgArgs a) {
-  __shared__ double part[4];
-  const int tid = threadIdx.x;
-  const int64_t h = blockIdx.x % a.H;
-  int64_t slot = blockIdx.x / a.H;
-  const float *s = nullptr, *d = nullptr;
-  double* out;
-  double mul = 1.0;
-  if (slot < a.slots) {
-    const Place pl = place_of(a.cu, slot, a.anchor, a.per_seq, a.nseq, a.L);
-    if (!pl.valid) return;
-    const int64_t t1 = (pl.part + 1) * a.anchor;
-    s = a.S + (slot * a.H + h) * a.KV;
-    if (t1 < pl.len) {
-      d = a.dS + (slot * a.H + h) * a.KV;
-      const int64_t b = a.cu ? 0 : pl.n;
-      mul = exp((double)clamp_g(a.g[b * a.g_sb + (pl.first + t1) * a.g_sl + h * a.g_sh]));
-    } else if (a.dh_last && pl.len > 0) {
-      d = a.dh_last + (pl.n * a.H + h) * a.KV;
-    }
-    out = a.ends + slot * a.H + h;
-  } else {
-    slot -= a.slots;
-    if (a.h0) {
-      s = a.h0 + (slot * a.H + h) * a.KV;
-      d = a.dh0 + (slot * a.H + h) * a.KV;
-    }
-    out = a.starts + slot * a.H + h;
-  }
-  double dot = 0.0;
-  if (d) {
-    int64_t e = 4 * tid;
-    if (a.KV % 4 == 0 && ((uintptr_t)s | (uintptr_t)d) % 16 == 0)
-#pragma unroll 4
-      for (; e < a.KV; e += 1024) {
-        const f4 x = *reinterpret_cast<const f4*>(s + e), y = *reinterpret_cast<const f4*>(d + e);
-        dot += ((double)x[0] * y[0] + (double)x[1] * y[1]) + ((double)x[2] * y[2] + (double)x[3] * y[3]);
-      }
-    else
-      for (e = tid; e < a.KV; e += 256) dot += (double)s[e] * d[e];
-  }
-  dot = wave_sum(dot);
-  if ((tid & 63) == 0) part[tid >> 6] = dot;
-  __syncthreads();
-  if (tid == 0) *out = mul * (part[0] + part[1] + part[2] + part[3]);
-}
-
-// v summed over this lane and the later (LATER) or the earlier ones; whole: over the wave.
-template <bool LATER>
-__device__ __forceinline__ double wave_scan(double v, int lane) {
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const double o = LATER ? __shfl_down(v, k) : __shfl_up(v, k);
-    if (LATER ? lane + k < 64 : lane >= k) v += o;
-  }
-  return v;
-}
-
-// A workgroup of `anchor` threads for each interval and head.
-__global__ __launch_bounds__(STEP_ANCHOR) void dg_kernel(DgArgs a) {
-  __shared__ double whole[STEP_ANCHOR / 64], sums[STEP_ANCHOR / 64];
-  const int waves = a.anchor / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t slot = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  const Place pl = place_of(a.cu, slot, a.anchor, a.per_seq, a.nseq, a.L);
-  if (!pl.valid || pl.len == 0) {
-    if (a.by_slot && tid == 0) a.by_slot[slot * a.H + h] = 0.0;
-    return;
-  }
-  const int64_t b = a.cu ? 0 : pl.n;
-  const int64_t t0 = pl.part * a.anchor, n = pl.len - t0 < a.anchor ? pl.len - t0 : a.anchor;
-  const int64_t at = b * a.L + pl.first + t0 + tid;
-  double x = 0.0, end = 0.0, start = 0.0, g = 0.0;
-  if (tid < n) {
-    for (int q = 0; q < a.tiles; ++q) {
-      const int64_t i = ((int64_t)q * a.H + h) * (a.B * a.L) + at;
-      x += (double)a.rdots[i] - a.cdots[i];
-    }
-    g = a.g[b * a.g_sb + (pl.first + t0 + tid) * a.g_sl + h * a.g_sh];
-  }
-  if (a.ends) {
-    end = a.ends[slot * a.H + h];
-    start = pl.part ? a.ends[(slot - 1) * a.H + h] : a.starts[pl.n * a.H + h];
-  }
-  const double suf = wave_scan<true>(x, lane);
-  if (lane == 0) whole[wave] = suf;
-  __syncthreads();
-  double all = 0.0, v = suf + end;
-  for (int q = 0; q < waves; ++q) {
-    all += whole[q];
-    if (q > wave) v += whole[q];
-  }
-  const double miss = start - (end + all);
-  if (miss - miss == 0.0) {
-    v += miss * ((double)(n - tid) / (double)n);
-  } else {
-    // A value that is not finite: from the end down to it, and from the start up to
-    // it, so that it reaches the steps it reaches in the recurrence.
-    double pre = start - (wave_scan<false>(x, lane) - x);
-    for (int q = 0; q < wave; ++q) pre -= whole[q];
-    if (!(v - v == 0.0)) v = pre;
-  }
-  // where e^g is held at zero its derivative is zero too
-  if (tid >= n || g < G_MIN) v = 0.0;
-  if (a.dg && tid < n) a.dg[at * a.H + h] = (float)v;
-  if (a.by_slot) {
-    v = wave_sum(v);
-    if (lane == 0) sums[wave] = v;
-    __syncthreads();
-    if (tid == 0) {
-      double t = 0.0;
-      for (int q = 0; q < waves; ++q) t += sums[q];
-      a.by_slot[slot * a.H + h] = t;
-    }
+// dg where a head's columns of q and k are several tiles: each tile's share (tile, H,
+// B L) added up in order, to (B, L, H).
+__global__ __launch_bounds__(256) void dg_tiles_kernel(const float* share, float* dg, int tiles,
+                                                       int64_t H, int64_t T) {
+  const int64_t n = H * T;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+    double v = 0.0;
+    for (int q = 0; q < tiles; ++q) v += share[q * n + i];
+    const int64_t h = i / T;
+    dg[(i - h * T) * H + h] = (float)v;
   }
 }
 
-// The gradient of a decay per head: the intervals' sums, in a fixed order.
+// The gradient of a decay per head: the sums of segments and tiles, in a fixed order.
 __global__ __launch_bounds__(64) void dg_head_kernel(const double* by_slot, float* dg,
                                                      int64_t slots, int64_t H) {
   const int64_t h = blockIdx.x;
@@ -330,8 +196,7 @@ struct Plan {
   int64_t lseg = CHUNK, per_seq = 1, slots = 0;  // segments
   bool cut = false;                // some sequence may have several
   Mode out = OUT;                  // how the output (or dv) is rounded
-  int anchor = STEP_ANCHOR;        // dg's intervals
-  int64_t aper = 1, aslots = 0;
+  int64_t kept = 0;                // chunk ends inside sequences: dS is kept there for dg
 };
 
 // What a chunk of a walk takes, in units of one alone, where `wgs` workgroups are
@@ -376,8 +241,8 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
     const double len = (double)((chunks + n - 1) / n) + (a.bf16 ? 2.0 : 1.0);
     double us;
     if (bwd) {
-      const double two = pace(rows * n * 2 * p.tiles_k, cus, a.V, p.nt_k, a.bf16);
-      us = len * (two * (9.5 + (n > 1 ? 3.0 : 0.0)) +
+      us = len * ((n > 1 ? 3.0 * pace(rows * n * 2 * p.tiles_k, cus, a.V, p.nt_k, a.bf16) : 0.0) +
+                  18.0 * pace(rows * n * p.tiles_k, cus, a.V, p.nt_k, a.bf16) +
                   5.5 * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16));
     } else {
       us = len * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16) * (n > 1 ? 8.5 : 5.5);
@@ -394,20 +259,18 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   p.cut = lseg < longest;
   p.per_seq = longest > 0 ? (longest + lseg - 1) / lseg : 1;
   p.slots = a.cu ? a.L / lseg + a.nseq : a.B * p.per_seq;
-  p.anchor = a.g_head ? HEAD_ANCHOR : STEP_ANCHOR;
-  p.aper = longest > 0 ? (longest + p.anchor - 1) / p.anchor : 1;
-  p.aslots = a.cu ? a.L / p.anchor + a.nseq : a.B * p.aper;
+  const int64_t step = a.bf16 ? Bf16::C : F32::C;
+  p.kept = !bwd || a.L == 0 ? 0 : a.cu ? a.L / step : a.B * ((a.L - 1) / step);
   return p;
 }
 
 // The workspace's parts, in bytes from its start; every one 256-byte aligned.
 struct Layout {
-  size_t carry[2] = {0, 0}, decay[2] = {0, 0}, S = 0, dS = 0, rdots = 0, cdots = 0, dq = 0, dk = 0,
-         dh0 = 0, ends = 0, starts = 0, by_slot = 0, bytes = 0;
+  size_t carry[2] = {0, 0}, decay[2] = {0, 0}, kept = 0, sums = 0, share = 0, dq = 0, dk = 0,
+         by_slot = 0, bytes = 0;
 };
 
-// What a call of these sizes may need with every optional operand (`all`), or does.
-Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool all) {
+Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd) {
   Layout l;
   auto take = [&](size_t n) {
     const size_t at = l.bytes;
@@ -421,18 +284,15 @@ Layout make_layout(const LinAttnArgs& a, const Plan& p, bool bwd, bool all) {
       l.decay[i] = take((size_t)(p.slots * a.H) * 4);
     }
   if (bwd) {
-    if (a.L > p.anchor || a.dh_last || all) l.S = take((size_t)p.aslots * HKV * 4);
-    if (a.L > p.anchor) l.dS = take((size_t)p.aslots * HKV * 4);
-    if ((a.h0 && !a.dh0) || all) l.dh0 = take((size_t)a.nseq * HKV * 4);
-    l.ends = take((size_t)(p.aslots * a.H) * 8);
-    l.starts = take((size_t)(a.nseq * a.H) * 8);
-    l.rdots = take((size_t)(p.tiles_k * a.H) * T * 4);
-    l.cdots = take((size_t)(p.tiles_k * a.H) * T * 4);
+    const size_t rows = (size_t)(p.tiles_k * a.H) * T * 4;
+    l.kept = take((size_t)p.kept * HKV * 4);
+    l.sums = take(rows);
+    if (p.tiles_k > 1 && !a.g_head) l.share = take(rows);
     if (a.H != a.Hk) {
       l.dq = take(T * (size_t)(a.H * a.K) * 4);
       l.dk = take(T * (size_t)(a.H * a.K) * 4);
     }
-    if (a.g_head) l.by_slot = take((size_t)(p.aslots * a.H) * 8);
+    if (a.g_head) l.by_slot = take((size_t)(p.slots * p.tiles_k * a.H) * 8);
   }
   return l;
 }
@@ -460,7 +320,6 @@ WalkArgs walk_args(const LinAttnArgs& a, const Plan& p) {
   w.lseg = p.lseg;
   w.per_seq = p.per_seq;
   w.slots = p.slots;
-  w.anchor = p.anchor;
   w.njobs = 1;
   return w;
 }
@@ -551,9 +410,8 @@ int check_grid(const LinAttnArgs& a, const Plan& p, bool bwd) {
   const int64_t jobs = bwd ? 2 : 1, blocks = (a.K * a.V + 1023) / 1024;
   const int64_t grids[][2] = {
       {p.slots * a.H, p.tiles_v},                            // o, or dv
-      {p.slots * a.H, bwd ? jobs * p.tiles_k : 0},           // dq and dk, and their carries
+      {p.slots * a.H, bwd ? jobs * p.tiles_k : 0},           // dq and dk's carries
       {p.cut ? a.nseq * a.H : 0, jobs * blocks},             // the composition
-      {bwd ? (p.aslots + a.nseq) * a.H : 0, 1},              // dg
   };
   for (const auto& g : grids) {
     int64_t n;
@@ -599,13 +457,13 @@ using namespace lin;
 int64_t linear_attn_fwd_workspace(const LinAttnArgs& a) {
   int cus;
   if (device_cus(&cus) != SW_OK) return 0;
-  return (int64_t)make_layout(a, make_plan(a, false, cus), false, false).bytes;
+  return (int64_t)make_layout(a, make_plan(a, false, cus), false).bytes;
 }
 
 int64_t linear_attn_bwd_workspace(const LinAttnArgs& a) {
   int cus;
   if (device_cus(&cus) != SW_OK) return 0;
-  return (int64_t)make_layout(a, make_plan(a, true, cus), true, true).bytes;
+  return (int64_t)make_layout(a, make_plan(a, true, cus), true).bytes;
 }
 
 int linear_attn_fwd(const LinAttnArgs& a) {
@@ -613,7 +471,7 @@ int linear_attn_fwd(const LinAttnArgs& a) {
   if ((st = device_cus(&cus)) != SW_OK) return st;
   const Plan p = make_plan(a, false, cus);
   if ((st = check_grid(a, p, false)) != SW_OK) return st;
-  const Layout l = make_layout(a, p, false, false);
+  const Layout l = make_layout(a, p, false);
   const hipStream_t s = current_stream();
   Workspace ws(s);
   if ((st = ws.get(a, l.bytes, "sw_linear_attn_fwd")) != SW_OK) return st;
@@ -653,7 +511,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   if (a.H == 0) return launch_clear(a, c, n, current_stream());
   const Plan p = make_plan(a, true, cus);
   if ((st = check_grid(a, p, true)) != SW_OK) return st;
-  const Layout l = make_layout(a, p, true, false);
+  const Layout l = make_layout(a, p, true);
   const hipStream_t s = current_stream();
   Workspace ws(s);
   if ((st = ws.get(a, l.bytes, "sw_linear_attn_bwd")) != SW_OK) return st;
@@ -676,7 +534,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   jv.wscale = a.scale;
   jv.rscale = jv.neg ? -1.0f : 1.0f;
   jv.init = a.dh_last;
-  jv.last = a.dh0 ? a.dh0 : a.h0 ? at(l.dh0) : nullptr;
+  jv.last = a.dh0;
   set_out(jv, a, a.dv, a.H, a.V, !a.bf16);
   set_out(jq, a, shared ? at(l.dq) : a.dq, a.H, a.K, shared || !a.bf16);
   set_out(jk, a, shared ? at(l.dk) : a.dk, a.H, a.K, shared || !a.bf16);
@@ -694,67 +552,49 @@ int linear_attn_bwd(const LinAttnArgs& a) {
     f.job[1] = {jk.carry, jk.decay, a.dh_last, true};
     if ((st = launch_fold(a, p, f, 2, s)) != SW_OK) return st;
   }
-  // dq and dk: their products with q and k are the decays' gradient
-  jq.A = a.q;
-  jq.adiv = r;
-  jq.avec = rows_vec(a.q, a.K, a.bf16);
-  jq.dots = at(l.rdots);
+  // dk, then dq, and their parts of dg
   jk.A = a.k;
   jk.adiv = r;
   jk.avec = rows_vec(a.k, a.K, a.bf16);
-  jk.dots = at(l.cdots);
-  if (a.L > p.anchor || a.dh_last) jq.anchors = at(l.S);
-  jq.last_anchor = a.dh_last != nullptr;
-  if (a.L > p.anchor) jk.anchors = at(l.dS);
-  w.job[0] = jq;
-  w.job[1] = jk;
-  w.njobs = 2;
-  if ((st = launch_walk_any(a, w, GRAD, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
-  w.job[0] = jv;
+  jk.sums = jq.sums = at(l.sums);
+  jk.kept = jq.kept = at(l.kept);
+  jq.A = a.q;
+  jq.adiv = r;
+  jq.avec = rows_vec(a.q, a.K, a.bf16);
+  jq.dlast = a.dh_last;
+  jq.dvec = (uintptr_t)a.dh_last % 16 == 0;
+  if (a.g_head) {
+    jq.by_slot = (double*)at(l.by_slot);
+  } else if (p.tiles_k == 1) {
+    jq.dg = a.dg;
+    jq.dg_st = a.H;
+    jq.dg_sh = 1;
+  } else {
+    jq.dg = at(l.share);
+    jq.dg_st = 1;
+    jq.dg_sh = a.B * a.L;
+    jq.dg_sq = a.H * jq.dg_sh;
+  }
   w.njobs = 1;
+  w.job[0] = jk;
+  if ((st = launch_walk_any(a, w, GRAD_K, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
+  w.job[0] = jq;
+  if ((st = launch_walk_any(a, w, GRAD_Q, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
+  w.job[0] = jv;
   if ((st = launch_walk_any(a, w, p.out, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
 
-  DgArgs d{};
-  d.rdots = at(l.rdots);
-  d.cdots = at(l.cdots);
-  d.tiles = (int)p.tiles_k;
-  d.g = a.g;
-  d.g_sb = w.g_sb;
-  d.g_sl = w.g_sl;
-  d.g_sh = w.g_sh;
-  d.cu = a.cu;
-  d.S = at(l.S);
-  d.dS = at(l.dS);
-  d.h0 = a.h0;
-  d.dh0 = jv.last;
-  d.dh_last = a.dh_last;
-  const bool ends = a.L > p.anchor || a.h0 || a.dh_last;
-  d.ends = ends ? (double*)at(l.ends) : nullptr;
-  d.starts = (double*)at(l.starts);
-  d.dg = a.g_head ? nullptr : a.dg;
-  d.by_slot = a.g_head ? (double*)at(l.by_slot) : nullptr;
-  d.B = a.B;
-  d.L = a.L;
-  d.nseq = a.nseq;
-  d.H = a.H;
-  d.KV = a.K * a.V;
-  d.per_seq = p.aper;
-  d.slots = p.aslots;
-  d.anchor = p.anchor;
-  if (ends) {
-    hipLaunchKernelGGL(ends_kernel, dim3((unsigned)((p.aslots + a.nseq) * a.H)), dim3(256), 0, s, d);
-    if ((st = check_launch("ends_kernel")) != SW_OK) return st;
-  }
-  if (p.aslots > 0) {
-    hipLaunchKernelGGL(dg_kernel, dim3((unsigned)(p.aslots * a.H)), dim3((unsigned)p.anchor), 0, s, d);
-    if ((st = check_launch("dg_kernel")) != SW_OK) return st;
-  }
+  const int64_t T = a.B * a.L;
   if (a.g_head) {
-    hipLaunchKernelGGL(dg_head_kernel, dim3((unsigned)a.H), dim3(64), 0, s, d.by_slot, a.dg, p.aslots,
-                       a.H);
+    hipLaunchKernelGGL(dg_head_kernel, dim3((unsigned)a.H), dim3(64), 0, s, jq.by_slot, a.dg,
+                       p.slots * p.tiles_k, a.H);
     if ((st = check_launch("dg_head_kernel")) != SW_OK) return st;
+  } else if (p.tiles_k > 1 && T > 0) {
+    const int64_t wgs = (T * a.H + 255) / 256 < 4096 ? (T * a.H + 255) / 256 : 4096;
+    hipLaunchKernelGGL(dg_tiles_kernel, dim3((unsigned)wgs), dim3(256), 0, s, jq.dg, a.dg,
+                       (int)p.tiles_k, a.H, T);
+    if ((st = check_launch("dg_tiles_kernel")) != SW_OK) return st;
   }
-  const int64_t groups = a.B * a.L * a.Hk;
+  const int64_t groups = T * a.Hk;
   if (shared && groups > 0) {
     ShareArgs h{};
     h.part[0] = at(l.dq);

@@ -23,10 +23,11 @@
 //
 // Rounding (bf16): products of inputs are exact in fp32 accumulators.  The
 // weighted Z is split in three bf16 parts whose sum is the fp32 value, so S
-// keeps fp32 accuracy whatever the number of chunks.  For an output in bf16
-// (NS = 1), P and S are rounded to bf16 once as operands; for outputs whose
-// products with an input feed an fp32 gradient, and for outputs of few steps
-// (NS = 3), both are split in three.  fp32 inputs run on the fp32 matrix instructions throughout.
+// keeps fp32 accuracy whatever the number of chunks.  For an output in bf16, P
+// and S are rounded to bf16 once as operands (NS = NP = 1); for outputs of few
+// steps both are split in three.  For dq and dk S is split in three, since its
+// products make dg too, and P in two: 2^-17 of the weights beside the result's
+// own rounding of 2^-9.  fp32 inputs run on the fp32 matrix instructions throughout.
 #pragma once
 
 #include "linear_attn.h"
@@ -38,7 +39,7 @@ constexpr int CHUNK = 64;      // steps between the places where walks may start
 constexpr float G_MIN = -104.0f;  // e^g is zero in fp32 here: the lowest that counts
 
 struct Job {
-  HeadRows X, Y, Z, A;   // A: the input whose products with out are summed (dots)
+  HeadRows X, Y, Z, A;   // A: in the gradients' walks the input of which out is the gradient
   int xdiv, ydiv, zdiv, adiv;  // head h reads head h / div
   bool xvec, yvec, zvec, avec;  // rows are 16-byte aligned whole vectors
   bool ovec, orows;             // out's rows: whole fours of columns; and 16-byte granules
@@ -46,13 +47,18 @@ struct Job {
   int64_t ob, ol, oh;
   bool out_f32;
   bool reverse;
-  float* dots;           // [tile][H][B * L] or NULL
   const float* init;     // (sequences, H, K, V): the state before the first step, or NULL
   float* last;           // the state after the last step, or NULL
   float* carry;          // (slots, H, K, V): carries written, or initial states read, or NULL
   float* decay;          // (slots, H): the segments' decays (written with the carries)
-  float* anchors;        // (anchor slots, H, K, V) or NULL
-  bool last_anchor;      // the state after the last step is an anchor too
+  // dg: dk's walk writes its rows' sums and its states between chunks, dq's reads them
+  float* sums;           // [tile][H][B * L]
+  float* kept;           // (chunk ends inside sequences, H, K, V)
+  const float* dlast;    // (sequences, H, K, V): the state after the last step, or NULL
+  bool dvec;             // its rows are whole aligned fours
+  float* dg;             // dg of step i, head h and tile q at dg[i dg_st + h dg_sh + q dg_sq], or NULL
+  int64_t dg_st, dg_sh, dg_sq;
+  double* by_slot;       // (slots, tiles, H): dg's sums over the segment's steps, or NULL
   int64_t skk, svv;      // where state element (Y's column, Z's column) lies in (K, V)
   // scales of P (its absolute value and log2), of the state's increments and of the
   // read-out; neg: out changes its sign
@@ -73,7 +79,6 @@ struct WalkArgs {
   int64_t per_seq;       // segments of a sequence (cu == NULL)
   int64_t slots;
   int tiles, njobs;
-  int anchor;            // steps between the states kept for dg, a multiple of CHUNK
 };
 
 // Where slot `slot` of width `w` steps lies: packed sequence n's slots start at
@@ -113,11 +118,6 @@ __device__ __forceinline__ Place place_of(const int32_t* cu, int64_t slot, int64
   return p;
 }
 
-__device__ __forceinline__ int64_t first_slot(const Place& p, const int32_t* cu, int64_t w,
-                                              int64_t per_seq) {
-  return cu ? p.first / w + p.n : p.n * per_seq;
-}
-
 // e^g of a decay as the walks use it.
 __device__ __forceinline__ float clamp_g(float g) { return g < G_MIN ? G_MIN : g; }
 
@@ -144,6 +144,15 @@ __device__ __forceinline__ double wave_running_sum(double v, double* all) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), 63);
   *all = __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+  return v;
+}
+
+// The sum over the 16 lanes of a lane's row, on each of them.
+__device__ __forceinline__ float row_sum16(float v) {
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x124, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x122, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x121, 0xf, 0xf, false));
   return v;
 }
 
@@ -218,6 +227,29 @@ __device__ __forceinline__ Frag<F32> row_frag(const float* t) {
   *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(t);
   *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(t + 4);
   return f;
+}
+// The same of a row in memory, `left` columns of it from p on (vec: whole 16-byte granules).
+__device__ __forceinline__ void load_frag(Frag<Bf16>& f, const uint16_t* p, int left, bool vec) {
+  f.v = s8{0, 0, 0, 0, 0, 0, 0, 0};
+  if (vec) {
+    if (left > 0) f.v = *reinterpret_cast<const s8*>(p);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) f.v[j] = (short)p[j];
+  }
+}
+__device__ __forceinline__ void load_frag(Frag<F32>& f, const float* p, int left, bool vec) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j] = 0.0f;
+  if (vec) {
+    if (left > 0) *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(p);
+    if (left > 4) *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(p + 4);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) f.v[j] = p[j];
+  }
 }
 // X's fragment in the order of Y's.
 __device__ __forceinline__ Frag<Bf16> as_y(const Frag<Bf16>& f, int g) {
@@ -398,22 +430,40 @@ struct Tile {
   }
 };
 
-// What a walk is for: the segments' carries; an output; an output whose
-// products with an input are summed by step (with the states kept for dg); a
-// bf16 output rounded once, at its end.
-enum Mode { CARRY, OUT, GRAD, OUT_ONCE };
+// What a walk is for: the segments' carries; an output; a bf16 output rounded once,
+// at its end; dk, and dq, with their parts of dg.
+//
+// dg_t = e^{g_t} <dS_t, S_{t-1}> is the sum over the pairs of a step s < t and a step
+// t' >= t of scale (q_t' . k_s) (do_t' . v_s) e^{G_t' - G_s} (and h0's and dh_last's
+// with them).  A difference of what q . dq and k . dk sum to is shorter, but keeps
+// only the digits of its largest terms: where a step forgets much, dg_t is far
+// smaller than they are (at decays of e^-16 nothing of it was left).  So the pairs are
+// added up as they are, those of one chunk and head as
+//   dg_t = D + sum_{t' >= t} a_t' + sum_{s < t} b_s + sum_{t' >= t, s < t} M_t's
+//   M_t's = P_t's (q_t' . k_s)                       both steps in the chunk
+//   a_t' = q_t' . (dq's part from the state before)  s before the chunk
+//   b_s  = k_s . (dk's part from the state after)    t' after it
+//   D    = e^{G_C} <S before, dS after>              the one before, the other after
+// with no difference anywhere.  dk's walk runs first: it leaves b, and its state at
+// each chunk's end, decayed by the step after it.  dq's walk has S before each chunk
+// in its accumulators.  The states' traffic is 8 K V bytes a chunk and head; keeping
+// both and multiplying them apart would be twice that.
+enum Mode { CARRY, OUT, OUT_ONCE, GRAD_K, GRAD_Q };
+constexpr bool is_grad(Mode m) { return m >= GRAD_K; }
 
 template <class T, int KP, int NT, Mode MODE>
 struct Shared {
   static constexpr int VT = 64 * NT, C = T::C;
-  static constexpr int NS = MODE >= GRAD && T::SPLIT ? 3 : 1;  // parts of P and S
+  // Parts of P and S: S makes a and b, which have fp32 accuracy
+  static constexpr int NS = MODE >= OUT_ONCE && T::SPLIT ? 3 : 1;
+  static constexpr int NP = !T::SPLIT || MODE < OUT_ONCE ? 1 : is_grad(MODE) ? 2 : 3;
   static constexpr bool XS = MODE != CARRY;
   // fp32 results take the decays between steps to fp32: their running sums in two parts
-  static constexpr bool FINE = MODE >= GRAD || !T::SPLIT;
+  static constexpr bool FINE = MODE >= OUT_ONCE || !T::SPLIT;
   typename T::E y[C * ROW<T, KP>];
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
-  typename T::E p[XS ? NS * P_SIZE<T> : 8];
+  typename T::E p[XS ? NP * P_SIZE<T> : 8];
   // A chunk's decays, of this chunk and the next.
   struct Decays {
     float gs[C], gsl[FINE ? C : 4];  // by step s: the running log2 decay, high and low parts
@@ -426,7 +476,10 @@ struct Shared {
   // bf16 outputs leave as whole rows: a wave's columns are 32 or 64 bytes of each step's
   static constexpr bool ROWS = MODE == OUT && T::SPLIT;
   typename T::E o[ROWS ? C * VT : 8];  // granule c of row t at c ^ oswz(t)
-  float dots[MODE == GRAD ? 4 * C : 4];
+  float dots[is_grad(MODE) ? 4 * C : 4];       // a or b: each wave's columns' part
+  alignas(16) float pairs[MODE == GRAD_Q ? 4 * C : 4];     // by wave and step s: M summed for dg of step s + 1
+  float rows[MODE == GRAD_Q && C == 32 ? 16 : 4];  // steps 16 ..: M summed over the steps before 16
+  float ends[4];                               // <S, dS>: each wave's part
   uint32_t bad[2];                // the chunk (of odd or even number) holds what is not finite
 };
 
@@ -480,7 +533,7 @@ __device__ __forceinline__ LanePlace lane_place(int tid) {
 // fragment of X, Y and P for twice the products: with eight waves of 16 columns
 // instead, LDS reads doubled and set the pace.
 constexpr int walk_waves(int KP, int NT, Mode m) {
-  return KP >= 256 ? 1 : NT == 2 ? 2 : KP == 128 || m >= GRAD ? 2 : 4;
+  return KP >= 256 ? 1 : NT == 2 || KP == 128 ? 2 : m >= OUT_ONCE ? 3 : 4;
 }
 
 template <class T, int KP, int NT, Mode MODE, bool VEC>
@@ -488,6 +541,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   typedef typename T::E E;
   typedef Shared<T, KP, NT, MODE> Sh;
   constexpr bool XS = MODE != CARRY;
+  constexpr bool GRAD = is_grad(MODE);
   constexpr int C = T::C, KT = KP / 16, VT = 64 * NT, SB = C / 32, TT = C / 16, NS = Sh::NS;
   constexpr int THREADS = 256;
   constexpr int KR = ROW<T, KP>, VR = ROW<T, VT>, G = T::G;
@@ -503,7 +557,10 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
   const int64_t slot = w % (uint32_t)a.slots;
   const Job& job = a.job[w / (uint32_t)a.slots];
   const Place pl = place_of(a.cu, slot, a.lseg, a.per_seq, a.nseq, a.L);
-  if (!pl.valid) return;
+  if (!pl.valid) {
+    if (MODE == GRAD_Q && job.by_slot && tid == 0) job.by_slot[(slot * a.tiles + tile) * a.H + h] = 0.0;
+    return;
+  }
   const bool rev = job.reverse;
   // the last segment in the walk's order hands nothing on
   const bool final_seg = rev ? pl.part == 0 : pl.part == pl.parts - 1;
@@ -545,25 +602,26 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     each_state([&](int kt, int nt, int i, int64_t at)
                    __attribute__((always_inline)) { p[at] = S[kt][nt][i] * f; });
   };
-  // A kept state: the gradients' walks have Y's columns side by side (skk == 1).
-  auto store_anchor = [&](float* p) __attribute__((always_inline)) {
-    if (a.KK % 4) return store_state(p, 1.0f);
+  // The gradients' walks have Y's columns side by side in a state (skk == 1): fn of each
+  // accumulator's four of them, which the address is of and of which `left` are there.
+  auto each_four = [&](auto* p, auto fn) __attribute__((always_inline)) {
     int kk = 8 * g, vv = v0 + vb + r;
     asm volatile("" : "+v"(kk), "+v"(vv));
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
       if (vv + 16 * nt < a.VV) {
-        float* row = p + (int64_t)(vv + 16 * nt) * job.svv + kk;
+        auto* row = p + (int64_t)(vv + 16 * nt) * job.svv + kk;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           const int k = 32 * (kt >> 1) + 4 * (kt & 1);
-          if (kk + k < a.KK) *reinterpret_cast<f4*>(row + k) = S[kt][nt];
+          if (kk + k < a.KK) fn(kt, nt, row + k, a.KK - kk - k);
         }
       }
   };
-  auto anchor_at = [&](int64_t i) {  // the sequence's i-th
-    const int64_t per = (a.L + a.anchor - 1) / a.anchor;
-    return job.anchors + ((first_slot(pl, a.cu, a.anchor, per) + i) * a.H + h) * a.KV;
+  // dS at the end of a chunk, before the sequence's step t
+  auto kept_at = [&](int t) {
+    const int64_t base = a.cu ? pl.first / C : pl.n * ((a.L - 1) / C);
+    return job.kept + ((base + t / C - 1) * a.H + h) * a.KV;
   };
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt)
@@ -578,6 +636,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
                      __attribute__((always_inline)) { S[kt][nt][i] = p[at]; });
   }
   float seg_decay = 1.0f;
+  double dg_sum = 0.0;
 
   Tile<T, KP, THREADS, VEC> tx, ty;
   Tile<T, VT, THREADS, VEC> tz;
@@ -629,7 +688,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 
   const int64_t ob = b * job.ob + pl.first * job.ol + h * job.oh;
   const E* ap = nullptr;
-  if (MODE == GRAD)
+  if (GRAD)
     ap = (const E*)job.A.p + b * job.A.sb + pl.first * job.A.sl + h / job.adiv * job.A.sh;
 
   if (tid < 2) sh.bad[tid] = 0;
@@ -657,9 +716,200 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 
     // rows of this chunk: cnt, the first of them step tfirst, the next tstep on
     const int cnt = n, tfirst = rev ? t0 + n - 1 : t0, tstep = rev ? -1 : 1;
-    const int reached = rev ? t0 : t0 + n;  // after the chunk the state stands before this step
+    const int tend = t0 + n;  // the step after the chunk's last in time
+
+    if constexpr (MODE == GRAD_K) {
+      if (tend < len) {
+        const float g1 = dec.g1[0];  // of step tend
+        each_four(kept_at(tend), [&](int kt, int nt, float* p, int left) __attribute__((always_inline)) {
+          const f4 x = S[kt][nt] * g1;
+          if (a.KK % 4 == 0) {
+            *reinterpret_cast<f4*>(p) = x;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (i < left) p[i] = x[i];
+          }
+        });
+      }
+    }
+    // dg: what one wave adds up at the chunk's end is on its way from here on
+    float later = 0.0f, own_g = 0.0f;
+    f4 after[MODE == GRAD_Q ? KT : 1][NT];  // dS
+    if constexpr (MODE == GRAD_Q) {
+      if (wave == 1 && lane < cnt) {
+        const int64_t at = ((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst + lane;
+        if (lane > 0) later = job.sums[at - 1];
+        own_g = gp[(int64_t)(tfirst + lane) * a.g_sl];
+      }
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) after[kt][nt] = f4{0.f, 0.f, 0.f, 0.f};
+      const float* p = tend < len  ? kept_at(tend)
+                       : job.dlast ? job.dlast + (pl.n * a.H + h) * a.KV
+                                   : nullptr;
+      const bool vec = a.KK % 4 == 0 && (tend < len || job.dvec);
+      if (p)
+        each_four(p, [&](int kt, int nt, const float* q, int left) __attribute__((always_inline)) {
+          if (vec) {
+            after[kt][nt] = *reinterpret_cast<const f4*>(q);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (i < left) after[kt][nt][i] = q[i];
+          }
+        });
+    }
+
+    if (XS && (MODE == GRAD_Q || !bad)) {
+      // P^T = Y X^T: a wave has 16 steps t (columns) and of the tiles of 16 steps s
+      // (rows) those up to the diagonal's; the pair that holds it is filled with zeros
+      const LanePlace me = lane_place(tid);
+      const int g = me.g, r = me.r;
+      const int tt = wave & (TT - 1), t = tt * 16 + r;
+      const int first = C == 32 ? wave >> 1 : 0;  // its first tile of steps s
+      Frag<T> xf[KP / 32];
+      const E* const xr = sh.x + t * KR + 8 * g;
+#pragma unroll
+      for (int p = 0; p < KP / 32; ++p) xf[p] = as_y(row_frag(xr + 32 * p), g);
+      // A's row of step t, for the products of the pairs
+      Frag<T> af[MODE == GRAD_Q ? VT / 32 : 1];
+      if constexpr (MODE == GRAD_Q) {
+        const E* const ar = ap + (int64_t)(tfirst + t) * job.A.sl + v0 + 8 * g;
+#pragma unroll
+        for (int p = 0; p < VT / 32; ++p)
+          load_frag(af[p], ar + 32 * p, t < cnt ? a.VV - v0 - 8 * g - 32 * p : 0, job.avec);
+      }
+      const float gt = dec.gt[t], gtl = Sh::FINE ? dec.gtl[t] : 0.0f;
+      E* const pw = sh.p + p_row<T>(t);
+      const int m = pswz<T>(t);
+      // N tiles from `first`, the last of them the diagonal's if `diag`
+      auto weigh = [&](auto count, bool diag) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
+        f4 acc[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+        const E* const yr = sh.y + (16 * first + r) * KR + 8 * g;
+#pragma unroll
+        for (int p = 0; p < KP / 32; ++p)
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            acc[i] = mma(row_frag(yr + 16 * i * KR + 32 * p), xf[p], acc[i]);
+        float pv[4 * (N + (N & 1))];
+#pragma unroll
+        for (int i = 0; i < N + (N & 1); ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) pv[4 * i + j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          f4 d = gt - *reinterpret_cast<const f4*>(dec.gs + 16 * (first + i) + 4 * g);
+          if (Sh::FINE) d += gtl - *reinterpret_cast<const f4*>(dec.gsl + 16 * (first + i) + 4 * g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float e = acc[i][j] * __builtin_amdgcn_exp2f(d[j]);
+            pv[4 * i + j] = i == N - 1 && diag && 4 * g + j > r ? 0.0f : e;
+          }
+        }
+        if constexpr (T::SPLIT) {
+#pragma unroll
+          for (int i = 0; i < (N + 1) / 2; ++i) {  // places 32 i + 8 g .. + 7
+            Frag<T> f[Sh::NP];
+            parts_of<Sh::NP>(pv + 8 * i, f);
+#pragma unroll
+            for (int q = 0; q < Sh::NP; ++q)
+              *reinterpret_cast<s8*>(pw + q * P_SIZE<T> + ((4 * i + g) ^ m) * 8) = f[q].v;
+          }
+        } else {  // places 8 g + 4 first .. + 3
+          *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
+        }
+        if constexpr (MODE == GRAD_Q) {
+          // M: this lane's step t = t', its rows s.  Summed over s up to each, then over t'.
+          f4 kq[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) kq[i] = f4{0.f, 0.f, 0.f, 0.f};
+          const E* const zr = sh.z + (16 * first + r) * VR + 8 * g;
+#pragma unroll
+          for (int p = 0; p < VT / 32; ++p)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+              kq[i] = mma(row_frag(zr + 16 * i * VR + 32 * p), af[p], kq[i]);
+          float upto = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const bool whole = i < N - 1 || !diag;
+            f4 c;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = whole || 4 * g + j < r ? pv[4 * i + j] * kq[i][j] : 0.0f;
+              c[j] = j ? c[j ? j - 1 : 0] + x : x;
+            }
+            const float other = __shfl_xor(c[3], 16), two = c[3] + other, far = __shfl_xor(two, 32);
+            const float before = upto + ((g & 1 ? other : 0.0f) + (g & 2 ? far : 0.0f));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              c[j] = row_sum16(whole || 4 * g + j < r ? before + c[j] : 0.0f);
+            if (r == 0) *reinterpret_cast<f4*>(sh.pairs + wave * C + 16 * (first + i) + 4 * g) = c;
+            upto += two + far;
+          }
+          if (C == 32 && !diag && g == 0) sh.rows[r] = upto;
+        }
+      };
+      if constexpr (C == 64) {
+        if (tt == 0) weigh(Count<1>(), true);
+        else if (tt == 1) weigh(Count<2>(), true);
+        else if (tt == 2) weigh(Count<3>(), true);
+        else weigh(Count<4>(), true);
+      } else if (first <= tt) {
+        weigh(Count<1>(), first == tt);
+      } else {
+        *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+    if constexpr (MODE == GRAD_Q) {
+      f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(S[kt][nt][i], after[kt][nt][i], sum[i]);
+      float d = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int q = 1; q < 64; q <<= 1) d += __shfl_xor(d, q);
+      if (lane == 0) sh.ends[wave] = d;
+    }
 
     if (__builtin_expect(bad, 0)) {
+      if constexpr (GRAD) {  // a or b, of the state that the chunk starts from
+#pragma unroll 1
+        for (int i = 0; i < cnt; ++i) {
+          int vc = v0 + vb + r, kg = 8 * g;
+          asm volatile("" : "+v"(vc), "+v"(kg));
+          float d = 0.0f, acc[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) acc[nt] = 0.0f;
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int kk = kg + 32 * (kt >> 1) + 4 * (kt & 1) + j;
+              if (kk < a.KK) {
+                const float x = widen1(sh.x[i * KR + kk]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) acc[nt] = __builtin_fmaf(x, S[kt][nt][j], acc[nt]);
+              }
+            }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            if (vc + 16 * nt < a.VV)
+              d += acc[nt] * widen1(ap[(int64_t)(tfirst + tstep * i) * job.A.sl + vc + 16 * nt]);
+          d *= job.neg ? -dec.er[i] : dec.er[i];
+#pragma unroll
+          for (int q = 1; q < 64; q <<= 1) d += __shfl_xor(d, q);
+          if (lane == 0) sh.dots[wave * C + i] = d;
+        }
+      }
       // A zero weight does not silence an infinity or a NaN in a product: such a
       // chunk goes step by step, as the recurrence says, on plain arithmetic.
 #pragma unroll 1
@@ -667,7 +917,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         const float a1 = dec.g1[i];
         int vc = v0 + vb + r, kg = 8 * g;
         asm volatile("" : "+v"(vc), "+v"(kg));  // worked out here, not kept across the walk
-        float xy = 0.0f, d = 0.0f, acc[NT], z[NT];
+        float xy = 0.0f, acc[NT], z[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           acc[nt] = 0.0f;
@@ -706,13 +956,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
                 ((uint16_t*)job.out)[off] = (uint16_t)bf16_rne(y);
               else
                 ((float*)job.out)[off] = y;
-              if (MODE == GRAD) d += y * widen1(ap[t * job.A.sl + vc + 16 * nt]);
             }
-          }
-          if (MODE == GRAD) {
-#pragma unroll
-            for (int q = 1; q < 16; q <<= 1) d += __shfl_xor(d, q);
-            if (lane == 0) sh.dots[wave * C + i] = d;
           }
         }
       }
@@ -723,85 +967,20 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       }
     } else {
       f4 O[TT][NT];
-      if (XS) {
-        // P^T = Y X^T: a wave has 16 steps t (columns) and of the tiles of 16 steps s
-        // (rows) those up to the diagonal's; the pair that holds it is filled with zeros
-        {
-          const auto [g, r] = lane_place(tid);
-          const int tt = wave & (TT - 1), t = tt * 16 + r;
-          const int first = C == 32 ? wave >> 1 : 0;  // its first tile of steps s
-          Frag<T> xf[KP / 32];
-          const E* const xr = sh.x + t * KR + 8 * g;
-#pragma unroll
-          for (int p = 0; p < KP / 32; ++p) xf[p] = as_y(row_frag(xr + 32 * p), g);
-          const float gt = dec.gt[t], gtl = Sh::FINE ? dec.gtl[t] : 0.0f;
-          E* const pw = sh.p + p_row<T>(t);
-          const int m = pswz<T>(t);
-          // N tiles from `first`, the last of them the diagonal's if `diag`
-          auto weigh = [&](auto count, bool diag) __attribute__((always_inline)) {
-            constexpr int N = decltype(count)::value;
-            f4 acc[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
-            const E* const yr = sh.y + (16 * first + r) * KR + 8 * g;
-#pragma unroll
-            for (int p = 0; p < KP / 32; ++p)
-#pragma unroll
-              for (int i = 0; i < N; ++i)
-                acc[i] = mma(row_frag(yr + 16 * i * KR + 32 * p), xf[p], acc[i]);
-            float pv[4 * (N + (N & 1))];
-#pragma unroll
-            for (int i = 0; i < N + (N & 1); ++i)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) pv[4 * i + j] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-              f4 d = gt - *reinterpret_cast<const f4*>(dec.gs + 16 * (first + i) + 4 * g);
-              if (Sh::FINE) d += gtl - *reinterpret_cast<const f4*>(dec.gsl + 16 * (first + i) + 4 * g);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float e = acc[i][j] * __builtin_amdgcn_exp2f(d[j]);
-                pv[4 * i + j] = i == N - 1 && diag && 4 * g + j > r ? 0.0f : e;
-              }
-            }
-            if constexpr (T::SPLIT) {
-#pragma unroll
-              for (int i = 0; i < (N + 1) / 2; ++i) {  // places 32 i + 8 g .. + 7
-                Frag<T> f[NS];
-                parts_of<NS>(pv + 8 * i, f);
-#pragma unroll
-                for (int q = 0; q < NS; ++q)
-                  *reinterpret_cast<s8*>(pw + q * P_SIZE<T> + ((4 * i + g) ^ m) * 8) = f[q].v;
-              }
-            } else {  // places 8 g + 4 first .. + 3
-              *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{pv[0], pv[1], pv[2], pv[3]};
-            }
-          };
-          if constexpr (C == 64) {
-            if (tt == 0) weigh(Count<1>(), true);
-            else if (tt == 1) weigh(Count<2>(), true);
-            else if (tt == 2) weigh(Count<3>(), true);
-            else weigh(Count<4>(), true);
-          } else if (first <= tt) {
-            weigh(Count<1>(), first == tt);
-          } else {
-            *reinterpret_cast<f4*>(pw + ((2 * g + first) ^ m) * 4) = f4{0.f, 0.f, 0.f, 0.f};
-          }
-        }
-      }
       if (wave == 0) {
         put_decays(c + 1);
         load_decays(c + 2);
       }
       // the next chunk's loads fly during the products (after X S where its operands' parts
       // leave no room for them)
-      constexpr bool LATE = MODE == GRAD && NT == 2;
+      constexpr bool LATE = GRAD && NT == 2;
       if (!LATE) load_chunk(c + 1);
 
       // From here to the barrier the products and the vector instructions that make
       // their operands alternate, so that both units work: while the products of
       // one block run, the next one's parts are worked out.
-      const auto [g, r] = lane_place(tid);
+      const LanePlace me = lane_place(tid);
+      const int g = me.g, r = me.r;
       const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
       const E* const ycol[2] = {y_base<KP>(sh.y, g, r, 0), y_base<KP>(sh.y, g, r, 1)};
       const E* const xrow = sh.x + r * KR + 8 * g;
@@ -980,9 +1159,39 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         }
       }
 
+      if constexpr (GRAD) {  // a or b: O is the state's part yet
+        const LanePlace me = lane_place(tid);
+        const int g = me.g, r = me.r;
+        const int vc = v0 + vb + 4 * g;
+#pragma unroll
+        for (int i = 0; i < TT; ++i) {
+          const int row = i * 16 + r;
+          const E* const p = ap + (int64_t)(tfirst + tstep * row) * job.A.sl + vc;
+          float d = 0.0f;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            if (row < cnt && vc + 16 * nt < a.VV) {
+              if (job.avec) {
+                E e[4];
+                __builtin_memcpy(e, __builtin_assume_aligned(p + 16 * nt, 4 * sizeof(E)), sizeof(e));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][nt][j], widen1(e[j]), d);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (vc + 16 * nt + j < a.VV) d = __builtin_fmaf(O[i][nt][j], widen1(p[16 * nt + j]), d);
+              }
+            }
+          d += __shfl_xor(d, 16);
+          d += __shfl_xor(d, 32);
+          if (g == 0) sh.dots[wave * C + row] = job.neg ? -d : d;
+        }
+      }
+
       if (XS) {
         __syncthreads();  // P is whole
-        const auto [g, r] = lane_place(tid);
+        const LanePlace me = lane_place(tid);
+        const int g = me.g, r = me.r;
         const E* const zcol = z_base<VT>(sh.z, g, r) + vb;
 #pragma unroll
         for (int sb = 0; sb < SB; ++sb) {
@@ -990,7 +1199,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) zf[nt] = col_frag<VT>(zcol + 32 * sb * VR + 16 * nt);
 #pragma unroll
-          for (int q = NS - 1; q >= 0; --q)
+          for (int q = Sh::NP - 1; q >= 0; --q)
 #pragma unroll
             for (int i = 2 * sb; i < TT; ++i) {  // steps t before the block have no weight in it
               const Frag<T> pf = p_frag(sh.p + q * P_SIZE<T>, i * 16 + r, sb, g);
@@ -1011,26 +1220,10 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         for (int i = 0; i < TT; ++i) {
           const int row = i * 16 + r;
           const int64_t t = tfirst + tstep * row;
-          float d = 0.0f;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             const int v = vc + 16 * nt;
             const bool live = row < cnt && v < a.VV;
-            if constexpr (MODE == GRAD) {
-              if (live) {
-                const E* p = ap + t * job.A.sl + v;
-                if (job.avec) {
-                  E e[4];
-                  __builtin_memcpy(e, __builtin_assume_aligned(p, 4 * sizeof(E)), sizeof(e));
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][nt][j], widen1(e[j]), d);
-                } else {
-#pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    if (v + j < a.VV) d = __builtin_fmaf(O[i][nt][j], widen1(p[j]), d);
-                }
-              }
-            }
             if constexpr (Sh::ROWS) {
               if (job.orows) {
                 const int c = 2 * (NT * wave + nt) + (g >> 1);  // its granule
@@ -1065,17 +1258,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
               }
             }
           }
-          if constexpr (MODE == GRAD) {
-            d += __shfl_xor(d, 16);
-            d += __shfl_xor(d, 32);
-            if (g == 0) sh.dots[wave * C + row] = d;
-          }
         }
       }
-    }
-    if constexpr (MODE == GRAD) {
-      if (job.anchors && reached > 0 && reached < len && reached % a.anchor == 0)
-        store_anchor(anchor_at(reached / a.anchor - 1));
     }
     __syncthreads();  // the tiles are free
     if constexpr (Sh::ROWS) {
@@ -1093,13 +1277,49 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         }
       }
     }
-    if constexpr (MODE == GRAD) {
+    if constexpr (MODE == GRAD_K) {
       if (wave == 0 && lane < cnt) {
         float d = 0.0f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) d += sh.dots[q * C + lane];
-        job.dots[((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst +
-                 tstep * lane] = d;
+        job.sums[((int64_t)tile * a.H + h) * (a.B * a.L) + b * a.L + pl.first + tfirst -
+                 lane] = d;
+      }
+    }
+    if constexpr (MODE == GRAD_Q) {
+      if (wave == 1) {  // lane t: step t of the chunk; its sums in 64 bits
+        const int back = C - 1 - lane;  // the running sum over the steps from the last on
+        double x = 0.0, y = 0.0, all, pairs = 0.0;
+        if (back >= 0 && back < cnt)
+          x = ((double)sh.dots[back] + sh.dots[C + back]) + ((double)sh.dots[2 * C + back] + sh.dots[3 * C + back]);
+        x = wave_running_sum(x, &all);
+        double v = __shfl(x, back & 63);
+        if (lane > 0 && lane < cnt) {
+          const int s = lane - 1;
+          if (C == 64) {
+            for (int q = 0; q < 4; ++q)
+              if (q >= s >> 4) pairs += sh.pairs[q * C + s];
+          } else if (s < 16) {
+            pairs = (double)sh.pairs[s] + sh.pairs[C + s];
+          } else {
+            pairs = sh.pairs[3 * C + s];
+          }
+        }
+        if constexpr (C == 32) {  // pairs of the steps before 16 and from 16 on
+          if (back >= 16 && back < cnt) y = sh.rows[back - 16];
+          y = wave_running_sum(y, &all);
+          y = __shfl(y, back & 63);
+          if (lane > 16) pairs += y;
+        }
+        v += job.neg ? -pairs : pairs;
+        v += wave_running_sum(later, &all);
+        v += ((double)sh.ends[0] + sh.ends[1] + sh.ends[2] + sh.ends[3]) * dec.ec;
+        // where e^g is held at zero its derivative is zero too
+        if (lane >= cnt || own_g < G_MIN) v = 0.0;
+        if (job.dg && lane < cnt)
+          job.dg[(b * a.L + pl.first + tfirst + lane) * job.dg_st + h * job.dg_sh + tile * job.dg_sq] =
+              (float)v;
+        dg_sum += v;
       }
     }
   }
@@ -1112,8 +1332,13 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
     if (job.last)
       store_state(job.last + (pl.n * a.H + h) * a.KV,
                   rev && len > 0 ? exp2_of((double)clamp_g(gp[0]) * 1.4426950408889634) : 1.0f);
-    if (MODE == GRAD && job.anchors && job.last_anchor && len > 0)
-      store_anchor(anchor_at((len + a.anchor - 1) / a.anchor - 1));
+  }
+  if constexpr (MODE == GRAD_Q) {
+    if (job.by_slot && wave == 1) {
+#pragma unroll
+      for (int q = 32; q > 0; q >>= 1) dg_sum += __shfl_xor(dg_sum, q);
+      if (lane == 0) job.by_slot[(slot * a.tiles + tile) * a.H + h] = dg_sum;
+    }
   }
 }
 
@@ -1122,8 +1347,10 @@ int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
   const dim3 grid((unsigned)wgs), block(256);
   if (m == CARRY)
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, CARRY, VEC>), grid, block, 0, st, a);
-  else if (m == GRAD)
-    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD, VEC>), grid, block, 0, st, a);
+  else if (m == GRAD_K)
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD_K, VEC>), grid, block, 0, st, a);
+  else if (m == GRAD_Q)
+    hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD_Q, VEC>), grid, block, 0, st, a);
   else if constexpr (T::SPLIT && NT == 1) {  // OUT_ONCE takes tiles of 64 columns
     if (m == OUT_ONCE)
       hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT_ONCE, VEC>), grid, block, 0, st, a);
