@@ -465,7 +465,7 @@ struct Shared {
   typename T::E x[XS ? C * ROW<T, KP> : 8];
   typename T::E p[XS ? NP * P_SIZE<T> : 8];
   // A chunk's decays, of this chunk and the next.
-  struct Decays {
+  struct alignas(16) Decays {  // read in fours
     float gs[C], gsl[FINE ? C : 4];  // by step s: the running log2 decay, high and low parts
     float gt[C], gtl[FINE ? C : 4];  // by step t: the same with log2 |pscale|
     float er[C];                     // by step: rscale 2^G
