@@ -461,9 +461,8 @@ int64_t sw_selective_scan_bwd_workspace(int64_t B, int64_t D, int64_t N, int64_t
  * its h0 (or zero).
  *
  * The state and all sums are fp32; bf16 inputs run on bf16 matrix instructions
- * with the state's increments split so that they keep fp32 accuracy.  o is then
- * rounded once more where the chunk's weights and the state become operands (not
- * so in calls of at most 128 steps with few heads, nor with fp32 inputs).
+ * with the states, the state's increments and the chunk's weights split in bf16
+ * parts: o is rounded once, at its end, whatever the sizes of the call.
  * An infinity or NaN in q, k, v or g reaches the steps from its own on, as in
  * the recurrence, and no earlier one.
  *
@@ -495,11 +494,11 @@ int64_t sw_linear_attn_fwd_workspace(int64_t B, int64_t L, int64_t Hk, int64_t H
  *   dh_last : (nseq, H, K, V) fp32 or NULL (zero)
  *   dq, dk, dv : dense, of dtype, rounded once from fp32;  dg : (B, L, H) fp32, or
  *   (H) with SW_LINEAR_G_HEAD;  dh0 : (nseq, H, K, V) fp32 or NULL
- * The states in dq, dk and dg keep fp32 accuracy; dv is rounded as o is.  dg is a
- * sum of products of steps before t with steps from t on, without a difference, so
- * that it keeps its digits where a step forgets nearly everything; it is zero where
- * g < -104.  An infinity or NaN reaches the steps that it reaches through these sums.
- * Results are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
+ * The states in dq, dk and dg keep fp32 accuracy.  dg is a sum of products of
+ * steps before t with steps from t on, without a difference, so that it keeps its
+ * digits where a step forgets nearly everything; it is zero where g < -104.  An
+ * infinity or NaN reaches the steps that it reaches through these sums.  Results
+ * are deterministic.  With no steps, dg (H) is zero and dh0 = dh_last.
  * The workspace holds a state of each head for every 64 steps (32 for fp32 inputs):
  * 4 H K V / 64 bytes a step, 2.7 GB at L = 65536, H = 40, K = V = 128; and fp32
  * gradients of q and k for every head where heads share them.  Otherwise as

@@ -195,7 +195,6 @@ struct Plan {
   int64_t tiles_v = 1, tiles_k = 1;
   int64_t lseg = CHUNK, per_seq = 1, slots = 0;  // segments
   bool cut = false;                // some sequence may have several
-  Mode out = OUT;                  // how the output (or dv) is rounded
   int64_t kept = 0;                // chunk ends inside sequences: dS is kept there for dg
 };
 
@@ -213,11 +212,11 @@ double pace(int64_t wgs, int cus, int64_t contracted, int nt, bool bf16) {
 }
 
 // Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
-// alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, gradient
-// with its row sums 9.5; a workgroup's start and end are worth two chunks of the
-// kernel's (one of these for fp32), the composition 12 us and 0.1 for each segment.
-// At B=8 L=2048 H=12 forward and backward took 680 us with the backward's sequences
-// whole and 552 in the parts chosen.
+// alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, dk and dq
+// with their parts of dg 22 together; a workgroup's start and end are worth two
+// chunks of the kernel's (one of these for fp32), the composition 12 us and 0.1 for
+// each segment.  At B=8 L=2048 H=12 forward and backward took 1010 us with the
+// backward's sequences whole and 594 in the parts chosen.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
   p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
@@ -226,15 +225,6 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   p.tiles_k = (a.K + 64 * p.nt_k - 1) / (64 * p.nt_k);
   const int64_t longest = a.L, chunks = (longest + CHUNK - 1) / CHUNK;
   const int64_t rows = a.B * a.H;
-  // Rounded once where a call is so short that its launch is what it costs: one or
-  // two chunks, and no compute unit with more than one workgroup (L=100 H=4 K=V=64:
-  // 12.0 us, 11.7 otherwise).  Elsewhere P and S are rounded to bf16 as operands, which
-  // with the output's own rounding makes 1.41 times its error.
-  if (a.bf16 && chunks <= 2 && (a.cu ? a.nseq : a.B) * a.H * ((a.V + 63) / 64) <= cus) {
-    p.out = OUT_ONCE;
-    p.nt_v = 1;
-    p.tiles_v = (a.V + 63) / 64;
-  }
   int64_t parts = 1;
   double best = 0.0;
   for (int64_t n = 1; n <= 256 && (n == 1 || 2 * n <= chunks); ++n) {
@@ -242,7 +232,7 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
     double us;
     if (bwd) {
       us = len * ((n > 1 ? 3.0 * pace(rows * n * 2 * p.tiles_k, cus, a.V, p.nt_k, a.bf16) : 0.0) +
-                  18.0 * pace(rows * n * p.tiles_k, cus, a.V, p.nt_k, a.bf16) +
+                  22.0 * pace(rows * n * p.tiles_k, cus, a.V, p.nt_k, a.bf16) +
                   5.5 * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16));
     } else {
       us = len * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16) * (n > 1 ? 8.5 : 5.5);
@@ -492,7 +482,7 @@ int linear_attn_fwd(const LinAttnArgs& a) {
     if ((st = launch_fold(a, p, f, 1, s)) != SW_OK) return st;
   }
   w.job[0] = j;
-  if ((st = launch_walk_any(a, w, p.out, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
+  if ((st = launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
   if (!a.cu || a.L == 0) return SW_OK;
   ClearArgs c{};
   int n = 0;
@@ -581,7 +571,7 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   w.job[0] = jq;
   if ((st = launch_walk_any(a, w, GRAD_Q, a.V, a.K, p.nt_k, p.tiles_k, s)) != SW_OK) return st;
   w.job[0] = jv;
-  if ((st = launch_walk_any(a, w, p.out, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
+  if ((st = launch_walk_any(a, w, OUT, a.K, a.V, p.nt_v, p.tiles_v, s)) != SW_OK) return st;
 
   const int64_t T = a.B * a.L;
   if (a.g_head) {

@@ -23,11 +23,12 @@
 //
 // Rounding (bf16): products of inputs are exact in fp32 accumulators.  The
 // weighted Z is split in three bf16 parts whose sum is the fp32 value, so S
-// keeps fp32 accuracy whatever the number of chunks.  For an output in bf16, P
-// and S are rounded to bf16 once as operands (NS = NP = 1); for outputs of few
-// steps both are split in three.  For dq and dk S is split in three, since its
-// products make dg too, and P in two: 2^-17 of the weights beside the result's
-// own rounding of 2^-9.  fp32 inputs run on the fp32 matrix instructions throughout.
+// keeps fp32 accuracy whatever the number of chunks.  P and S are split in two as
+// operands of an output: 2^-17 of its terms beside its own rounding of 2^-9, so that
+// every output is rounded to bf16 once, at its end, in calls of any size (one part
+// each made 1.41 times that error and took 72 us for o's walk at B=8 L=2048 H=12
+// K=V=128 where two take 76).  For dq and dk S is split in three, since its products
+// make dg too.  fp32 inputs run on the fp32 matrix instructions throughout.
 #pragma once
 
 #include "linear_attn.h"
@@ -430,8 +431,8 @@ struct Tile {
   }
 };
 
-// What a walk is for: the segments' carries; an output; a bf16 output rounded once,
-// at its end; dk, and dq, with their parts of dg.
+// What a walk is for: the segments' carries; an output; dk, and dq, with their parts
+// of dg.
 //
 // dg_t = e^{g_t} <dS_t, S_{t-1}> is the sum over the pairs of a step s < t and a step
 // t' >= t of scale (q_t' . k_s) (do_t' . v_s) e^{G_t' - G_s} (and h0's and dh_last's
@@ -448,26 +449,24 @@ struct Tile {
 // each chunk's end, decayed by the step after it.  dq's walk has S before each chunk
 // in its accumulators.  The states' traffic is 8 K V bytes a chunk and head; keeping
 // both and multiplying them apart would be twice that.
-enum Mode { CARRY, OUT, OUT_ONCE, GRAD_K, GRAD_Q };
+enum Mode { CARRY, OUT, GRAD_K, GRAD_Q };
 constexpr bool is_grad(Mode m) { return m >= GRAD_K; }
 
 template <class T, int KP, int NT, Mode MODE>
 struct Shared {
   static constexpr int VT = 64 * NT, C = T::C;
-  // Parts of P and S: S makes a and b, which have fp32 accuracy
-  static constexpr int NS = MODE >= OUT_ONCE && T::SPLIT ? 3 : 1;
-  static constexpr int NP = !T::SPLIT || MODE < OUT_ONCE ? 1 : is_grad(MODE) ? 2 : 3;
+  // Parts of S, which makes a and b too, of fp32 accuracy; and of P
+  static constexpr int NS = !T::SPLIT ? 1 : is_grad(MODE) ? 3 : 2;
+  static constexpr int NP = T::SPLIT ? 2 : 1;
   static constexpr bool XS = MODE != CARRY;
-  // fp32 results take the decays between steps to fp32: their running sums in two parts
-  static constexpr bool FINE = MODE >= OUT_ONCE || !T::SPLIT;
   typename T::E y[C * ROW<T, KP>];
   typename T::E z[C * ROW<T, VT>];
   typename T::E x[XS ? C * ROW<T, KP> : 8];
   typename T::E p[XS ? NP * P_SIZE<T> : 8];
   // A chunk's decays, of this chunk and the next.
   struct alignas(16) Decays {  // read in fours
-    float gs[C], gsl[FINE ? C : 4];  // by step s: the running log2 decay, high and low parts
-    float gt[C], gtl[FINE ? C : 4];  // by step t: the same with log2 |pscale|
+    float gs[C], gsl[C];  // by step s: the running log2 decay, high and low parts
+    float gt[C], gtl[C];  // by step t: the same with log2 |pscale|
     float er[C];                     // by step: rscale 2^G
     float g1[C];                     // by step: its own decay
     float ew[C];                     // by place: wscale 2^(G_C - G)
@@ -475,7 +474,8 @@ struct Shared {
   } dec[2];
   // bf16 outputs leave as whole rows: a wave's columns are 32 or 64 bytes of each step's
   static constexpr bool ROWS = MODE == OUT && T::SPLIT;
-  typename T::E o[ROWS ? C * VT : 8];  // granule c of row t at c ^ oswz(t)
+  static constexpr bool IN_X = ROWS && KP >= VT;  // x is read by then
+  typename T::E o[ROWS && !IN_X ? C * VT : 8];  // granule c of row t at c ^ oswz(t)
   float dots[is_grad(MODE) ? 4 * C : 4];       // a or b: each wave's columns' part
   alignas(16) float pairs[MODE == GRAD_Q ? 4 * C : 4];     // by wave and step s: M summed for dg of step s + 1
   float rows[MODE == GRAD_Q && C == 32 ? 16 : 4];  // steps 16 ..: M summed over the steps before 16
@@ -533,7 +533,7 @@ __device__ __forceinline__ LanePlace lane_place(int tid) {
 // fragment of X, Y and P for twice the products: with eight waves of 16 columns
 // instead, LDS reads doubled and set the pace.
 constexpr int walk_waves(int KP, int NT, Mode m) {
-  return KP >= 256 ? 1 : NT == 2 || KP == 128 ? 2 : m >= OUT_ONCE ? 3 : 4;
+  return KP >= 256 ? 1 : NT == 2 || KP == 128 ? 2 : m != CARRY ? 3 : 4;
 }
 
 template <class T, int KP, int NT, Mode MODE, bool VEC>
@@ -636,6 +636,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
                      __attribute__((always_inline)) { S[kt][nt][i] = p[at]; });
   }
   float seg_decay = 1.0f;
+  E* const orow = Sh::IN_X ? sh.x : sh.o;
   double dg_sum = 0.0;
 
   Tile<T, KP, THREADS, VEC> tx, ty;
@@ -674,10 +675,8 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         const float s_ = (float)G, t_ = (float)Gt;
         d.gs[lane] = s_;
         d.gt[lane] = t_;
-        if (Sh::FINE) {
-          d.gsl[lane] = (float)(G - (double)s_);
-          d.gtl[lane] = job.plog > -1.0e30 ? (float)(Gt - (double)t_) : 0.0f;
-        }
+        d.gsl[lane] = (float)(G - (double)s_);
+        d.gtl[lane] = job.plog > -1.0e30 ? (float)(Gt - (double)t_) : 0.0f;
         d.er[lane] = exp2_of(G) * job.rscale;
       }
       d.ew[place_in(lane)] = exp2_of(GC - G) * job.wscale;
@@ -781,7 +780,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         for (int p = 0; p < VT / 32; ++p)
           load_frag(af[p], ar + 32 * p, t < cnt ? a.VV - v0 - 8 * g - 32 * p : 0, job.avec);
       }
-      const float gt = dec.gt[t], gtl = Sh::FINE ? dec.gtl[t] : 0.0f;
+      const float gt = dec.gt[t], gtl = dec.gtl[t];
       E* const pw = sh.p + p_row<T>(t);
       const int m = pswz<T>(t);
       // N tiles from `first`, the last of them the diagonal's if `diag`
@@ -804,7 +803,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           f4 d = gt - *reinterpret_cast<const f4*>(dec.gs + 16 * (first + i) + 4 * g);
-          if (Sh::FINE) d += gtl - *reinterpret_cast<const f4*>(dec.gsl + 16 * (first + i) + 4 * g);
+          d += gtl - *reinterpret_cast<const f4*>(dec.gsl + 16 * (first + i) + 4 * g);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float e = acc[i][j] * __builtin_amdgcn_exp2f(d[j]);
@@ -1227,7 +1226,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
             if constexpr (Sh::ROWS) {
               if (job.orows) {
                 const int c = 2 * (NT * wave + nt) + (g >> 1);  // its granule
-                *reinterpret_cast<uint2*>(sh.o + row * VT + (c ^ oswz<VT>(row)) * 8 + 4 * (g & 1)) =
+                *reinterpret_cast<uint2*>(orow + row * VT + (c ^ oswz<VT>(row)) * 8 + 4 * (g & 1)) =
                     make_uint2(bf16x2_rne(O[i][nt][0], O[i][nt][1]),
                                bf16x2_rne(O[i][nt][2], O[i][nt][3]));
                 continue;
@@ -1273,8 +1272,9 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
           const int row = id / NG + i * (THREADS / NG);
           if (row < cnt && v0 + col < a.VV)
             *reinterpret_cast<u4*>((E*)job.out + ob + (tfirst + tstep * row) * job.ol + v0 + col) =
-                *reinterpret_cast<const u4*>(sh.o + row * VT + (col / G ^ oswz<VT>(row)) * G);
+                *reinterpret_cast<const u4*>(orow + row * VT + (col / G ^ oswz<VT>(row)) * G);
         }
+        if (Sh::IN_X) __syncthreads();  // x is free
       }
     }
     if constexpr (MODE == GRAD_K) {
@@ -1351,12 +1351,7 @@ int launch_walk_at(const WalkArgs& a, Mode m, int64_t wgs, hipStream_t st) {
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD_K, VEC>), grid, block, 0, st, a);
   else if (m == GRAD_Q)
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, GRAD_Q, VEC>), grid, block, 0, st, a);
-  else if constexpr (T::SPLIT && NT == 1) {  // OUT_ONCE takes tiles of 64 columns
-    if (m == OUT_ONCE)
-      hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT_ONCE, VEC>), grid, block, 0, st, a);
-    else
-      hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
-  } else
+  else
     hipLaunchKernelGGL((walk_kernel<T, KP, NT, OUT, VEC>), grid, block, 0, st, a);
   return check_launch("walk_kernel");
 }
