@@ -213,10 +213,13 @@ double pace(int64_t wgs, int cus, int64_t contracted, int nt, bool bf16) {
 
 // Segments: the count with the lowest price.  Prices in us, of a chunk of a walk
 // alone on its compute unit (K = V = 128, bf16): output 5.5, carries 3, dk and dq
-// with their parts of dg 22 together; a workgroup's start and end are worth two
-// chunks of the kernel's (one of these for fp32), the composition 12 us and 0.1 for
-// each segment.  At B=8 L=2048 H=12 forward and backward took 1010 us with the
-// backward's sequences whole and 594 in the parts chosen.
+// with their parts of dg 22 together; a workgroup's start and end are worth one
+// chunk of the kernel's (half of one for fp32), the two launches more 20 us and 0.2 for
+// each segment.  Over 44 forwards and 44 backwards of all widths, lengths and both
+// types, timed at every count, the count so priced took 2.8% and 1.6% more than the
+// best (geometric mean): starts of two chunks, no segment below two and 12 us took 5.7%
+// and 6.4%.  At B=8 L=2048 H=12 K=V=128 forward and backward take 1010 us with the
+// backward's sequences whole and 612 in the parts chosen.
 Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   Plan p;
   p.nt_v = a.V <= 64 || a.K > 128 ? 1 : 2;
@@ -227,17 +230,19 @@ Plan make_plan(const LinAttnArgs& a, bool bwd, int cus) {
   const int64_t rows = a.B * a.H;
   int64_t parts = 1;
   double best = 0.0;
-  for (int64_t n = 1; n <= 256 && (n == 1 || 2 * n <= chunks); ++n) {
-    const double len = (double)((chunks + n - 1) / n) + (a.bf16 ? 2.0 : 1.0);
+  for (int64_t n = 1; n <= 256 && (n == 1 || n <= chunks); ++n) {
+    const double len = (double)((chunks + n - 1) / n) + (a.bf16 ? 1.0 : 0.5);
+    // packed: sequences end inside a segment
+    const int64_t segs = a.cu ? a.H * n + 3 * a.H * a.nseq / 4 : rows * n;
     double us;
     if (bwd) {
-      us = len * ((n > 1 ? 3.0 * pace(rows * n * 2 * p.tiles_k, cus, a.V, p.nt_k, a.bf16) : 0.0) +
-                  22.0 * pace(rows * n * p.tiles_k, cus, a.V, p.nt_k, a.bf16) +
-                  5.5 * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16));
+      us = len * ((n > 1 ? 3.0 * pace(2 * segs * p.tiles_k, cus, a.V, p.nt_k, a.bf16) : 0.0) +
+                  22.0 * pace(segs * p.tiles_k, cus, a.V, p.nt_k, a.bf16) +
+                  5.5 * pace(segs * p.tiles_v, cus, a.K, p.nt_v, a.bf16));
     } else {
-      us = len * pace(rows * n * p.tiles_v, cus, a.K, p.nt_v, a.bf16) * (n > 1 ? 8.5 : 5.5);
+      us = len * pace(segs * p.tiles_v, cus, a.K, p.nt_v, a.bf16) * (n > 1 ? 8.5 : 5.5);
     }
-    if (n > 1) us += 12.0 + 0.1 * (double)n;
+    if (n > 1) us += 20.0 + 0.2 * (double)n;
     if (n == 1 || us < best) {
       best = us;
       parts = n;
@@ -545,12 +550,14 @@ int linear_attn_bwd(const LinAttnArgs& a) {
   // dk, then dq, and their parts of dg
   jk.A = a.k;
   jk.adiv = r;
-  jk.avec = rows_vec(a.k, a.K, a.bf16);
+  if (a.L <= 1) jk.A.sl = a.K;
+  jk.avec = rows_vec(jk.A, a.K, a.bf16);
   jk.sums = jq.sums = at(l.sums);
   jk.kept = jq.kept = at(l.kept);
   jq.A = a.q;
   jq.adiv = r;
-  jq.avec = rows_vec(a.q, a.K, a.bf16);
+  if (a.L <= 1) jq.A.sl = a.K;
+  jq.avec = rows_vec(jq.A, a.K, a.bf16);
   jq.dlast = a.dh_last;
   jq.dvec = (uintptr_t)a.dh_last % 16 == 0;
   if (a.g_head) {

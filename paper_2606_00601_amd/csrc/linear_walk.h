@@ -56,7 +56,7 @@ struct Job {
   float* sums;           // [tile][H][B * L]
   float* kept;           // (chunk ends inside sequences, H, K, V)
   const float* dlast;    // (sequences, H, K, V): the state after the last step, or NULL
-  bool dvec;             // its rows are whole aligned fours
+  bool dvec;             // it lies on 16 bytes
   float* dg;             // dg of step i, head h and tile q at dg[i dg_st + h dg_sh + q dg_sq], or NULL
   int64_t dg_st, dg_sh, dg_sq;
   double* by_slot;       // (slots, tiles, H): dg's sums over the segment's steps, or NULL
@@ -234,10 +234,12 @@ __device__ __forceinline__ void load_frag(Frag<Bf16>& f, const uint16_t* p, int 
   f.v = s8{0, 0, 0, 0, 0, 0, 0, 0};
   if (vec) {
     if (left > 0) f.v = *reinterpret_cast<const s8*>(p);
-  } else {
+  } else if (left > 0) {  // in flight together: past the row its last one, not used
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) f.v[j] = (short)p[j];
+    for (int j = 0; j < 8; ++j) {
+      const short x = (short)p[min(j, left - 1)];
+      f.v[j] = j < left ? x : (short)0;
+    }
   }
 }
 __device__ __forceinline__ void load_frag(Frag<F32>& f, const float* p, int left, bool vec) {
@@ -246,10 +248,12 @@ __device__ __forceinline__ void load_frag(Frag<F32>& f, const float* p, int left
   if (vec) {
     if (left > 0) *reinterpret_cast<f4*>(f.v) = *reinterpret_cast<const f4*>(p);
     if (left > 4) *reinterpret_cast<f4*>(f.v + 4) = *reinterpret_cast<const f4*>(p + 4);
-  } else {
+  } else if (left > 0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < left) f.v[j] = p[j];
+    for (int j = 0; j < 8; ++j) {
+      const float x = p[min(j, left - 1)];
+      f.v[j] = j < left ? x : 0.0f;
+    }
   }
 }
 // X's fragment in the order of Y's.
@@ -722,7 +726,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         const float g1 = dec.g1[0];  // of step tend
         each_four(kept_at(tend), [&](int kt, int nt, float* p, int left) __attribute__((always_inline)) {
           const f4 x = S[kt][nt] * g1;
-          if (a.KK % 4 == 0) {
+          if (VEC) {
             *reinterpret_cast<f4*>(p) = x;
           } else {
 #pragma unroll
@@ -748,15 +752,16 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
       const float* p = tend < len  ? kept_at(tend)
                        : job.dlast ? job.dlast + (pl.n * a.H + h) * a.KV
                                    : nullptr;
-      const bool vec = a.KK % 4 == 0 && (tend < len || job.dvec);
       if (p)
         each_four(p, [&](int kt, int nt, const float* q, int left) __attribute__((always_inline)) {
-          if (vec) {
+          if (VEC) {
             after[kt][nt] = *reinterpret_cast<const f4*>(q);
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (i < left) after[kt][nt][i] = q[i];
+            for (int i = 0; i < 4; ++i) {
+              const float x = q[min(i, left - 1)];
+              after[kt][nt][i] = i < left ? x : 0.0f;
+            }
           }
         });
     }
@@ -778,7 +783,7 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
         const E* const ar = ap + (int64_t)(tfirst + t) * job.A.sl + v0 + 8 * g;
 #pragma unroll
         for (int p = 0; p < VT / 32; ++p)
-          load_frag(af[p], ar + 32 * p, t < cnt ? a.VV - v0 - 8 * g - 32 * p : 0, job.avec);
+          load_frag(af[p], ar + 32 * p, t < cnt ? a.VV - v0 - 8 * g - 32 * p : 0, VEC);
       }
       const float gt = dec.gt[t], gtl = dec.gtl[t];
       E* const pw = sh.p + p_row<T>(t);
@@ -1170,15 +1175,18 @@ __global__ __launch_bounds__(256, walk_waves(KP, NT, MODE)) void walk_kernel(Wal
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
             if (row < cnt && vc + 16 * nt < a.VV) {
-              if (job.avec) {
+              if (VEC) {
                 E e[4];
                 __builtin_memcpy(e, __builtin_assume_aligned(p + 16 * nt, 4 * sizeof(E)), sizeof(e));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) d = __builtin_fmaf(O[i][nt][j], widen1(e[j]), d);
               } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (vc + 16 * nt + j < a.VV) d = __builtin_fmaf(O[i][nt][j], widen1(p[16 * nt + j]), d);
+                for (int j = 0; j < 4; ++j) {
+                  const int last = a.VV - 1 - vc - 16 * nt;
+                  const float x = widen1(p[16 * nt + min(j, last)]);
+                  d = __builtin_fmaf(O[i][nt][j], j <= last ? x : 0.0f, d);
+                }
               }
             }
           d += __shfl_xor(d, 16);
@@ -1376,7 +1384,8 @@ int launch_walk(const WalkArgs& a, Mode m, int nt, hipStream_t st) {
   if (wgs == 0) return SW_OK;
   bool vec = true;
   for (int i = 0; i < a.njobs; ++i)
-    vec = vec && (m == CARRY || a.job[i].xvec) && a.job[i].yvec && a.job[i].zvec;
+    vec = vec && (m == CARRY || a.job[i].xvec) && a.job[i].yvec && a.job[i].zvec &&
+          (!is_grad(m) || a.job[i].avec) && (m != GRAD_Q || a.job[i].dvec);
   return vec ? launch_walk_vec<T, true>(a, m, nt, wgs, st)
              : launch_walk_vec<T, false>(a, m, nt, wgs, st);
 }
