@@ -42,7 +42,7 @@ from __future__ import annotations
 
 import torch
 
-from ._bind import _need, _on, _ptr
+from ._bind import _differentiable_once, _need, _on, _ptr
 from ._lib import (SW_DELTA_SOFTPLUS, SW_DTYPE_BF16, SW_DTYPE_F32,  # noqa: F401
                    ScanWeaverError, check, fast, last_error, lib, status_string)
 from ._linear import linear_attn_bwd, linear_attn_fn, linear_attn_fwd, linear_attn_step
@@ -442,9 +442,11 @@ class _SelectiveScanFn(torch.autograd.Function):
         g = _bwd(x, delta, A, Bm, Cm, Dskip, dy, dh_last, z, delta_bias, h0, ctx.delta_softplus,
                  h0 is not None and h0.requires_grad, ck, sp, gdt)
         cast = lambda t, like: None if t is None else t.to(like.dtype)  # noqa: E731
-        return (cast(g["dx"], x), cast(g["ddelta"], delta), g["dA"], cast(g["dB"], Bm),
-                cast(g["dC"], Cm), g.get("dDskip"), cast(g.get("dz"), z) if z is not None else None,
-                g.get("ddelta_bias"), g.get("dh0"), None)
+        grads = (cast(g["dx"], x), cast(g["ddelta"], delta), g["dA"], cast(g["dB"], Bm),
+                 cast(g["dC"], Cm), g.get("dDskip"), cast(g.get("dz"), z) if z is not None else None,
+                 g.get("ddelta_bias"), g.get("dh0"), None)
+        return _differentiable_once("selective_scan_fn", grads,
+                                    (x, delta, A, Bm, Cm, Dskip, z, delta_bias, h0, dy, dh_last))
 
 
 def selective_scan_fn(x, delta, A, Bm, Cm, Dskip=None, z=None, delta_bias=None, h0=None,

@@ -71,3 +71,32 @@ class _on:
         if self.prev >= 0:
             torch.cuda.set_device(self.prev)
         return False
+
+
+class _Once(torch.autograd.Function):
+    """Gradients on their way out of a backward: themselves, and an error where they
+    are differentiated again."""
+
+    @staticmethod
+    def forward(ctx, name, count, *tensors):
+        ctx.name = name
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError(f"{ctx.name} cannot be differentiated twice: its backward is not "
+                           "differentiable")
+
+
+def _differentiable_once(name, grads, inputs):
+    """``grads`` (tensors or None) of a backward that read ``inputs``.  Under
+    ``create_graph`` they depend on those, so that a second derivative raises instead of
+    coming out without their share."""
+    if not torch.is_grad_enabled():
+        return grads
+    there = []
+    for g in grads:
+        if g is not None and not any(g is t for t in there):
+            there.append(g)
+    out = _Once.apply(name, len(there), *there, *(t for t in inputs if t is not None))
+    return tuple(None if g is None else next(o for o, t in zip(out, there) if t is g) for g in grads)

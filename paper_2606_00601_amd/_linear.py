@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import torch
 
-from ._bind import _dense_like, _need, _on, _ptr
+from ._bind import _dense_like, _differentiable_once, _need, _on, _ptr
 from ._lib import SW_DTYPE_BF16, SW_DTYPE_F32, SW_LINEAR_G_HEAD, check, fast
 
 _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
@@ -174,7 +174,8 @@ class _LinearAttnFn(torch.autograd.Function):
             dh_last = dh_last.contiguous().to(torch.float32)
         r = linear_attn_bwd(q, k, v, g, do, dh_last, scale=ctx.scale, h0=h0, cu_seqlens=cu,
                             want_dh0=h0 is not None and ctx.needs_input_grad[4])
-        return r["dq"], r["dk"], r["dv"], r["dg"], r.get("dh0"), None, None, None
+        grads = r["dq"], r["dk"], r["dv"], r["dg"], r.get("dh0"), None, None, None
+        return _differentiable_once("linear_attn_fn", grads, (q, k, v, g, h0, do, dh_last))
 
 
 def linear_attn_fn(q, k, v, g, *, scale=None, h0=None, cu_seqlens=None, return_last_state=False):

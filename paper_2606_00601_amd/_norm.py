@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import torch
 
-from ._bind import _dense_like, _need, _on, _ptr
+from ._bind import _dense_like, _differentiable_once, _need, _on, _ptr
 from ._lib import SW_DTYPE_BF16, SW_DTYPE_F32, SW_GATE_AFTER, check, fast
 
 _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
@@ -147,8 +147,9 @@ class _ResidualNormFn(torch.autograd.Function):
             dy = torch.zeros(out.shape, dtype=ctx.dtype, device=out.device)
         r = residual_norm_bwd(_grad_like(dy, ctx.dtype), _grad_like(dres, out.dtype), out, weight,
                               x=x, res_scale=res_scale, eps=ctx.eps)
-        return (r["dx"], r["dweight"], None if ctx.alone else r["dresidual"],
-                r.get("dres_scale"), None)
+        grads = (r["dx"], r["dweight"], None if ctx.alone else r["dresidual"],
+                 r.get("dres_scale"), None)
+        return _differentiable_once("residual_norm_fn", grads, (out, weight, x, res_scale, dy, dres))
 
 
 def residual_norm_fn(x, weight, residual=None, *, res_scale=None, eps=1e-6):
@@ -217,7 +218,8 @@ class _GatedNormFn(torch.autograd.Function):
     def backward(ctx, dy):
         x, z, weight = ctx.saved_tensors
         r = gated_norm_bwd(_grad_like(dy, x.dtype), x, z, weight, **ctx.how)
-        return r["dx"], r.get("dz"), r["dweight"], None, None, None
+        grads = r["dx"], r.get("dz"), r["dweight"], None, None, None
+        return _differentiable_once("gated_norm_fn", grads, (x, z, weight, dy))
 
 
 def gated_norm_fn(x, z, weight, *, group=None, gate_after=False, eps=1e-6):
