@@ -7,8 +7,28 @@ namespace sw {
 namespace norm {
 namespace {
 
-__device__ __forceinline__ float sigmoid_f32(float z) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * 1.4426950408889634f));
+// 1 / (1 + e^-z) and, in rest, 1 minus it.  fp32 inputs: to fp32 rounding.  -z log2 e
+// is rounded to h, which alone would cost 2^-24 |z| of the result; what that misses, r,
+// multiplies 2^h by 1 + r ln 2.  z is held only where 2^h is 0 or infinite already: an
+// infinite one would make r NaN.  bf16 inputs go without these (2^-18 at |z| = 64, beside
+// results of 2^-9): with them the backward of 16384 rows of 12 groups of 128 took 54 us
+// for 50.
+template <class E>
+__device__ __forceinline__ float sigmoid_f32(float z, float& rest) {
+  constexpr float C = 1.4426950408889634f, REST = (float)(1.4426950408889634 - (double)C);
+  if constexpr (sizeof(E) == 2) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * C));
+    rest = 1.0f - s;
+    return s;
+  } else {
+    const float m = -__builtin_amdgcn_fmed3f(z, -200.0f, 200.0f);
+    const float h = m * C;
+    const float r = __builtin_fmaf(m, REST, __builtin_fmaf(m, C, -h));
+    const float e = __builtin_amdgcn_exp2f(h) * __builtin_fmaf(r, 0.6931471805599453f, 1.0f);
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    rest = z > 0.0f ? e * s : 1.0f - s;
+    return s;
+  }
 }
 
 enum Gate { NONE, BEFORE, AFTER };
@@ -41,7 +61,8 @@ __global__ __launch_bounds__(threads_of(LPR)) void gated_fwd_kernel(GatedNormArg
         load8((const E*)a.z + m * a.z_st + g0 + c, gate[v], a.group - c, vec);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          gate[v][j] *= sigmoid_f32(gate[v][j]);
+          float rest;
+          gate[v][j] *= sigmoid_f32<E>(gate[v][j], rest);
           if (GATE == BEFORE) x[v][j] *= gate[v][j];
         }
       }
@@ -88,7 +109,7 @@ __global__ __launch_bounds__(threads_of(LPR)) void gated_bwd_kernel(GatedNormArg
     for (int j = 0; j < 8; ++j) dw[v][j] = 0.0f;
   }
   for (int64_t m = blk * RPW + sub; m < a.M; m += blocks * RPW) {
-    float x[NV][8], z[NV][8], sg[NV][8], d[NV][8];
+    float x[NV][8], z[NV][8], slope[NV][8], d[NV][8];  // z becomes silu(z)
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -100,9 +121,12 @@ __global__ __launch_bounds__(threads_of(LPR)) void gated_bwd_kernel(GatedNormArg
       for (int j = 0; j < 8; ++j) {
         float u = x[v][j], dn = w[v][j] * d[v][j];
         if (GATE != NONE) {
-          sg[v][j] = sigmoid_f32(z[v][j]);
-          if (GATE == BEFORE) u *= z[v][j] * sg[v][j];
-          if (GATE == AFTER) dn *= z[v][j] * sg[v][j];
+          float rest;
+          const float sg = sigmoid_f32<E>(z[v][j], rest);
+          slope[v][j] = sg * __builtin_fmaf(z[v][j], rest, 1.0f);
+          z[v][j] *= sg;
+          if (GATE == BEFORE) u *= z[v][j];
+          if (GATE == AFTER) dn *= z[v][j];
         }
         sum[0] = __builtin_fmaf(u, u, sum[0]);
         sum[1] = __builtin_fmaf(dn, u, sum[1]);
@@ -117,16 +141,13 @@ __global__ __launch_bounds__(threads_of(LPR)) void gated_bwd_kernel(GatedNormArg
       float dx[8], dz[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float gate = GATE == NONE ? 1.0f : z[v][j] * sg[v][j];
+        const float gate = GATE == NONE ? 1.0f : z[v][j];
         const float n = (GATE == BEFORE ? x[v][j] * gate : x[v][j]) * inv;
         const float wd = w[v][j] * d[v][j];
         const float du = inv * ((GATE == AFTER ? wd * gate : wd) - n * mean);
         dw[v][j] = __builtin_fmaf(GATE == AFTER ? d[v][j] * gate : d[v][j], n, dw[v][j]);
         dx[j] = GATE == BEFORE ? du * gate : du;
-        if (GATE != NONE) {
-          const float slope = sg[v][j] * (1.0f + z[v][j] * (1.0f - sg[v][j]));
-          dz[j] = (GATE == AFTER ? wd * n : du * x[v][j]) * slope;
-        }
+        if (GATE != NONE) dz[j] = (GATE == AFTER ? wd * n : du * x[v][j]) * slope[v][j];
       }
       store8((E*)a.dx + m * a.D + g0 + c, dx, a.group - c, vec);
       if (GATE != NONE) store8((E*)a.dz + m * a.D + g0 + c, dz, a.group - c, vec);
