@@ -439,8 +439,10 @@ int64_t sw_selective_scan_bwd_workspace(int64_t B, int64_t D, int64_t N, int64_t
  *
  *   q, k : (B, L, Hk, K) of dtype      v : (B, L, H, V) of dtype
  *   g    : (B, L, H) fp32 log decays, or, with SW_LINEAR_G_HEAD, (H) fp32, one
- *          for all of a head's steps.  g <= 0 decays; any value is taken, and
- *          e^g is zero for g < -104 (as it is in fp32), -inf included.
+ *          for all of a head's steps.  g <= 0 decays, and e^g is zero for
+ *          g < -104 (as it is in fp32), -inf included.  g > 0 grows the state:
+ *          where those of steps in a row add up to more than 87 (e^88 is more
+ *          than fp32 holds), results may be infinite or NaN.
  *   o    : (B, L, H, V) of dtype, dense
  *   h0, h_last : (nseq, H, K, V) fp32, dense, or NULL
  * H is a multiple of Hk; head h reads the q and k of head h / (H / Hk).
