@@ -1,5 +1,5 @@
-"""Linear attention at the edges of its contract: rows of packed sequences padded to a
-fixed length; no heads; many sequences."""
+"""Linear attention at the edges of its contract: packed rows padded to a fixed length,
+no heads, many sequences, graphs of the backward, offsets past 32 bits."""
 import numpy as np
 import pytest
 
@@ -124,3 +124,56 @@ def test_many_short_sequences_of_wide_heads(sw):
     want = (q.float() * k.float()).sum(-1, keepdim=True) * K ** -0.5 * v.float()
     # q.k and the result are rounded to bf16; the sums of q.k to fp32
     assert ((o.float() - want).abs() <= 2.0 ** -7 * want.abs() + 1e-6 * v.abs()).all()
+
+
+@pytest.mark.parametrize("const", [False, True])
+def test_backward_captured(sw, const):
+    """As a graph replayed on new inputs, a packed and padded row with shared heads."""
+    L, Hk, H, K, V = 900, 2, 4, 64, 64
+    t = _rand(31, "bf16", q=(1, L, Hk, K), k=(1, L, Hk, K), v=(1, L, H, V), do=(1, L, H, V),
+              g=(H,) if const else (1, L, H), h0=(3, H, K, V), dh=(3, H, K, V))
+    t["g"] = -0.1 * t["g"].abs()
+    c = torch.tensor([0, 500, 512, 850], dtype=torch.int32, device="cuda")
+    q = t["q"].clone()
+
+    def run():
+        return sw.linear_attn_bwd(q, t["k"], t["v"], t["g"], t["do"], t["dh"], h0=t["h0"], cu_seqlens=c)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for i in range(3):
+        q.copy_(t["q"] * (i + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run()
+        for n in want:
+            assert torch.equal(out[n], want[n]), (i, n)
+
+
+def test_offsets_past_32_bits(sw):
+    """2^31 elements and more in v, o, dout and dv, the heads' rows far apart: the last
+    head as of a call of its own."""
+    L, H, K, V = 2 ** 18, 66, 16, 128
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    q, k = rand(1, L, 1, K), rand(1, L, 1, K)
+    v, do = rand(1, H, L, V).transpose(1, 2), rand(1, L, H, V)
+    assert v.numel() > 2 ** 31
+    g = -0.1 * torch.rand(1, L, H, generator=gen, device="cuda")
+    last = lambda x: x[:, :, H - 1:]  # noqa: E731
+    near = lambda a, b, rel: ((a.double() - b.double()).square().mean()  # noqa: E731
+                              <= rel ** 2 * b.double().square().mean()).item()
+    print("case far offsets, forward", flush=True)
+    o, h = sw.linear_attn_fwd(q, k, v, g)
+    o1, h1 = sw.linear_attn_fwd(q, k, last(v), last(g))
+    # single bf16 roundings that fall the other way, and fp32 sums
+    assert near(last(o), o1, 2.0 ** -11) and near(h[:, H - 1:], h1, 2.0 ** -18)
+    del o, o1
+    print("case far offsets, backward", flush=True)
+    r = sw.linear_attn_bwd(q, k, v, g, do)
+    r1 = sw.linear_attn_bwd(q, k, last(v), last(g), last(do))
+    assert near(last(r["dv"]), r1["dv"], 2.0 ** -11) and near(last(r["dg"]), r1["dg"], 2.0 ** -18)
+    assert torch.isfinite(r["dq"]).all() and torch.isfinite(r["dk"]).all()
