@@ -592,6 +592,136 @@ int sw_gated_norm_bwd(const void* dy, const void* x, const void* z, const float*
                       int64_t dy_stride, int64_t x_stride, int64_t z_stride, int dtype, int flags,
                       float eps, void* workspace, int64_t workspace_bytes);
 
+/*
+ * Gated linear recurrence: the affine recurrence of Eq. (3) with one state for
+ * each channel and gates that make its pairs,
+ *
+ *   m_t = c softplus(lam) sigmoid(r_t),  a_t = e^{-m_t}
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t
+ *   h_last = the state after the last step; h_{-1} = h0, or zero
+ *
+ *   x, r, i : (B, L, D) of dtype, r and i before their sigmoids
+ *   lam     : (D) fp32;  c > 0 and finite
+ *   h       : (B, L, D) of dtype, dense, rounded once from fp32; NULL: not written
+ *   h0, h_last : (nseq, D) fp32, dense, or NULL
+ *   ckpt    : (B, ceil(L / SW_GATED_CKPT), D) fp32 or NULL: the state before every
+ *             SW_GATED_CKPT-th step, for the backward
+ * strides: host array of 6 element strides >= 0, over (B, L) of x, r and i in turn;
+ * the D channels of a step are contiguous.
+ *
+ * cu_seqlens: NULL (then nseq = B), or (nseq + 1) int32 device values, ascending
+ * within [0, L], B = 1: sequences packed into one row, as for sw_linear_attn_fwd.
+ * Steps that no sequence covers read as zero in h and in every gradient, whatever
+ * x, r and i hold there; an empty sequence's h_last is its h0 (or zero).
+ *
+ * The state, the gates and all sums are fp32.  sqrt(1 - a^2) is formed from m, so
+ * that it keeps its digits as a nears 1.  An infinity or NaN in a step's inputs
+ * makes that step and those after it in its channel and sequence infinite or NaN,
+ * as far as the recurrence carries it, and touches no other.
+ *
+ * workspace: 16-byte aligned, at least sw_gated_scan_fwd_workspace bytes, that nothing
+ * else uses until the call completes, or NULL: from the device's stream-ordered
+ * pool for the call (no capture then).  Results do not depend on it; every call
+ * of the same inputs gives the same bits.
+ */
+enum { SW_GATED_CKPT = 128 };
+int sw_gated_scan_fwd(const void* x, const void* r, const void* i, const float* lam,
+                      const float* h0, const int32_t* cu_seqlens, void* h, float* h_last,
+                      float* ckpt, int64_t B, int64_t L, int64_t D, int64_t nseq,
+                      const int64_t* strides, int dtype, float c, void* workspace,
+                      int64_t workspace_bytes);
+int64_t sw_gated_scan_fwd_workspace(int64_t B, int64_t L, int64_t D);
+
+/*
+ * Backward: the gradients of sum(dh * h) + sum(dh_last * h_last).  With g_t that with
+ * respect to h_t, g_t = dh_t + a_{t+1} g_{t+1} (the last step's: + dh_last), b =
+ * sqrt(1 - a^2), s = sigmoid(i) and
+ *   e_t = g_t (a^2 (m / b) s x - m a h_{t-1}):
+ *   dx = g b s,  di = g b s (1 - s) x,  dr = e (1 - sigmoid(r)),
+ *   dlam = sum e * sigmoid(lam) / softplus(lam),  dh0 = a_0 g_0
+ * (m / b tends to sqrt(m / 2) where a nears 1, so nothing here is singular).
+ *   dh : (B, L, D) of dtype; its strides follow i's in `strides` (8 values)
+ *   dx, dr, di : (B, L, D) of dtype, dense;  dlam : (D) fp32;  dh0 : (nseq, D) fp32 or
+ *   NULL;  ckpt : the forward's, or NULL (formed again)
+ * Sums run in a fixed order.  With no steps dlam is zero and dh0 = dh_last.
+ */
+int sw_gated_scan_bwd(const void* x, const void* r, const void* i, const float* lam,
+                      const float* h0, const int32_t* cu_seqlens, const float* ckpt,
+                      const void* dh, const float* dh_last, void* dx, void* dr, void* di,
+                      float* dlam, float* dh0, int64_t B, int64_t L, int64_t D, int64_t nseq,
+                      const int64_t* strides, int dtype, float c, void* workspace,
+                      int64_t workspace_bytes);
+int64_t sw_gated_scan_bwd_workspace(int64_t B, int64_t L, int64_t D, int ckpt);
+
+/*
+ * One step of B sequences, their states updated in place (serving): x, r, i (B, D)
+ * of dtype, rows strides[0..2] apart; h (B, D) of dtype, dense; state (pool, D)
+ * fp32; slots : (B) int32 device values or NULL, as for sw_linear_attn_step.
+ */
+int sw_gated_scan_step(const void* x, const void* r, const void* i, const float* lam,
+                       float* state, const int32_t* slots, void* h, int64_t B, int64_t D,
+                       int64_t pool, const int64_t* strides, int dtype, float c);
+
+/*
+ * The norm of each head's query and key, with the rotation by the token's position:
+ *   u = w * x / sqrt(mean(x^2) + eps)   over the K columns of a head
+ *   y = u with its first R columns turned, pair j by the angle position * inv_freq[j]:
+ *       (p, q) -> (p cos - q sin, q cos + p sin)
+ * where pair j is columns (j, j + R / 2), or, with SW_HEAD_ADJACENT, (2 j, 2 j + 1).
+ *   q, yq : (B, L, H, K);  k, yk : (B, L, Hk, K), of dtype; 1 <= K <= 256.  The
+ *           outputs are dense.  H and Hk may be any, zero among them.
+ *   wq, wk : (K) fp32 or NULL (ones)
+ *   inv_freq : (R / 2) fp32; R even, at most K; R = 0: no rotation (inv_freq unused)
+ *   positions : (B, L) int32, with SW_HEAD_POS_I64 int64 values, of any sign; NULL: l
+ * Angles are formed and reduced in 64 bits, so that far positions keep theirs to
+ * fp32.  Sums are fp32, outputs rounded once.
+ * strides: host array of 8 element strides >= 0: q's and k's over (B, L, heads), then
+ * positions' over (B, L).  One launch; can be captured.
+ */
+enum { SW_HEAD_ADJACENT = 1, SW_HEAD_POS_I64 = 2 };
+int sw_head_norm_fwd(const void* q, const void* k, const float* wq, const float* wk,
+                     const void* positions, const float* inv_freq, void* yq, void* yk, int64_t B,
+                     int64_t L, int64_t H, int64_t Hk, int64_t K, int64_t R,
+                     const int64_t* strides, int dtype, int flags, float eps);
+
+/*
+ * Its gradients: dq and dk dense, of dtype; dwq, dwk (K) fp32 (both or neither NULL),
+ * their sums over tokens and heads in a fixed order.  strides: dyq's, dyk's, q's and
+ * k's over (B, L, heads), then positions' (14 values).  workspace as for
+ * sw_residual_norm_bwd, of sw_head_norm_bwd_workspace bytes; none without dwq.
+ */
+int sw_head_norm_bwd(const void* dyq, const void* dyk, const void* q, const void* k,
+                     const float* wq, const float* wk, const void* positions,
+                     const float* inv_freq, void* dq, void* dk, float* dwq, float* dwk, int64_t B,
+                     int64_t L, int64_t H, int64_t Hk, int64_t K, int64_t R,
+                     const int64_t* strides, int dtype, int flags, float eps, void* workspace,
+                     int64_t workspace_bytes);
+int64_t sw_head_norm_bwd_workspace(int64_t B, int64_t L, int64_t H, int64_t Hk, int64_t K);
+
+/*
+ * Rows of a table by token, scaled: y_t = scale * table[token_t], rounded once.
+ *   tokens : (T) int32, or int64 with SW_EMBED_TOKENS_I64; one outside [0, V) is no
+ *            token (padding): its row is zero
+ *   table  : (V, D) of table_dtype, dense;  y : (T, D) of y_dtype, dense
+ * One launch; can be captured.
+ */
+enum { SW_EMBED_TOKENS_I64 = 1 };
+int sw_embedding_fwd(const void* tokens, const void* table, void* y, int64_t T, int64_t V,
+                     int64_t D, int table_dtype, int y_dtype, int flags, float scale);
+
+/*
+ * The table's gradient, dense: dtable[v] = scale * (the sum of dy_t over the t with
+ * token_t = v), rounded once to table_dtype; zero where there is none.  Sums are fp32,
+ * in an order that T and the tokens alone fix: the same inputs give the same bits.
+ * dy : T rows of D of dy_dtype, dy_stride elements apart.  T < 2^31.  workspace: 16-byte aligned,
+ * at least sw_embedding_bwd_workspace bytes, or NULL: from the device's
+ * stream-ordered pool (no capture then).
+ */
+int sw_embedding_bwd(const void* tokens, const void* dy, void* dtable, int64_t T, int64_t V,
+                     int64_t D, int64_t dy_stride, int dy_dtype, int table_dtype, int flags,
+                     float scale, void* workspace, int64_t workspace_bytes);
+int64_t sw_embedding_bwd_workspace(int64_t T, int64_t V, int64_t D);
+
 /* Stream used by the calling thread's subsequent calls (a hipStream_t;
  * NULL = the null stream).  Always SW_OK. */
 int sw_set_stream(void* hip_stream);

@@ -45,9 +45,12 @@ import torch
 from ._bind import _differentiable_once, _need, _on, _ptr
 from ._lib import (SW_DELTA_SOFTPLUS, SW_DTYPE_BF16, SW_DTYPE_F32,  # noqa: F401
                    ScanWeaverError, check, fast, last_error, lib, status_string)
+from ._gated import gated_scan_bwd, gated_scan_fn, gated_scan_fwd, gated_scan_step
 from ._linear import linear_attn_bwd, linear_attn_fn, linear_attn_fwd, linear_attn_step
 from ._norm import (gated_norm_bwd, gated_norm_fn, gated_norm_fwd, residual_norm_bwd,
                     residual_norm_fn, residual_norm_fwd)
+from ._token import (embedding_bwd, embedding_fn, embedding_fwd, head_norm_bwd, head_norm_fn,
+                     head_norm_fwd)
 
 __all__ = ["last_launch", "selective_scan_plan", "affine_scan", "affine_scan_noalloc", "affine_scan_i32", "affine_scan_schedule", "affine_scan_schedule_i32",
            "affine_scan_proj", "affine_scan_proj_i32",
@@ -56,6 +59,9 @@ __all__ = ["last_launch", "selective_scan_plan", "affine_scan", "affine_scan_noa
            "linear_attn_fwd", "linear_attn_bwd", "linear_attn_fn", "linear_attn_step",
            "residual_norm_fwd", "residual_norm_bwd", "residual_norm_fn",
            "gated_norm_fwd", "gated_norm_bwd", "gated_norm_fn",
+           "gated_scan_fwd", "gated_scan_bwd", "gated_scan_fn", "gated_scan_step",
+           "head_norm_fwd", "head_norm_bwd", "head_norm_fn",
+           "embedding_fwd", "embedding_bwd", "embedding_fn",
            "ScanWeaverError",
            "version"]
 

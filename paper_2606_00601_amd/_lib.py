@@ -21,6 +21,10 @@ SW_DTYPE_BF16 = 1
 SW_DELTA_SOFTPLUS = 1
 SW_LINEAR_G_HEAD = 1
 SW_GATE_AFTER = 1
+SW_GATED_CKPT = 128
+SW_HEAD_ADJACENT = 1
+SW_HEAD_POS_I64 = 2
+SW_EMBED_TOKENS_I64 = 1
 SW_SCHED_DEFAULT = 0
 SW_SCHED_BLELLOCH = 1
 
@@ -58,6 +62,17 @@ SIGNATURES = {
     "sw_gated_norm_fwd": (_int, [_vp] * 4 + [_i64] * 5 + [_int] * 2 + [_f32]),
     "sw_gated_norm_bwd": (_int, [_vp] * 7 + [_i64] * 6 + [_int] * 2 + [_f32, _vp, _i64]),
     "sw_norm_bwd_workspace": (_i64, [_i64] * 3 + [_int]),
+    "sw_gated_scan_fwd": (_int, [_vp] * 9 + [_i64] * 4 + [_strides, _int, _f32, _vp, _i64]),
+    "sw_gated_scan_fwd_workspace": (_i64, [_i64] * 3),
+    "sw_gated_scan_bwd": (_int, [_vp] * 14 + [_i64] * 4 + [_strides, _int, _f32, _vp, _i64]),
+    "sw_gated_scan_bwd_workspace": (_i64, [_i64] * 3 + [_int]),
+    "sw_gated_scan_step": (_int, [_vp] * 7 + [_i64] * 3 + [_strides, _int, _f32]),
+    "sw_head_norm_fwd": (_int, [_vp] * 8 + [_i64] * 6 + [_strides, _int, _int, _f32]),
+    "sw_head_norm_bwd": (_int, [_vp] * 12 + [_i64] * 6 + [_strides, _int, _int, _f32, _vp, _i64]),
+    "sw_head_norm_bwd_workspace": (_i64, [_i64] * 5),
+    "sw_embedding_fwd": (_int, [_vp] * 3 + [_i64] * 3 + [_int] * 3 + [_f32]),
+    "sw_embedding_bwd": (_int, [_vp] * 3 + [_i64] * 4 + [_int] * 3 + [_f32, _vp, _i64]),
+    "sw_embedding_bwd_workspace": (_i64, [_i64] * 3),
     "sw_set_stream": (_int, [_vp]),
     "sw_get_stream": (_vp, []),
     "sw_status_string": (ctypes.c_char_p, [_int]),

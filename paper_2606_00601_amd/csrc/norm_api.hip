@@ -36,31 +36,6 @@ size_t reach(int64_t M, int64_t D, int64_t st, size_t es) {
   return M == 0 ? 0 : (size_t)((M - 1) * st + D) * es;
 }
 
-struct In {
-  const void* p;
-  size_t align, bytes;
-  const char* name;
-  bool required;
-};
-
-// Inputs, then outputs: device memory, aligned, no output over another array.
-int check_arrays(const In* ins, int nin, const In* outs, int nout) {
-  int dev, st;
-  if ((st = current_device(&dev)) != SW_OK) return st;
-  Span is[8], os[8];
-  for (int i = 0; i < nin; ++i) {
-    if ((st = check_ptr(ins[i].p, ins[i].align, ins[i].name, ins[i].required, dev)) != SW_OK)
-      return st;
-    is[i] = {ins[i].p, ins[i].bytes, ins[i].name};
-  }
-  for (int i = 0; i < nout; ++i) {
-    if ((st = check_ptr(outs[i].p, outs[i].align, outs[i].name, outs[i].required, dev)) != SW_OK)
-      return st;
-    os[i] = {outs[i].p, outs[i].bytes, outs[i].name};
-  }
-  return check_spans(os, nout, is, nin);
-}
-
 int res_fwd(const ResNormArgs& a) {
   int st;
   if ((st = check_rows(a.M, a.D, a.D, {a.x_st, a.res_st})) != SW_OK) return st;

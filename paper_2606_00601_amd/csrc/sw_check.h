@@ -68,6 +68,31 @@ inline int check_spans(const Span* outs, int nout, const Span* ins, int nin) {
   return SW_OK;
 }
 
+struct In {
+  const void* p;
+  size_t align, bytes;
+  const char* name;
+  bool required;
+};
+
+// Inputs, then outputs: device memory, aligned, no output over another array.
+inline int check_arrays(const In* ins, int nin, const In* outs, int nout) {
+  int dev, st;
+  if ((st = current_device(&dev)) != SW_OK) return st;
+  Span is[16], os[8];
+  for (int i = 0; i < nin; ++i) {
+    if ((st = check_ptr(ins[i].p, ins[i].align, ins[i].name, ins[i].required, dev)) != SW_OK)
+      return st;
+    is[i] = {ins[i].p, ins[i].bytes, ins[i].name};
+  }
+  for (int i = 0; i < nout; ++i) {
+    if ((st = check_ptr(outs[i].p, outs[i].align, outs[i].name, outs[i].required, dev)) != SW_OK)
+      return st;
+    os[i] = {outs[i].p, outs[i].bytes, outs[i].name};
+  }
+  return check_spans(os, nout, is, nin);
+}
+
 inline bool all_aligned16(std::initializer_list<const void*> ps) {
   for (const void* p : ps)
     if (p && (uintptr_t)p % 16 != 0) return false;

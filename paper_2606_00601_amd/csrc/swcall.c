@@ -176,6 +176,36 @@ SW_CALL(sw_gated_norm_bwd, "PPPPPPPLLLLLLIIFPL", 18,
         sw_gated_norm_bwd(AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AL(7), AL(8), AL(9), AL(10),
                           AL(11), AL(12), AI(13), AI(14), AF(15), AP(16), AL(17)))
 
+SW_CALL(sw_gated_scan_fwd, "PPPPPPPPPLLLLfIFPL", 18,
+        sw_gated_scan_fwd(
+            AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AP(8), AL(9), AL(10), AL(11),
+            AL(12), AS(13), AI(14), AF(15), AP(16), AL(17)))
+SW_CALL(sw_gated_scan_bwd, "PPPPPPPPPPPPPPLLLLhIFPL", 23,
+        sw_gated_scan_bwd(
+            AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AP(8), AP(9), AP(10), AP(11),
+            AP(12), AP(13), AL(14), AL(15), AL(16), AL(17), AS(18), AI(19), AF(20), AP(21),
+            AL(22)))
+SW_CALL(sw_gated_scan_step, "PPPPPPPLLLcIF", 13,
+        sw_gated_scan_step(
+            AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AL(7), AL(8), AL(9), AS(10), AI(11),
+            AF(12)))
+SW_CALL(sw_head_norm_fwd, "PPPPPPPPLLLLLLhIIF", 18,
+        sw_head_norm_fwd(
+            AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AL(8), AL(9), AL(10), AL(11),
+            AL(12), AL(13), AS(14), AI(15), AI(16), AF(17)))
+SW_CALL(sw_head_norm_bwd, "PPPPPPPPPPPPLLLLLLnIIFPL", 24,
+        sw_head_norm_bwd(
+            AP(0), AP(1), AP(2), AP(3), AP(4), AP(5), AP(6), AP(7), AP(8), AP(9), AP(10), AP(11),
+            AL(12), AL(13), AL(14), AL(15), AL(16), AL(17), AS(18), AI(19), AI(20), AF(21),
+            AP(22), AL(23)))
+SW_CALL(sw_embedding_fwd, "PPPLLLIIIF", 10,
+        sw_embedding_fwd(
+            AP(0), AP(1), AP(2), AL(3), AL(4), AL(5), AI(6), AI(7), AI(8), AF(9)))
+SW_CALL(sw_embedding_bwd, "PPPLLLLIIIFPL", 13,
+        sw_embedding_bwd(
+            AP(0), AP(1), AP(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8), AI(9), AF(10), AP(11),
+            AL(12)))
+
 /* A query of sizes: int64 in, int64 out. */
 #define SW_QUERY(NAME, FMT, NARGS, CALL)                                                       \
   static PyObject* py_##NAME(PyObject* self, PyObject* const* args, Py_ssize_t nargs) { \
@@ -192,6 +222,11 @@ SW_QUERY(sw_norm_bwd_workspace, "LLLI", 4, sw_norm_bwd_workspace(AL(0), AL(1), A
 SW_QUERY(sw_linear_attn_bwd_workspace, "LLLLLLLIII", 10,
          sw_linear_attn_bwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4), AL(5), AL(6), AI(7), AI(8),
                                       AI(9)))
+
+SW_QUERY(sw_gated_scan_fwd_workspace, "LLL", 3, sw_gated_scan_fwd_workspace(AL(0), AL(1), AL(2)))
+SW_QUERY(sw_gated_scan_bwd_workspace, "LLLI", 4, sw_gated_scan_bwd_workspace(AL(0), AL(1), AL(2), AI(3)))
+SW_QUERY(sw_head_norm_bwd_workspace, "LLLLL", 5, sw_head_norm_bwd_workspace(AL(0), AL(1), AL(2), AL(3), AL(4)))
+SW_QUERY(sw_embedding_bwd_workspace, "LLL", 3, sw_embedding_bwd_workspace(AL(0), AL(1), AL(2)))
 
 static PyObject* py_sw_selective_scan_fwd_workspace(PyObject* self, PyObject* const* args,
                                                     Py_ssize_t nargs) {
@@ -290,6 +325,17 @@ static PyMethodDef methods[] = {
     FAST(sw_gated_norm_fwd),
     FAST(sw_gated_norm_bwd),
     FAST(sw_norm_bwd_workspace),
+    FAST(sw_gated_scan_fwd),
+    FAST(sw_gated_scan_bwd),
+    FAST(sw_gated_scan_step),
+    FAST(sw_head_norm_fwd),
+    FAST(sw_head_norm_bwd),
+    FAST(sw_embedding_fwd),
+    FAST(sw_embedding_bwd),
+    FAST(sw_gated_scan_fwd_workspace),
+    FAST(sw_gated_scan_bwd_workspace),
+    FAST(sw_head_norm_bwd_workspace),
+    FAST(sw_embedding_bwd_workspace),
     FAST(sw_set_stream),
     NOARG(sw_get_stream),
     FAST(sw_status_string),

@@ -1,0 +1,390 @@
+"""The gated recurrence against its 64-bit definition: gated_ref derives the bounds.  A
+result in bf16 is off by its rounding, 2^-8 of the value, more."""
+import numpy as np
+import pytest
+
+import gated_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+C = 8.0
+
+
+@pytest.fixture(scope="module")
+def sw():
+    import paper_2606_00601_amd as pkg
+    return pkg
+
+
+def _make(seed, B, L, D, dtype, n=None, dh=True):
+    """Tensors and their values in 64 bits; channels of long and of short memory."""
+    g = np.random.Generator(np.random.PCG64(seed))
+    dt = TYPES[dtype]
+    t = {name: torch.from_numpy(np.clip(g.standard_normal((B, L, D)) * 1.5, -8, 8)).to(dt)
+         for name in ("x", "r", "i", "dh")}
+    t["lam"] = torch.from_numpy(g.uniform(-9, 1, D)).float()
+    for name in ("h0", "dh_last"):
+        t[name] = torch.from_numpy(g.standard_normal((B if n is None else n, D))).float()
+    val = {k: v.double().numpy() for k, v in t.items()}
+    return {k: v.cuda() for k, v in t.items()}, val
+
+
+def _near(got, want, off, what):
+    g = got.double().cpu().numpy()
+    most = off + 1e-30
+    if got.dtype is torch.bfloat16:
+        most = most * 1.01 + 2.0 ** -8 * np.abs(want)
+    err = np.abs(g - want)
+    bad = ~(err <= most)
+    assert not bad.any(), f"{what}: {np.nanmax(err / most):.3g} of the bound at {np.argwhere(bad)[0]}"
+
+
+def _check(sw, t, v, h0, cu, spans, tail=True):
+    ins = [t[n] for n in ("x", "r", "i", "lam")]
+    how = dict(c=C, h0=t["h0"] if h0 else None, cu_seqlens=cu)
+    dl = t["dh_last"] if tail else None
+    want, off = ref.scan(v["x"], v["r"], v["i"], v["lam"], C, v["h0"] if h0 else None, spans, v["dh"],
+                         v["dh_last"] if tail else None)
+    h, last = sw.gated_scan_fwd(*ins, **how)
+    _near(h, want["h"], off["h"], "h")
+    _near(last, want["h_last"], off["h_last"], "h_last")
+    g = sw.gated_scan_bwd(*ins, t["dh"], dl, **how)
+    for name in ("dx", "dr", "di", "dlam", "dh0"):
+        _near(g[name], want[name], off[name], name)
+    # with the states that a training forward keeps: the same
+    leaves = [a.clone().requires_grad_(True) for a in ins]
+    hh, ll = sw.gated_scan_fn(*leaves, **how, return_last_state=True)
+    assert torch.equal(hh, h) and torch.equal(ll, last)
+    ups = [t["dh"]] + ([dl] if tail else [])
+    auto = torch.autograd.grad([hh, ll][:len(ups)], leaves, ups)
+    for a, name in zip(auto, ("dx", "dr", "di", "dlam")):
+        _near(a, want[name], off[name], "autograd " + name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1), (2, 1, 64), (1, 2, 3), (3, 7, 65), (1, 8, 2), (1, 9, 130),
+                                   (2, 15, 63), (1, 16, 64), (1, 17, 66), (1, 100, 256), (2, 127, 5),
+                                   (1, 128, 32), (1, 129, 128), (2, 255, 33), (1, 256, 64), (3, 257, 70),
+                                   (1, 513, 1), (2, 700, 96), (1, 1537, 40)])
+def test_batches(sw, shape, dtype):
+    print("case gated", shape, dtype, flush=True)
+    t, v = _make(sum(shape), *shape, dtype)
+    _check(sw, t, v, shape[1] % 2 == 0, None, None, tail=shape[1] % 3 != 0)
+
+
+@pytest.mark.parametrize("dtype,L,D", [("f32", 9000, 34), ("bf16", 12345, 6), ("bf16", 5000, 200)])
+def test_long_rows(sw, dtype, L, D):
+    """Carries through dozens of chunks, channels that remember thousands of steps."""
+    print("case gated long", dtype, L, D, flush=True)
+    t, v = _make(L, 1, L, D, dtype)
+    _check(sw, t, v, True, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L,D,edges", [
+    (1, 4, [0, 1]), (40, 70, [0, 0, 1, 1, 2, 17, 40]), (300, 64, [0, 16, 128, 129, 255, 256, 300]),
+    (600, 33, [5, 5, 100, 100, 580, 580]), (50, 8, [20, 20]), (50, 8, [0, 0, 0]), (700, 20, [3, 690]),
+    (2000, 10, [0, 1, 130, 131, 640, 1280, 1999]), (300, 16, list(range(0, 301)))])
+def test_packed(sw, L, D, edges, dtype):
+    """Sequences of every length, none and one among them, and steps that none covers."""
+    print("case gated packed", L, D, edges[:8], dtype, flush=True)
+    n = len(edges) - 1
+    t, v = _make(L + D, 1, L, D, dtype, n)
+    cu = torch.tensor(edges, dtype=torch.int32, device="cuda")
+    for t0, t1 in ((0, edges[0]), (edges[-1], L)):
+        for name in ("x", "r", "i", "dh"):
+            t[name][:, t0:t1] = float("nan")
+    spans = [(0, edges[i], edges[i + 1]) for i in range(n)]
+    _check(sw, t, v, D % 4 == 0, cu, spans)
+
+
+def test_many_sequences_of_one_step_and_none(sw):
+    n, D = 5000, 3
+    lens = np.random.Generator(np.random.PCG64(5)).integers(0, 3, n)
+    edges = np.concatenate([[0], np.cumsum(lens)])
+    t, v = _make(6, 1, int(edges[-1]), D, "f32", n)
+    _check(sw, t, v, True, torch.tensor(edges, dtype=torch.int32, device="cuda"),
+           [(0, int(edges[i]), int(edges[i + 1])) for i in range(n)])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_at_their_ends(sw, dtype):
+    """Gates wide open and shut, decays of next to one and of nothing: finite, and as the
+    64-bit form.  a nears 1 down to m = 1e-9, where sqrt(1 - a^2) is 4e-5."""
+    L, D = 300, 60
+    t, v = _make(9, 1, L, D, dtype)
+    t["lam"][:20] = torch.linspace(-22, -10, 20, device="cuda")
+    t["lam"][20:40] = torch.linspace(2, 40, 20, device="cuda")
+    t["lam"][40], t["lam"][41] = -200.0, -float("inf")
+    t["r"][:, :, 42:46] = -8.0
+    t["r"][:, :, 46:50] = 8.0
+    v = {n: x.double().cpu().numpy() for n, x in t.items()}
+    _check(sw, t, v, True, None, None)
+    # beyond what the bounds are derived for: gates of +-1e4 and infinities
+    t["r"][:, ::3, 50:], t["i"][:, ::2, 50:] = 1e4, -1e4
+    t["r"][:, 1::3, 50:], t["i"][:, 1::2, 50:] = -float("inf"), float("inf")
+    t["lam"][55:] = 1e30
+    t["r"][:, 1::3, 55:] = 2.0
+    h, _ = sw.gated_scan_fwd(t["x"], t["r"], t["i"], t["lam"], c=C)
+    g = sw.gated_scan_bwd(t["x"], t["r"], t["i"], t["lam"], t["dh"], c=C)
+    assert torch.isfinite(h).all()
+    assert all(torch.isfinite(g[n]).all() for n in ("dx", "dr", "di", "dlam"))
+    shut = torch.isinf(t["r"][0, :, 50])
+    assert (g["dr"][0, shut, 50] == 0).all() and (g["dx"][0, shut, 50] == 0).all()
+
+
+def test_not_finite_stays_in_its_channel_and_sequence(sw):
+    L, D, edges = 700, 40, [0, 290, 290, 650]
+    cu = torch.tensor(edges, dtype=torch.int32, device="cuda")
+    t, _ = _make(11, 1, L, D, "f32", 3)
+    args = lambda: [t[n] for n in ("x", "r", "i", "lam")]  # noqa: E731
+    clean, last = sw.gated_scan_fwd(*args(), cu_seqlens=cu, h0=t["h0"])
+    gc = sw.gated_scan_bwd(*args(), t["dh"], cu_seqlens=cu, h0=t["h0"])
+    for name, bad, at, d in (("x", float("inf"), 100, 3), ("r", float("nan"), 288, 7), ("i", float("nan"), 290, 21)):
+        keep = t[name][0, at, d].item()
+        t[name][0, at, d] = bad
+        h, hl = sw.gated_scan_fwd(*args(), cu_seqlens=cu, h0=t["h0"])
+        g = sw.gated_scan_bwd(*args(), t["dh"], cu_seqlens=cu, h0=t["h0"])
+        end = 290 if at < 290 else 650
+        assert not torch.isfinite(h[0, at, d])
+        hit = torch.zeros_like(h, dtype=torch.bool)
+        hit[0, at:end, d] = True
+        assert torch.equal(h[~hit], clean[~hit])
+        seq = torch.zeros_like(hit)
+        seq[0, (0 if at < 290 else 290):end, d] = True
+        for n in ("dx", "dr", "di"):
+            assert torch.equal(g[n][~seq], gc[n][~seq]), (name, n)
+        other = torch.arange(D, device="cuda") != d
+        assert torch.equal(hl[:, other], last[:, other])
+        assert torch.equal(g["dlam"][other], gc["dlam"][other])
+        t[name][0, at, d] = keep
+    # a state that is not finite goes on to its own steps only
+    h0 = t["h0"].clone()
+    h0[0, 5] = float("nan")
+    h, _ = sw.gated_scan_fwd(*args(), cu_seqlens=cu, h0=h0)
+    assert torch.isnan(h[0, :290, 5]).all()
+    assert torch.equal(h[0, 290:], clean[0, 290:]) and torch.equal(h[0, :290, 6:], clean[0, :290, 6:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides(sw, dtype):
+    """Parts of a fused row, rows off any vector, orders of batch and step, broadcasts:
+    the same bits as dense."""
+    dt = TYPES[dtype]
+    for D in (64, 47):
+        both = torch.randn(2, 270, 3 * D + 1, device="cuda").to(dt)
+        x, r, i = (both[..., 1 + j * D:1 + (j + 1) * D] for j in range(3))
+        lam = torch.randn(D, device="cuda")
+        swap = torch.randn(270, 2, D, device="cuda").to(dt).transpose(0, 1)
+        dh = torch.randn(270, 2, D, device="cuda").to(dt).transpose(0, 1)
+        wide = torch.randn(1, 270, D, device="cuda").to(dt).expand(2, -1, -1)
+        one = torch.randn(1, 1, D, device="cuda").to(dt).expand(2, 270, -1)
+        for ins in ((x, r, i), (swap, r, wide), (one, wide, swap)):
+            dense = [t.contiguous() for t in ins]
+            a, b = sw.gated_scan_fwd(*ins, lam), sw.gated_scan_fwd(*dense, lam)
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+            g, h = sw.gated_scan_bwd(*ins, lam, dh), sw.gated_scan_bwd(*dense, lam, dh.contiguous())
+            assert all(torch.equal(g[n], h[n]) for n in g)
+
+
+def test_gradients_against_differences(sw):
+    """Central differences over 2^-7 of a sum weighted at random, fp32: e^2 / 6 of a third
+    derivative some ten times the first's size, 2^-7, and the sums' rounding over 2 e."""
+    L, D = 150, 12
+    t, _ = _make(13, 2, L, D, "f32")
+    t["lam"].uniform_(-4, 0)
+    names = ("x", "r", "i", "lam", "h0")
+    dot = lambda a, b: (a.double() * b.double()).sum().item()  # noqa: E731
+
+    def loss(a):
+        h, last = sw.gated_scan_fwd(a["x"], a["r"], a["i"], a["lam"], h0=a["h0"])
+        return dot(h, t["dh"]) + dot(last, t["dh_last"])
+
+    g = sw.gated_scan_bwd(t["x"], t["r"], t["i"], t["lam"], t["dh"], t["dh_last"], h0=t["h0"])
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for n in names:
+        d = torch.randn(t[n].shape, generator=gen, device="cuda")
+        e = 2.0 ** -7
+        got = (loss({**t, n: t[n] + e * d}) - loss({**t, n: t[n] - e * d})) / (2 * e)
+        size = (g["d" + n].double() * d.double()).abs().sum().item()
+        assert abs(got - dot(g["d" + n], d)) <= 2.0 ** -9 * size, (n, got, dot(g["d" + n], d), size)
+
+
+def test_runs_repeat_and_outputs_given(sw):
+    t, _ = _make(15, 2, 3000, 90, "bf16")
+    args = [t[n] for n in ("x", "r", "i", "lam")]
+    h, last = sw.gated_scan_fwd(*args, h0=t["h0"])
+    out, ol = torch.full_like(h, 7.0), torch.full_like(last, 7.0)
+    again = sw.gated_scan_fwd(*args, h0=t["h0"], h=out, h_last=ol)
+    assert again[0] is out and again[1] is ol and torch.equal(out, h) and torch.equal(ol, last)
+    assert sw.gated_scan_fwd(*args, want_h_last=False)[1] is None
+    g = sw.gated_scan_bwd(*args, t["dh"], h0=t["h0"])
+    for _ in range(3):
+        k = sw.gated_scan_bwd(*args, t["dh"], h0=t["h0"])
+        assert all(torch.equal(g[n], k[n]) for n in g)
+    # parts of a row one after the other are the row
+    a, sa = sw.gated_scan_fwd(*(p[:, :1111] for p in args[:3]), t["lam"], h0=t["h0"])
+    b, sb = sw.gated_scan_fwd(*(p[:, 1111:] for p in args[:3]), t["lam"], h0=sa)
+    whole = torch.cat([a, b], 1)
+    assert ((whole.float() - h.float()).abs() <= 2.0 ** -7 * h.float().abs() + 1e-4).all()
+    assert torch.allclose(sb, last, rtol=1e-4, atol=1e-4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,D", [(1, 1), (3, 64), (64, 5120), (7, 333)])
+def test_step_is_the_scan(sw, B, D, dtype):
+    t, v = _make(B + D, B, 4, D, dtype)
+    pool = torch.full((B + 3, D), 7.0, device="cuda")
+    slots = torch.randperm(B + 3, device="cuda")[:B].to(torch.int32)
+    pool[slots.long()] = t["h0"]
+    want, off = ref.scan(v["x"], v["r"], v["i"], v["lam"], C, v["h0"])
+    fused = torch.cat([t[n] for n in ("x", "r", "i")], -1)
+    for s in range(4):
+        x, r, i = fused[:, s].split(D, -1)
+        h = sw.gated_scan_step(x, r, i, t["lam"], pool, c=C, slots=slots)
+        _near(h, want["h"][:, s], off["h"][:, s], f"step {s}")
+    _near(pool[slots.long()], want["h_last"], off["h_last"], "states")
+    rest = torch.ones(B + 3, dtype=torch.bool, device="cuda")
+    rest[slots.long()] = False
+    assert (pool[rest] == 7.0).all()
+
+
+def test_step_without_slots_and_with_padding(sw):
+    t, _ = _make(17, 5, 1, 70, "f32")
+    x, r, i = (t[n][:, 0] for n in ("x", "r", "i"))
+    a, b = t["h0"].clone(), t["h0"].clone()
+    h = sw.gated_scan_step(x, r, i, t["lam"], a)
+    slots = torch.tensor([0, -1, 2, 5, 4], dtype=torch.int32, device="cuda")
+    k = sw.gated_scan_step(x, r, i, t["lam"], b, slots=slots)
+    for n in (0, 2, 4):
+        assert torch.equal(h[n], k[n]) and torch.equal(a[n], b[n])
+    for n in (1, 3):
+        assert (k[n] == 0).all() and torch.equal(b[n], t["h0"][n])
+
+
+def test_no_steps_and_no_channels(sw):
+    for B, L, D in ((2, 0, 8), (0, 5, 8), (2, 5, 0)):
+        t = [torch.empty(B, L, D, device="cuda") for _ in range(3)]
+        lam, h0 = torch.zeros(D, device="cuda"), torch.randn(B, D, device="cuda")
+        h, last = sw.gated_scan_fwd(*t, lam, h0=h0)
+        assert h.shape == (B, L, D) and last.shape == (B, D)
+        g = sw.gated_scan_bwd(*t, lam, torch.empty(B, L, D, device="cuda"), h0, h0=h0)
+        assert (g["dlam"] == 0).all()
+        if L == 0:
+            assert torch.equal(last, h0) and torch.equal(g["dh0"], h0)
+            assert (sw.gated_scan_fwd(*t, lam)[1] == 0).all()
+            assert (sw.gated_scan_bwd(*t, lam, t[0])["dh0"] == 0).all()
+    t = [torch.empty(1, 0, 8, device="cuda") for _ in range(3)]
+    cu = torch.zeros(4, dtype=torch.int32, device="cuda")
+    h0 = torch.randn(3, 8, device="cuda")
+    assert torch.equal(sw.gated_scan_fwd(*t, torch.zeros(8, device="cuda"), h0=h0, cu_seqlens=cu)[1], h0)
+
+
+def test_only_the_last_state_reaches_the_loss(sw):
+    t, v = _make(19, 2, 300, 20, "bf16")
+    leaves = [t[n].clone().requires_grad_(True) for n in ("x", "r", "i", "lam", "h0")]
+    _, last = sw.gated_scan_fn(*leaves[:4], c=C, h0=leaves[4], return_last_state=True)
+    got = torch.autograd.grad(last, leaves, t["dh_last"])
+    want, off = ref.scan(v["x"], v["r"], v["i"], v["lam"], C, v["h0"], None, np.zeros(v["x"].shape), v["dh_last"])
+    for a, n in zip(got, ("dx", "dr", "di", "dlam", "dh0")):
+        _near(a, want[n], off[n], n)
+
+
+def test_graphs(sw):
+    """Two captured graphs and eager calls in turn, each replay as the eager call."""
+    t, _ = _make(21, 1, 2500, 80, "bf16", 3)
+    cu = torch.tensor([0, 700, 701, 2400], dtype=torch.int32, device="cuda")
+    x = t["x"].clone()
+    state, slots = torch.zeros(4, 80, device="cuda"), torch.tensor([2], dtype=torch.int32, device="cuda")
+
+    def work():
+        h, last = sw.gated_scan_fwd(x, t["r"], t["i"], t["lam"], cu_seqlens=cu, h0=t["h0"])
+        g = sw.gated_scan_bwd(x, t["r"], t["i"], t["lam"], h, last, cu_seqlens=cu, h0=t["h0"])
+        s = sw.gated_scan_step(x[:, 0], t["r"][:, 0], t["i"][:, 0], t["lam"], state, slots=slots)
+        return [h, last, s, *g.values()]
+
+    work()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        state.zero_()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = work()
+        graphs.append((graph, outs))
+    for k in range(3):
+        x.copy_(t["x"] * (k + 1))
+        for graph, outs in graphs:
+            state.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            kept = [o.clone() for o in outs]
+            state.zero_()
+            assert all(torch.equal(a, b) for a, b in zip(kept, work())), k
+
+
+def test_streams(sw):
+    """Calls on several streams at once give the bits of calls one after the other."""
+    cases = [_make(30 + j, 1, 4000 + j, 60, "bf16")[0] for j in range(3)]
+    args = [[t[n] for n in ("x", "r", "i", "lam")] for t in cases]
+    want = [(sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])) for a, t in zip(args, cases)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(4):
+        got = []
+        for a, t, s in zip(args, cases, streams):
+            with torch.cuda.stream(s):
+                got.append((sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])))
+        torch.cuda.synchronize()
+        for (h, g), (wh, wg) in zip(got, want):
+            assert torch.equal(h, wh) and all(torch.equal(g[n], wg[n]) for n in g)
+
+
+def test_offsets_past_32_bits(sw):
+    """Rows that lie 2^31 elements and more apart."""
+    L, D, step = 3, 8, 2 ** 30 + 5
+    big = torch.zeros(2 * step + D, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(3, 1, L, D, device="cuda").bfloat16()
+    x = big.as_strided((1, L, D), (0, step, 1))
+    x.copy_(v[0])
+    lam = torch.randn(D, device="cuda")
+    assert torch.equal(sw.gated_scan_fwd(x, v[1], v[2], lam)[0], sw.gated_scan_fwd(*v, lam)[0])
+    dh = torch.randn(1, L, D, device="cuda").bfloat16()
+    a, b = sw.gated_scan_bwd(x, v[1], v[2], lam, dh), sw.gated_scan_bwd(*v, lam, dh)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+def test_refusals(sw):
+    t, _ = _make(23, 2, 6, 8, "f32")
+    x, r, i, lam, h0 = (t[n] for n in ("x", "r", "i", "lam", "h0"))
+    with pytest.raises(TypeError):
+        sw.gated_scan_fwd(x, r.bfloat16(), i, lam)
+    with pytest.raises(TypeError):
+        sw.gated_scan_fwd(x.half(), r.half(), i.half(), lam)
+    with pytest.raises(TypeError):
+        sw.gated_scan_fwd(x, r, i, lam.bfloat16())
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x, r[:, :5], i, lam)
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x, r, i, lam[:4])
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x.transpose(1, 2), r.transpose(1, 2), i.transpose(1, 2), lam[:6])
+    for c in (0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(ValueError):
+            sw.gated_scan_fwd(x, r, i, lam, c=c)
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x, r, i, lam, h0=h0[:1])
+    cu = torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x, r, i, lam, cu_seqlens=cu)
+    with pytest.raises(TypeError):
+        sw.gated_scan_fwd(x[:1], r[:1], i[:1], lam, cu_seqlens=cu.long())
+    with pytest.raises(ValueError):
+        sw.gated_scan_step(x[:, 0], r[:, 0], i[:, 0], lam, h0[:1])
+    with pytest.raises(ValueError):
+        sw.gated_scan_fwd(x.cpu(), r.cpu(), i.cpu(), lam.cpu())
+    with pytest.raises(sw.ScanWeaverError) as e:
+        sw.gated_scan_fwd(x, r, i, lam, h=x)
+    assert e.value.status == 1 and "overlap" in str(e.value)

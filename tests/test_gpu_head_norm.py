@@ -1,0 +1,311 @@
+"""The norm of each head with its rotation against its 64-bit definition.
+
+Tolerances: a result is formed from terms (a turned value is a difference of two, the
+norm's gradient of two more) by some ten roundings of 2^-24, and an angle is off by less
+than 2^-23 (its reduced value is rounded once, the series cut at 2^-28): 2^-20 of the
+terms' size, and 2^-8 of the value more where it is rounded to bf16.  A weight's gradient
+adds at most 320 times in a row (heads and tokens of a lane, the workgroup's 256 lanes,
+rows of partial sums): 330 x 2^-24."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def sw():
+    import paper_2606_00601_amd as pkg
+    return pkg
+
+
+def _turn(x, pos, freq, adjacent, sign, size=False):
+    """Columns turned in extended precision; with ``size`` the terms' magnitudes."""
+    if freq is None:
+        return np.abs(x) if size else x.copy()
+    n = len(freq)
+    angle = pos.astype(np.longdouble)[..., None] * freq.astype(np.longdouble)
+    c, s = (f(angle).astype(np.float64)[:, :, None] for f in (np.cos, np.sin))
+    s = s * sign
+    y = np.abs(x) if size else x.copy()
+    p, q = (y[..., 0:2 * n:2], y[..., 1:2 * n:2]) if adjacent else (y[..., :n], y[..., n:2 * n])
+    a, b = (p + q, q + p) if size else (p * c - q * s, q * c + p * s)
+    out = y.copy()
+    if adjacent:
+        out[..., 0:2 * n:2], out[..., 1:2 * n:2] = a, b
+    else:
+        out[..., :n], out[..., n:2 * n] = a, b
+    return out
+
+
+def _ref(x, w, pos, freq, adjacent, d):
+    """(y, dx, dw) and the sizes of their terms."""
+    K = x.shape[-1]
+    inv = 1 / np.sqrt((x * x).mean(-1, keepdims=True) + EPS)
+    n = x * inv
+    ww = np.ones(K) if w is None else w
+    y, ty = (_turn(n * ww, pos, freq, adjacent, 1.0, z) for z in (False, True))
+    g, tg = (_turn(d, pos, freq, adjacent, -1.0, z) for z in (False, True))
+    dx = inv * (ww * g - n * (ww * g * n).mean(-1, keepdims=True))
+    tx = inv * (np.abs(ww) * tg + np.abs(n) * (np.abs(ww * n) * tg).mean(-1, keepdims=True))
+    return {"y": y, "dx": dx, "dw": (g * n).sum((0, 1, 2))}, \
+        {"y": ty, "dx": tx, "dw": (tg * np.abs(n)).sum((0, 1, 2))}
+
+
+def _near(got, want, terms, what, unit=2.0 ** -20):
+    g = got.double().cpu().numpy().reshape(want.shape)
+    most = unit * terms + 1e-30
+    if got.dtype is torch.bfloat16:
+        most = most * 1.01 + 2.0 ** -8 * np.abs(want)
+    err = np.abs(g - want)
+    assert (err <= most).all(), f"{what}: {np.max(err / most):.3g} of the bound"
+
+
+def _make(seed, B, L, H, Hk, K, dtype, far=0):
+    g = np.random.Generator(np.random.PCG64(seed))
+    dt = TYPES[dtype]
+    t = {n: torch.from_numpy(g.standard_normal((B, L, h, K))).to(dt)
+         for n, h in (("q", H), ("k", Hk), ("dq", H), ("dk", Hk))}
+    for n in ("wq", "wk"):
+        t[n] = torch.from_numpy(1 + 0.3 * g.standard_normal(K)).float()
+    pos = torch.from_numpy(g.integers(-far, far + 1, (B, L))) + torch.arange(L)
+    v = {n: x.double().numpy() for n, x in t.items()}
+    return {n: x.cuda() for n, x in t.items()}, v, pos
+
+
+def _freq(R):
+    return torch.tensor(10000.0 ** (-np.arange(0, R, 2) / max(R, 1)), dtype=torch.float32) if R else None
+
+
+def _check(sw, t, v, pos, R, adjacent, weights, given):
+    freq = _freq(R)
+    how = dict(inv_freq=None if freq is None else freq.cuda(), adjacent=adjacent, eps=EPS,
+               positions=pos.cuda() if given else None)
+    wq, wk = (t["wq"], t["wk"]) if weights else (None, None)
+    fv = None if freq is None else freq.numpy()
+    p = pos.numpy() if given else np.broadcast_to(np.arange(pos.shape[1]), pos.shape)
+    y = sw.head_norm_fwd(t["q"], t["k"], wq, wk, **how)
+    g = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], wq, wk, **how)
+    for n, got in zip("qk", y):
+        want, terms = _ref(v[n], v["w" + n] if weights else None, p, fv, adjacent, v["d" + n])
+        _near(got, want["y"], terms["y"], n)
+        _near(g["d" + n], want["dx"], terms["dx"], "d" + n)
+        _near(g["dweight_" + n], want["dw"], terms["dw"], "dw" + n, 330 * 2.0 ** -24)
+    less = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], wq, wk, want_dweight=False, **how)
+    assert set(less) == {"dq", "dk"} and all(torch.equal(less[n], g[n]) for n in less)
+
+
+# every number of lanes a head takes, widths off a vector, none, some and all columns turned
+_WIDTHS = [(1, 0), (2, 2), (7, 6), (8, 8), (15, 0), (16, 16), (17, 16), (24, 10), (32, 32), (33, 14),
+           (64, 64), (64, 32), (72, 48), (96, 96), (100, 50), (128, 128), (128, 64), (129, 2), (200, 112),
+           (250, 250), (256, 256), (256, 250), (256, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("K,R", _WIDTHS)
+def test_widths(sw, K, R, adjacent, dtype):
+    print("case head norm", K, R, adjacent, dtype, flush=True)
+    t, v, pos = _make(K + R, 2, 9, 6, 3, K, dtype, 1000)
+    _check(sw, t, v, pos, R, adjacent, K % 3 != 0, True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (64, 1, 40, 8), (1, 300, 2, 2), (3, 41, 5, 1), (2, 1, 33, 0),
+                                   (2, 3, 0, 4), (1, 2000, 1, 1), (1, 1, 300, 20), (8, 130, 12, 12)])
+def test_tokens_and_heads(sw, shape, dtype):
+    print("case head norm", shape, dtype, flush=True)
+    t, v, pos = _make(sum(shape), *shape, 64, dtype, 65536)
+    _check(sw, t, v, pos, 64, False, True, shape[1] % 2 == 0)
+
+
+def test_far_positions(sw):
+    """Positions up to 2^31 and negative ones keep their angles to 2^-21 (pos * freq in 64
+    bits is off by 2^-53 of 2^31), int32 and int64 alike; 2^-19 in all."""
+    K = 64
+    t, v, _ = _make(3, 1, 8, 4, 2, K, "f32")
+    pos = torch.tensor([[0, 1, -1, 10 ** 6, -10 ** 6, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31]])
+    freq = _freq(K)
+    for p in (pos, pos.int()):
+        y, _ = sw.head_norm_fwd(t["q"], t["k"], positions=p.cuda(), inv_freq=freq.cuda(), eps=EPS)
+        want, terms = _ref(v["q"], None, pos.numpy(), freq.numpy(), False, v["dq"])
+        _near(y, want["y"], terms["y"], "far", 2.0 ** -19)
+    # quarter and half turns exactly, by frequencies of 2 pi / 2^k
+    freq = torch.full((K // 2,), 2 * np.pi / 8, dtype=torch.float32)
+    p = torch.arange(-4, 4)[None]
+    y, _ = sw.head_norm_fwd(t["q"], t["k"], positions=p.cuda(), inv_freq=freq.cuda(), eps=EPS)
+    want, terms = _ref(v["q"], None, p.numpy(), freq.numpy(), False, v["dq"])
+    _near(y, want["y"], terms["y"], "eighths")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides(sw, dtype):
+    """Parts of fused rows, rows off a vector, orders and broadcasts: the same bits."""
+    dt = TYPES[dtype]
+    for K in (64, 40, 9):
+        R = K // 2 * 2
+        H, Hk = 6, 2
+        rows = torch.randn(2, 50, (H + 2 * Hk) * K + 1, device="cuda").to(dt)
+        q = rows[..., 1:1 + H * K].unflatten(-1, (H, K))
+        k = rows[..., 1 + H * K:1 + (H + Hk) * K].unflatten(-1, (Hk, K))
+        q2 = torch.randn(H, 50, 2, K, device="cuda").to(dt).permute(2, 1, 0, 3)
+        k2 = torch.randn(2, 1, 1, K, device="cuda").to(dt).expand(2, 50, Hk, K)
+        pos = torch.randint(0, 9999, (50, 2), device="cuda").t()
+        row = torch.arange(50, device="cuda").expand(2, 50)
+        how = dict(inv_freq=_freq(R).cuda(), eps=EPS)
+        for a, b, p in ((q, k, pos), (q2, k2, row), (q, k2, pos.int())):
+            A, Bc, P = a.contiguous(), b.contiguous(), p.contiguous()
+            x, y = sw.head_norm_fwd(a, b, positions=p, **how), sw.head_norm_fwd(A, Bc, positions=P, **how)
+            assert all(torch.equal(m, n) for m, n in zip(x, y))
+            g = sw.head_norm_bwd(q2, k, a, b, positions=p, **how)
+            h = sw.head_norm_bwd(q2.contiguous(), k.contiguous(), A, Bc, positions=P, **how)
+            assert all(torch.equal(g[n], h[n]) for n in g)
+        # one token of each sequence: the same as rows of one step
+        x = sw.head_norm_fwd(q[:, 7], k[:, 7], positions=pos[:, 7], **how)
+        y = sw.head_norm_fwd(q[:, 7:8], k[:, 7:8], positions=pos[:, 7:8], **how)
+        assert x[0].shape == (2, H, K) and all(torch.equal(m, n[:, 0]) for m, n in zip(x, y))
+
+
+def test_zero_rows_and_values_that_are_not_finite(sw):
+    t, _, pos = _make(5, 1, 12, 4, 2, 64, "f32", 100)
+    how = dict(positions=pos.cuda(), inv_freq=_freq(64).cuda())
+    clean = sw.head_norm_fwd(t["q"], t["k"], **how)
+    gc = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], **how)
+    t["q"][0, 2, 1] = 0
+    t["q"][0, 5, 3, 9] = float("nan")
+    t["k"][0, 5, 0, 40] = float("inf")
+    t["q"][0, 6, 0] = 1e-30
+    y = sw.head_norm_fwd(t["q"], t["k"], **how)
+    g = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], **how)
+    assert (y[0][0, 2, 1] == 0).all() and torch.isfinite(g["dq"][0, 2, 1]).all()
+    assert torch.isfinite(g["dq"][0, 6, 0]).all()
+    assert not torch.isfinite(y[0][0, 5, 3]).all() and not torch.isfinite(y[1][0, 5, 0]).all()
+    keep = torch.ones(12, 4, dtype=torch.bool, device="cuda")
+    keep[2, 1] = keep[5, 3] = keep[6, 0] = False
+    assert torch.equal(y[0][0][keep], clean[0][0][keep]) and torch.equal(g["dq"][0][keep], gc["dq"][0][keep])
+    keep = torch.ones(12, 2, dtype=torch.bool, device="cuda")
+    keep[5, 0] = False
+    assert torch.equal(y[1][0][keep], clean[1][0][keep]) and torch.equal(g["dk"][0][keep], gc["dk"][0][keep])
+
+
+def test_rotation_keeps_relative_positions(sw):
+    """Products of queries and keys depend on the distance of their positions alone."""
+    t, _, _ = _make(7, 1, 1, 3, 3, 128, "f32")
+    q, k = t["q"].expand(1, 6, 3, 128), t["k"].expand(1, 6, 3, 128)
+    dots = []
+    for first in (0, 12345, 10 ** 6):
+        a, b = (torch.arange(6, device="cuda")[None] + first + d for d in (7, 0))
+        how = dict(inv_freq=_freq(128).cuda())
+        x = sw.head_norm_fwd(q, k, positions=a, **how)[0]
+        y = sw.head_norm_fwd(q, k, positions=b, **how)[1]
+        dots.append((x.double() * y.double()).sum(-1))
+    # 128 terms of about 1, each off by 2^-20 of its size
+    assert all((d - dots[0][0, 0]).abs().max() < 128 * 2.0 ** -19 for d in dots)
+
+
+def test_gradients_against_differences(sw):
+    """Central differences over 2^-6 of sums weighted at random, fp32: e^2 / 6 of a third
+    derivative a few times the first, and fp32 sums over 2 e."""
+    t, _, pos = _make(9, 2, 5, 3, 2, 20, "f32", 50)
+    dot = lambda a, b: (a.double() * b.double()).sum().item()  # noqa: E731
+    for adjacent in (False, True):
+        how = dict(positions=pos.cuda(), inv_freq=_freq(12).cuda(), adjacent=adjacent)
+        g = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], t["wq"], t["wk"], **how)
+
+        def loss(a):
+            y = sw.head_norm_fwd(a["q"], a["k"], a["wq"], a["wk"], **how)
+            return dot(y[0], t["dq"]) + dot(y[1], t["dk"])
+
+        gen = torch.Generator(device="cuda").manual_seed(9)
+        for n, name in (("q", "dq"), ("k", "dk"), ("wq", "dweight_q"), ("wk", "dweight_k")):
+            d = torch.randn(t[n].shape, generator=gen, device="cuda")
+            e = 2.0 ** -6
+            got = (loss({**t, n: t[n] + e * d}) - loss({**t, n: t[n] - e * d})) / (2 * e)
+            assert abs(got - dot(g[name], d)) <= 2e-3 * (g[name].double() * d.double()).abs().sum().item(), n
+
+
+def test_autograd_matches_backward(sw):
+    t, _, pos = _make(11, 2, 30, 6, 2, 128, "bf16", 500)
+    how = dict(positions=pos.cuda(), inv_freq=_freq(128).cuda(), eps=EPS)
+    leaf = {n: t[n].clone().requires_grad_(True) for n in ("q", "k", "wq", "wk")}
+    y = sw.head_norm_fn(*leaf.values(), **how)
+    g = sw.head_norm_bwd(t["dq"], t["dk"], t["q"], t["k"], t["wq"], t["wk"], **how)
+    got = torch.autograd.grad(y, list(leaf.values()), [t["dq"], t["dk"]])
+    for a, n in zip(got, ("dq", "dk", "dweight_q", "dweight_k")):
+        assert torch.equal(a, g[n]), n
+    # one weight only, and only the keys in the loss
+    q, w = t["q"].clone().requires_grad_(True), t["wk"].clone().requires_grad_(True)
+    a, b = sw.head_norm_fn(q, t["k"], None, w, **how)
+    gq, gw = torch.autograd.grad(b, [q, w], t["dk"])
+    assert (gq == 0).all() and torch.equal(gw, g["dweight_k"])
+    # queries and keys are one tensor: its gradients add
+    x = t["q"].float().requires_grad_(True)
+    a, b = sw.head_norm_fn(x, x, **how)
+    (gx,) = torch.autograd.grad([a, b], [x], [t["dq"].float(), t["dq"].float()])
+    one = sw.head_norm_bwd(t["dq"].float(), t["dq"].float(), x.detach(), x.detach(), **how)
+    assert torch.equal(gx, one["dq"] + one["dk"])
+
+
+def test_graphs_and_no_tokens(sw):
+    t, _, pos = _make(13, 2, 60, 6, 2, 64, "bf16", 500)
+    q, p = t["q"].clone(), pos.cuda()
+    how = dict(positions=p, inv_freq=_freq(64).cuda())
+
+    def work():
+        y = sw.head_norm_fwd(q, t["k"], t["wq"], t["wk"], **how)
+        g = sw.head_norm_bwd(*y, q, t["k"], t["wq"], t["wk"], **how)
+        return [*y, *g.values()]
+
+    work()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = work()
+        graphs.append((graph, outs))
+    for i in range(3):
+        q.copy_(t["q"] * (i + 1))
+        p.add_(17)
+        for graph, outs in graphs:
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, work())), i
+    none = torch.empty(2, 0, 4, 64, device="cuda")
+    y = sw.head_norm_fwd(none, none[:, :, :1])
+    assert y[0].shape == (2, 0, 4, 64) and y[1].shape == (2, 0, 1, 64)
+    g = sw.head_norm_bwd(none, none[:, :, :1], none, none[:, :, :1])
+    assert (g["dweight_q"] == 0).all() and (g["dweight_k"] == 0).all()
+
+
+def test_refusals(sw):
+    t, _, pos = _make(15, 2, 4, 2, 2, 16, "f32")
+    q, k, f = t["q"], t["k"], _freq(16).cuda()
+    for bad in (dict(inv_freq=_freq(18).cuda()), dict(inv_freq=f[None]), dict(inv_freq=f.cpu()),
+                dict(positions=pos.cuda()[:1], inv_freq=f), dict(positions=pos, inv_freq=f)):
+        with pytest.raises(ValueError):
+            sw.head_norm_fwd(q, k, **bad)
+    for bad in (dict(inv_freq=f.double()), dict(positions=pos.cuda().float(), inv_freq=f)):
+        with pytest.raises(TypeError):
+            sw.head_norm_fwd(q, k, **bad)
+    with pytest.raises(TypeError):
+        sw.head_norm_fwd(q, k.bfloat16())
+    with pytest.raises(TypeError):
+        sw.head_norm_fwd(q, k, t["wq"].bfloat16())
+    with pytest.raises(ValueError):
+        sw.head_norm_fwd(q, k[:, :3])
+    with pytest.raises(ValueError):
+        sw.head_norm_fwd(q, k, t["wq"][:8])
+    with pytest.raises(ValueError):
+        sw.head_norm_fwd(q.transpose(-1, -2), k.transpose(-1, -2))
+    with pytest.raises(ValueError):
+        sw.head_norm_fwd(q[:, 0], k[:, 0], inv_freq=f)  # single tokens of no position
+    with pytest.raises(ValueError):
+        sw.head_norm_bwd(q[:, :3], k, q, k)
+    wide = torch.zeros(1, 1, 1, 257, device="cuda")
+    with pytest.raises(sw.ScanWeaverError) as e:
+        sw.head_norm_fwd(wide, wide)
+    assert e.value.status == 2
