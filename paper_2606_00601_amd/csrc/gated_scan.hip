@@ -1,198 +1,256 @@
-// gated_scan.hip -- the gated linear recurrence: forward, backward and one step.
-#include "gated_math.h"
-#include "gated_scan.h"
+// gated_scan.hip -- the gated linear recurrence: forward and one step.
+#include "gated_walk.h"
 #include "norm_rows.h"
 
 namespace sw {
 namespace gated {
 namespace {
 
-__device__ __forceinline__ float get(const StepRows& t, int64_t j, const float*) {
-  return ((const float*)t.p)[j];
-}
-__device__ __forceinline__ float get(const StepRows& t, int64_t j, const uint16_t*) {
-  return bf16_one(((const uint16_t*)t.p)[j]);
-}
-__device__ __forceinline__ void put(void* p, int64_t j, float v, const float*) { ((float*)p)[j] = v; }
-__device__ __forceinline__ void put(void* p, int64_t j, float v, const uint16_t*) {
-  ((uint16_t*)p)[j] = (uint16_t)bf16_rne(v);
-}
+// A chunk of 256 steps of a group of channels.
+template <class E, Mode MODE, bool PACKED>
+__global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, int64_t chunks) {
+  constexpr int N = VC<E>, S = FWD_S;
+  __shared__ Pairs<N> sh[SLOTS][LANES], back[SLOTS][LANES];
+  __shared__ Sequences<PACKED ? FWD_STEPS : 1> sq;
+  __shared__ float rates[GROUP<E>];
+  __shared__ uint32_t ticket;
+  const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  uint32_t work = blockIdx.x;
+  if (chunks > 1) {
+    if (threadIdx.x == 0) ticket = atomicAdd(k.ticket, 1u);
+    __syncthreads();
+    work = ticket;
+  }
+  const int64_t chunk = work / (uint32_t)k.groups, group = work % (uint32_t)k.groups;
+  const int64_t per = (a.D + GROUP<E> - 1) / GROUP<E>;
+  const int64_t b = group / per, c0 = group % per * GROUP<E> + lane * N;
+  const int64_t t0 = chunk * FWD_STEPS, left = a.L - t0, steps = left < FWD_STEPS ? left : FWD_STEPS;
+  const int first = slot * S;
+  if constexpr (PACKED) find_sequences(a, t0, sq);
 
-// Steps [first, end) of sequence n, in row b.
-struct Span {
-  int64_t b, first, end;
-};
-__device__ __forceinline__ Span span_of(const GatedArgs& a, int64_t n) {
-  if (!a.cu) return {n, 0, a.L};
-  int64_t f = a.cu[n], e = a.cu[n + 1];
-  f = f < 0 ? 0 : f > a.L ? a.L : f;
-  e = e < f ? f : e > a.L ? a.L : e;
-  return {0, f, e};
-}
-
-// A lane for each sequence and channel, step by step.
-template <class E>
-__global__ __launch_bounds__(64) void fwd_kernel(GatedArgs a, float* all) {
-  const int64_t d = blockIdx.x * 64ll + threadIdx.x;
-  if (d >= a.D) return;
-  const E* type = nullptr;
-  const int64_t nck = (a.L + SW_GATED_CKPT - 1) / SW_GATED_CKPT;
-  const float k = a.B * a.L ? rate_of(a.lam[d], a.c) : 0.0f;
-  for (int64_t n = blockIdx.y; n < a.nseq; n += gridDim.y) {
-    const Span s = span_of(a, n);
-    float h = a.h0 ? a.h0[n * a.D + d] : 0.0f;
-    for (int64_t t = s.first; t < s.end; ++t) {
-      if (a.ckpt && t % SW_GATED_CKPT == 0) a.ckpt[(s.b * nck + t / SW_GATED_CKPT) * a.D + d] = h;
-      float f, u;
-      pair_of<E>(get(a.x, s.b * a.x.sb + t * a.x.sl + d, type),
-                 get(a.r, s.b * a.r.sb + t * a.r.sl + d, type),
-                 get(a.i, s.b * a.i.sb + t * a.i.sl + d, type), k, f, u);
-      h = __builtin_fmaf(f, h, u);
-      if (all) all[(s.b * a.L + t) * a.D + d] = h;
-      if (a.h) put(a.h, (s.b * a.L + t) * a.D + d, h, type);
+  Rows<E, MODE> x, r, i;
+  x.init(a.x.p, b * a.x.sb + t0 * a.x.sl, a.x.sl, steps, a.D, first, c0);
+  r.init(a.r.p, b * a.r.sb + t0 * a.r.sl, a.r.sl, steps, a.D, first, c0);
+  i.init(a.i.p, b * a.i.sb + t0 * a.i.sl, a.i.sl, steps, a.D, first, c0);
+  const int nrate = (int)(a.D - (c0 - lane * N) < GROUP<E> ? a.D - (c0 - lane * N) : GROUP<E>);
+  if (threadIdx.x < GROUP<E>)
+    rates[threadIdx.x] =
+        (int)threadIdx.x < nrate && a.L > 0 ? rate_of(a.lam[c0 - lane * N + threadIdx.x], a.c) : 0.0f;
+  // pairs of this lane's steps; past the row's end they do not matter
+  float A[S][N], U[S][N];
+  Pairs<N> own;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    own.A[c] = 1.0f;
+    own.U[c] = 0.0f;
+  }
+  constexpr int BATCH = 8;  // steps whose loads are in flight together
+  float rate[N];
+#pragma unroll
+  for (int j0 = 0; j0 < S; j0 += BATCH) {
+    uint32_t xw[BATCH], rw[BATCH], iw[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      xw[j] = x.get(j0 + j);
+      rw[j] = r.get(j0 + j);
+      iw[j] = i.get(j0 + j);
     }
-    if (a.h_last) a.h_last[n * a.D + d] = h;
+    if (j0 == 0) {
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < N; ++c) rate[c] = rates[lane * N + c];
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        float f, u;
+        pair_of<E>(channel<E>(xw[j], c), channel<E>(rw[j], c), channel<E>(iw[j], c), rate[c], f, u);
+        if constexpr (PACKED) {
+          const int n = sq.seq[first + j0 + j];
+          if (n < 0) {
+            f = -1.0f;
+            u = 0.0f;
+          } else if (sq.first[first + j0 + j]) {
+            if (a.h0 && c0 + c < a.D) u = __builtin_fmaf(f, a.h0[n * a.D + c0 + c], u);
+            f = -1.0f;
+          }
+        }
+        A[j0 + j][c] = f;
+        U[j0 + j][c] = u;
+        own.U[c] = apply<PACKED>(f, u, own.U[c]);
+        if constexpr (PACKED)
+          own.A[c] = f < 0.0f || own.A[c] < 0.0f ? -1.0f : own.A[c] * f;
+        else
+          own.A[c] *= f;
+      }
+    }
+  }
+  sh[slot][lane] = own;
+  __syncthreads();
+  Pairs<N> before;  // the chunk's steps before this slot
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    before.A[c] = 1.0f;
+    before.U[c] = 0.0f;
+  }
+  for (int s = 0; s < slot; ++s) after<PACKED>(before, sh[s][lane]);
+
+  float start[N], in[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+    start[c] = !PACKED && a.h0 && c0 + c < a.D ? a.h0[b * a.D + c0 + c] : 0.0f;
+  if (chunks > 1) {
+    Pairs<N> all = before;
+    unsigned long long* w = word_at<E>(k, chunk, group, lane);
+    bool end[N];
+    const bool publishes = slot == SLOTS - 1 && chunk + 1 < chunks;
+    if (publishes) {
+      after<PACKED>(all, own);
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        end[c] = chunk == 0 || all.A[c] < 0.0f;
+        if (chunk == 0) all.U[c] = apply<PACKED>(all.A[c], all.U[c], start[c]);
+      }
+      publish<E>(w, all, end);
+    }
+    look_back<E>(k, chunk, group, slot, lane, start, back, in);
+    if (publishes)
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+        if (!end[c]) carry_put(w + c, CARRY_INC, __float_as_uint(__builtin_fmaf(all.A[c], in[c], all.U[c])));
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; ++c) in[c] = start[c];
+  }
+
+  float h[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c) h[c] = apply<PACKED>(before.A[c], before.U[c], in[c]);
+  if (a.ckpt && first % BWD_STEPS == 0 && first < steps) {
+    const int64_t row = b * ((a.L + BWD_STEPS - 1) / BWD_STEPS) + (t0 + first) / BWD_STEPS;
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+      if (c0 + c < a.D) a.ckpt[row * a.D + c0 + c] = h[c];
+  }
+  Rows<E, MODE> out;
+  out.init_out(a.h, (b * a.L + t0) * a.D, a.h ? steps : 0, a.D, first, c0);
+#pragma unroll
+  for (int j = 0; j < S; ++j) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) h[c] = apply<PACKED>(A[j][c], U[j][c], h[c]);
+    out.put(j, h);
+    if (PACKED ? sq.last[first + j] && a.h_last : a.h_last && t0 + first + j == a.L - 1) {
+      const int64_t n = PACKED ? sq.seq[first + j] : b;
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+        if (c0 + c < a.D) a.h_last[n * a.D + c0 + c] = h[c];
+    }
+  }
+  // sequences of no steps
+  if (a.h_last) {
+    if constexpr (PACKED) {
+      for (int64_t n = chunk + slot * chunks; n < a.nseq; n += chunks * SLOTS)
+        if (edge(a, n) >= edge(a, n + 1))
+#pragma unroll
+          for (int c = 0; c < N; ++c)
+            if (c0 + c < a.D) a.h_last[n * a.D + c0 + c] = a.h0 ? a.h0[n * a.D + c0 + c] : 0.0f;
+    } else if (a.L == 0 && slot == 0) {
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+        if (c0 + c < a.D) a.h_last[b * a.D + c0 + c] = start[c];
+    }
   }
 }
 
-template <class E>
-__global__ __launch_bounds__(64) void bwd_kernel(GatedArgs a, const float* all, float* part) {
-  const int64_t d = blockIdx.x * 64ll + threadIdx.x;
-  if (d >= a.D) return;
-  const E* type = nullptr;
-  const float k = a.B * a.L ? rate_of(a.lam[d], a.c) : 0.0f;
-  float sum = 0.0f;
-  for (int64_t n = blockIdx.y; n < a.nseq; n += gridDim.y) {
-    const Span s = span_of(a, n);
-    float g = a.dh_last ? a.dh_last[n * a.D + d] : 0.0f;
-    const float h0 = a.h0 ? a.h0[n * a.D + d] : 0.0f;
-    for (int64_t t = s.end - 1; t >= s.first; --t) {
-      const float x = get(a.x, s.b * a.x.sb + t * a.x.sl + d, type);
-      const Step p = step_of<E>(x, get(a.r, s.b * a.r.sb + t * a.r.sl + d, type),
-                                get(a.i, s.b * a.i.sb + t * a.i.sl + d, type), k);
-      const int64_t o = (s.b * a.L + t) * a.D + d;
-      const float prev = t > s.first ? all[o - a.D] : h0;
-      g += get(a.dh, s.b * a.dh.sb + t * a.dh.sl + d, type);
-      const float gx = g * p.b * p.si;
-      const float e = g * (p.q * p.si * x - (p.m < 1e3f ? p.m : 1e3f) * p.a * prev);
-      put(a.dx, o, gx, type);
-      put(a.di, o, gx * x * p.rest_i, type);
-      put(a.dr, o, e * p.rest_r, type);
-      sum += e;
-      g *= p.a;
-    }
-    if (a.dh0) a.dh0[n * a.D + d] = g;
-  }
-  part[blockIdx.y * a.D + d] = sum * (a.B * a.L ? rate_slope(a.lam[d]) : 0.0f);
-}
-
-// Zero in up to three (L, D) arrays at the steps that no sequence covers.
-template <class E>
-__global__ __launch_bounds__(256) void uncovered_kernel(GatedArgs a, E* p, E* q, E* r) {
-  int64_t f = a.cu[0], e = a.cu[a.nseq];
-  f = f < 0 ? 0 : f > a.L ? a.L : f;
-  e = e < f ? f : e > a.L ? a.L : e;
-  for (int64_t t = blockIdx.x; t < a.L; t += gridDim.x) {
-    if (t >= f && t < e) continue;
-    for (int64_t d = threadIdx.x; d < a.D; d += 256) {
-      if (p) p[t * a.D + d] = 0;
-      if (q) q[t * a.D + d] = 0;
-      if (r) r[t * a.D + d] = 0;
-    }
-  }
-}
-
+// A token of each sequence: bound by memory, or by the launch.
 template <class E>
 __global__ __launch_bounds__(256) void step_kernel(GatedStepArgs a) {
-  const E* type = nullptr;
   const int64_t d = blockIdx.x * 256ll + threadIdx.x;
   if (d >= a.D) return;
   const float k = rate_of(a.lam[d], a.c);
+  const auto value = [](const void* p, int64_t j) {
+    if constexpr (sizeof(E) == 4)
+      return ((const float*)p)[j];
+    else
+      return bf16_one(((const uint16_t*)p)[j]);
+  };
   for (int64_t b = blockIdx.y; b < a.B; b += gridDim.y) {
     const int64_t slot = a.slots ? a.slots[b] : b;
     float h = 0.0f;
     if (slot >= 0 && slot < a.pool) {
       float f, u;
-      pair_of<E>(get({a.x, 0, 0}, b * a.x_st + d, type), get({a.r, 0, 0}, b * a.r_st + d, type),
-                 get({a.i, 0, 0}, b * a.i_st + d, type), k, f, u);
+      pair_of<E>(value(a.x, b * a.x_st + d), value(a.r, b * a.r_st + d), value(a.i, b * a.i_st + d), k,
+                 f, u);
       float* s = a.state + slot * a.D + d;
       h = __builtin_fmaf(f, *s, u);
       *s = h;
     }
-    put(a.h, b * a.D + d, h, type);
+    if constexpr (sizeof(E) == 4)
+      ((float*)a.h)[b * a.D + d] = h;
+    else
+      ((uint16_t*)a.h)[b * a.D + d] = (uint16_t)bf16_rne(h);
   }
-}
-
-constexpr int64_t ROWS = 256;
-unsigned rows_of(int64_t n) { return (unsigned)(n < ROWS ? n : ROWS); }
-
-template <class E>
-int run_fwd(const GatedArgs& a, float* all, hipStream_t s) {
-  hipLaunchKernelGGL(fwd_kernel<E>, dim3((unsigned)((a.D + 63) / 64), rows_of(a.nseq)), dim3(64), 0, s,
-                     a, all);
-  int st = check_launch("fwd_kernel");
-  if (st == SW_OK && a.cu && a.h && a.L > 0) {
-    hipLaunchKernelGGL(uncovered_kernel<E>, dim3((unsigned)(a.L < 1024 ? a.L : 1024)), dim3(256), 0,
-                       s, a, (E*)a.h, (E*)nullptr, (E*)nullptr);
-    st = check_launch("uncovered_kernel");
-  }
-  return st;
-}
-
-template <class E>
-int run_bwd(const GatedArgs& a, float* ws, hipStream_t s) {
-  int st;
-  GatedArgs f = a;
-  f.h_last = nullptr;
-  if ((st = run_fwd<E>(f, ws, s)) != SW_OK) return st;
-  float* part = ws + a.B * a.L * a.D;
-  hipLaunchKernelGGL(bwd_kernel<E>, dim3((unsigned)((a.D + 63) / 64), rows_of(a.nseq)), dim3(64), 0, s,
-                     a, ws, part);
-  if ((st = check_launch("bwd_kernel")) != SW_OK) return st;
-  if (a.cu && a.L > 0) {
-    hipLaunchKernelGGL(uncovered_kernel<E>, dim3((unsigned)(a.L < 1024 ? a.L : 1024)), dim3(256), 0,
-                       s, a, (E*)a.dx, (E*)a.dr, (E*)a.di);
-    if ((st = check_launch("uncovered_kernel")) != SW_OK) return st;
-  }
-  float* outs[1] = {a.dlam};
-  return norm::fold_partials(part, rows_of(a.nseq), a.D, outs, 1, s);
 }
 
 }  // namespace
+
+int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
+  const int64_t chunks = chunks_of(a.L, FWD_STEPS), groups = groups_of(a.B, a.D, a.bf16);
+  if (chunks * groups > SW_MAX_WGS / 2)
+    return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
+                (long long)(chunks * groups));
+  int st;
+  if (chunks > 1 &&
+      (st = zero_words((uint32_t*)ws, (size_t)words_bytes(a.B, a.D, chunks, a.bf16) / 4, s)) != SW_OK)
+    return st;
+  const Words k = {(uint32_t*)ws, (unsigned long long*)((char*)ws + 64), groups};
+  const StepRows* rows[3] = {&a.x, &a.r, &a.i};
+  const void* outs[1] = {a.h};
+  const Mode mode = mode_of(a, rows, 3, outs, 1);
+#define CALL(MODE, PACKED)                                                                          \
+  do {                                                                                              \
+    if (a.bf16)                                                                                     \
+      hipLaunchKernelGGL((fwd_kernel<uint16_t, MODE, PACKED>), dim3((unsigned)(chunks * groups)),   \
+                         dim3(THREADS), 0, s, a, k, chunks);                                        \
+    else                                                                                            \
+      hipLaunchKernelGGL((fwd_kernel<float, MODE, PACKED>), dim3((unsigned)(chunks * groups)),      \
+                         dim3(THREADS), 0, s, a, k, chunks);                                        \
+  } while (0)
+  SW_GATED_PICK(mode, a.cu != nullptr, CALL);
+#undef CALL
+  return check_launch("gated fwd_kernel");
+}
+
 }  // namespace gated
 
 using namespace gated;
 
-int64_t gated_scan_fwd_workspace(int64_t, int64_t, int64_t) { return 0; }
-int64_t gated_scan_bwd_workspace(int64_t B, int64_t L, int64_t D, bool) {
-  return (B * L + ROWS) * D * 4;
+int64_t gated_scan_fwd_workspace(int64_t B, int64_t L, int64_t D) {
+  // of either type: fp32's groups are half as wide, its words as many
+  const int64_t chunks = chunks_of(L, FWD_STEPS), f = words_bytes(B, D, chunks, false);
+  const int64_t h = words_bytes(B, D, chunks, true);
+  return f > h ? f : h;
 }
 
 int gated_scan_fwd(const GatedArgs& a) {
   if (a.nseq == 0) return SW_OK;
   const hipStream_t s = current_stream();
-  return a.bf16 ? run_fwd<uint16_t>(a, nullptr, s) : run_fwd<float>(a, nullptr, s);
-}
-
-int gated_scan_bwd(const GatedArgs& a) {
-  const hipStream_t s = current_stream();
-  float* outs[1] = {a.dlam};
-  if (a.nseq == 0) return norm::fold_partials(nullptr, 0, a.D, outs, 1, s);
   norm::Partials ws(s);
   int st;
-  if ((st = ws.get(a.ws, a.ws_bytes, (size_t)gated_scan_bwd_workspace(a.B, a.L, a.D, false), "sw_gated_scan_bwd")) != SW_OK)
-    return st;
-  return a.bf16 ? run_bwd<uint16_t>(a, ws.p, s) : run_bwd<float>(a, ws.p, s);
+  const int64_t need = words_bytes(a.B, a.D, chunks_of(a.L, FWD_STEPS), a.bf16);
+  if (need > 0 && (st = ws.get(a.ws, a.ws_bytes, (size_t)need, "sw_gated_scan_fwd")) != SW_OK) return st;
+  return run_fwd(a, ws.p, s);
 }
 
 int gated_scan_step(const GatedStepArgs& a) {
   const hipStream_t s = current_stream();
-  const dim3 grid((unsigned)((a.D + 255) / 256), rows_of(a.B));
+  const dim3 grid((unsigned)((a.D + 255) / 256), (unsigned)(a.B < 65535 ? a.B : 65535));
   if (a.bf16)
     hipLaunchKernelGGL(step_kernel<uint16_t>, grid, dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL(step_kernel<float>, grid, dim3(256), 0, s, a);
-  return check_launch("step_kernel");
+  return check_launch("gated step_kernel");
 }
 
 }  // namespace sw
