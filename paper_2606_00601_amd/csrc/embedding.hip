@@ -1,6 +1,6 @@
-// embedding.hip -- rows of a table by token, and the table's gradient.
+// embedding.hip -- rows of a table by token.
 #include "norm_rows.h"
-#include "token_ops.h"
+#include "token_rows.h"
 
 namespace sw {
 namespace embed {
@@ -8,12 +8,6 @@ namespace {
 
 using norm::load8;
 using norm::store8;
-
-// The token as a row of the table, or V where it is none.
-__device__ __forceinline__ uint32_t row_of(const EmbedArgs& a, int64_t t) {
-  const int64_t v = a.wide ? ((const int64_t*)a.tokens)[t] : ((const int32_t*)a.tokens)[t];
-  return v >= 0 && v < a.V ? (uint32_t)v : (uint32_t)a.V;
-}
 
 // A wave's LPR lanes copy a row, 8 columns a lane at a time.  Bound by memory.
 template <class E, class Y, int LPR>
@@ -31,23 +25,6 @@ __global__ __launch_bounds__(256) void fwd_kernel(EmbedArgs a, bool vec) {
       store8((Y*)a.y + t * a.D + c, x, a.D - c, vec);
     }
   }
-}
-
-// A workgroup for each row of the table, which looks through all tokens.
-template <class E, class Y>
-__global__ __launch_bounds__(256) void bwd_kernel(EmbedArgs a) {
-  for (int64_t v = blockIdx.x; v < a.V; v += gridDim.x)
-    for (int64_t c = threadIdx.x; c < a.D; c += 256) {
-      float s = 0.0f;
-      for (int64_t t = 0; t < a.T; ++t)
-        if (row_of(a, t) == v) {
-          float x[8];
-          load8((const Y*)a.dy + t * a.dy_st + c, x, 1, false);
-          s += x[0];
-        }
-      const float y[8] = {s * a.scale};
-      store8((E*)a.dtable + v * a.D + c, y, 1, false);
-    }
 }
 
 template <class E, class Y>
@@ -72,18 +49,10 @@ int fwd_typed(const EmbedArgs& a, bool vec, int cus, hipStream_t s) {
   return check_launch("embedding fwd_kernel");
 }
 
-template <class E, class Y>
-int bwd_typed(const EmbedArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((bwd_kernel<E, Y>), dim3((unsigned)(a.V < 65536 ? a.V : 65536)), dim3(256), 0, s, a);
-  return check_launch("embedding bwd_kernel");
-}
-
 }  // namespace
 }  // namespace embed
 
 using namespace embed;
-
-int64_t embedding_bwd_workspace(int64_t, int64_t, int64_t) { return 0; }
 
 int embedding_fwd(const EmbedArgs& a) {
   int cus, st;
@@ -93,13 +62,6 @@ int embedding_fwd(const EmbedArgs& a) {
   if (a.table_bf16)
     return a.y_bf16 ? fwd_typed<uint16_t, uint16_t>(a, vec, cus, s) : fwd_typed<uint16_t, float>(a, vec, cus, s);
   return a.y_bf16 ? fwd_typed<float, uint16_t>(a, vec, cus, s) : fwd_typed<float, float>(a, vec, cus, s);
-}
-
-int embedding_bwd(const EmbedArgs& a) {
-  const hipStream_t s = current_stream();
-  if (a.table_bf16)
-    return a.y_bf16 ? bwd_typed<uint16_t, uint16_t>(a, s) : bwd_typed<uint16_t, float>(a, s);
-  return a.y_bf16 ? bwd_typed<float, uint16_t>(a, s) : bwd_typed<float, float>(a, s);
 }
 
 }  // namespace sw
