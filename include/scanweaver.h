@@ -624,7 +624,7 @@ int sw_gated_norm_bwd(const void* dy, const void* x, const void* z, const float*
  * pool for the call (no capture then).  Results do not depend on it; every call
  * of the same inputs gives the same bits.
  */
-enum { SW_GATED_CKPT = 128 };
+enum { SW_GATED_CKPT = 64 };
 int sw_gated_scan_fwd(const void* x, const void* r, const void* i, const float* lam,
                       const float* h0, const int32_t* cu_seqlens, void* h, float* h_last,
                       float* ckpt, int64_t B, int64_t L, int64_t D, int64_t nseq,

@@ -21,7 +21,7 @@ SW_DTYPE_BF16 = 1
 SW_DELTA_SOFTPLUS = 1
 SW_LINEAR_G_HEAD = 1
 SW_GATE_AFTER = 1
-SW_GATED_CKPT = 128
+SW_GATED_CKPT = 64
 SW_HEAD_ADJACENT = 1
 SW_HEAD_POS_I64 = 2
 SW_EMBED_TOKENS_I64 = 1

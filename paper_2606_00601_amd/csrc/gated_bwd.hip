@@ -1,6 +1,6 @@
 // gated_bwd.hip -- the gated linear recurrence: backward.
 //
-// The states before the backward's chunks of 128 steps are what a training forward kept, so
+// The states before the backward's chunks of 64 steps are what a training forward kept, so
 // a chunk's own are formed from its registers alone.  The gradient's recurrence runs the
 // other way, over v_t = a_t g_t, what step t hands to the one before it:
 //   v_t = a_t (dh_t + v_{t+1}),
@@ -13,30 +13,33 @@ namespace gated {
 namespace {
 
 template <class E, Mode MODE, bool PACKED>
-__global__ __launch_bounds__(THREADS, sizeof(E) == 4 ? 4 : 2) void bwd_kernel(GatedArgs a, const float* ckpt, float* part,
+__global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const float* ckpt, float* part,
                                                          Words k, int64_t chunks) {
-  constexpr int N = VC<E>, S = BWD_S;
-  __shared__ Pairs<N> sh[SLOTS][LANES], sg[SLOTS][LANES];
+  using G = BwdShape;
+  constexpr int S = BWD_S, SLOTS = G::SLOTS;
+  __shared__ Pairs<1> sh[LOOK][G::LANES], sg[SLOTS][G::LANES];
   __shared__ Sequences<PACKED ? BWD_STEPS : 1> sq;
-  __shared__ float rates[GROUP<E>];
+  __shared__ float rates[G::GROUP];
   __shared__ uint32_t ticket;
-  const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int slot = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G::LANES);
+  const int lane = threadIdx.x % G::LANES;
   uint32_t work = blockIdx.x;
   if (chunks > 1) {
     if (threadIdx.x == 0) ticket = atomicAdd(k.ticket, 1u);
     __syncthreads();
-    work = ticket;
+    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
   }
   // `turn` counts the chunks from the last one on
   const int64_t turn = work / (uint32_t)k.groups, group = work % (uint32_t)k.groups;
   const int64_t chunk = chunks - 1 - turn;
-  const int64_t per = (a.D + GROUP<E> - 1) / GROUP<E>;
-  const int64_t b = group / per, base = group % per * GROUP<E>, c0 = base + lane * N;
-  const int64_t t0 = chunk * BWD_STEPS, left = a.L - t0, steps = left < BWD_STEPS ? left : BWD_STEPS;
-  const int first = slot * S;
+  const int64_t per = (a.D + G::GROUP - 1) / G::GROUP;
+  const int64_t b = group / per, base = group % per * G::GROUP, c0 = base + lane;
+  const int64_t t0 = chunk * BWD_STEPS, left = a.L - t0;
+  const int steps = (int)(left < BWD_STEPS ? left : BWD_STEPS), first = slot * S;
+  const bool there = c0 < a.D;
   if constexpr (PACKED) find_sequences(a, t0, sq);
 
-  Rows<E, MODE> x, r, i, d;
+  Rows<E, MODE, 1> x, r, i, d;
   x.init(a.x.p, b * a.x.sb + t0 * a.x.sl, a.x.sl, steps, a.D, first, c0);
   r.init(a.r.p, b * a.r.sb + t0 * a.r.sl, a.r.sl, steps, a.D, first, c0);
   i.init(a.i.p, b * a.i.sb + t0 * a.i.sl, a.i.sl, steps, a.D, first, c0);
@@ -49,185 +52,135 @@ __global__ __launch_bounds__(THREADS, sizeof(E) == 4 ? 4 : 2) void bwd_kernel(Ga
     iw[j] = i.get(j);
     dw[j] = d.get(j);
   }
-  float start[N], in[N], tail[N];
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    const bool there = c0 + c < a.D;
-    start[c] = there ? ckpt[(b * chunks + chunk) * a.D + c0 + c] : 0.0f;
-    tail[c] = !PACKED && a.dh_last && there ? a.dh_last[b * a.D + c0 + c] : 0.0f;
-  }
-  if (threadIdx.x < GROUP<E>)
-    rates[threadIdx.x] = base + threadIdx.x < a.D ? rate_of(a.lam[base + threadIdx.x], a.c) : 0.0f;
+  const float start = there ? ckpt[(b * chunks + chunk) * a.D + c0] : 0.0f;
+  float tail = !PACKED && a.dh_last && there ? a.dh_last[b * a.D + c0] : 0.0f;
+  if (slot == 0) rates[lane] = there ? rate_of(a.lam[c0], a.c) : 0.0f;
   __syncthreads();
+  const float rate = rates[lane];
 
-  // of each step: a, b s, (m / b) a^2 s x, m a, 1 - sigmoid(r), (1 - s) x, dh
-  float A[S][N], bs[S][N], q[S][N], ma[S][N], rest[S][N], xi[S][N], dh[S][N];
-  float h0[PACKED ? S : 1][N];  // PACKED: the state before a sequence's first step
+  // of each step: a, b s, (m / b) a^2 s x, m a, 1 - sigmoid(r), (1 - s) x, u, dh
+  float A[S], bs[S], q[S], ma[S], rest[S], xi[S], u[S], dh[S];
   uint32_t none = 0, starts = 0, ends = 0;  // PACKED: steps of no sequence, first and last ones
-  Pairs<N> fwd, bwd;
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    fwd.A[c] = bwd.A[c] = 1.0f;
-    fwd.U[c] = bwd.U[c] = 0.0f;
-  }
+  Pairs<1> fwd = {{1.0f}, {0.0f}}, bwd = fwd;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
-    int n = 0;
+    const float xv = channel<E>(xw[j], 0);
+    const Step s = step_of<E>(xv, channel<E>(rw[j], 0), channel<E>(iw[j], 0), rate);
+    A[j] = s.a;
+    bs[j] = s.bs;
+    q[j] = s.q;
+    ma[j] = s.ma;
+    rest[j] = s.rest_r;
+    xi[j] = xv * s.rest_i;
+    u[j] = s.bs * xv;
+    dh[j] = channel<E>(dw[j], 0);
+    float f = s.a;
     if constexpr (PACKED) {
-      n = sq.seq[first + j];
-      none |= (uint32_t)(n < 0) << j;
-      starts |= (uint32_t)sq.first[first + j] << j;
-      ends |= (uint32_t)sq.last[first + j] << j;
-    }
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const float xv = channel<E>(xw[j], c);
-      const Step s = step_of<E>(xv, channel<E>(rw[j], c), channel<E>(iw[j], c), rates[lane * N + c]);
-      A[j][c] = s.a;
-      bs[j][c] = s.b * s.si;
-      q[j][c] = s.q * s.si * xv;
-      ma[j][c] = (s.m < 1e3f ? s.m : 1e3f) * s.a;
-      rest[j][c] = s.rest_r;
-      xi[j][c] = xv * s.rest_i;
-      dh[j][c] = channel<E>(dw[j], c);
-      float f = s.a, u = s.u;
-      if constexpr (PACKED) {
-        const bool there = c0 + c < a.D;
-        h0[j][c] = 0.0f;
-        if (n < 0) {
-          f = -1.0f;
-          u = 0.0f;
-          A[j][c] = bs[j][c] = q[j][c] = ma[j][c] = rest[j][c] = xi[j][c] = dh[j][c] = 0.0f;
-        } else {
-          if (starts >> j & 1) {
-            if (a.h0 && there) h0[j][c] = a.h0[n * a.D + c0 + c];
-            u = __builtin_fmaf(f, h0[j][c], u);
-            f = -1.0f;
-          }
-          if ((ends >> j & 1) && a.dh_last && there) dh[j][c] += a.dh_last[n * a.D + c0 + c];
-        }
+      const int n = __builtin_amdgcn_readfirstlane(sq.seq[first + j]);
+      if (n < 0) {
+        none |= 1u << j;
+        f = -1.0f;
+        A[j] = bs[j] = q[j] = ma[j] = rest[j] = xi[j] = u[j] = dh[j] = 0.0f;
       } else {
-        // past the row's end (rows of stride 0 are read there again) nothing is added, and
-        // what comes in passes through
-        if (first + j >= steps) {
-          f = A[j][c] = 1.0f;
-          dh[j][c] = 0.0f;
+        const int at = __builtin_amdgcn_readfirstlane((int)sq.ends[first + j]);
+        if (at & 1) {
+          starts |= 1u << j;
+          // the state before is known: what it adds is a constant
+          u[j] = __builtin_fmaf(f, a.h0 && there ? a.h0[n * a.D + c0] : 0.0f, u[j]);
+          f = -1.0f;
+        }
+        if (at & 2) {
+          ends |= 1u << j;
+          if (a.dh_last && there) dh[j] += a.dh_last[n * a.D + c0];
         }
       }
-      fwd.U[c] = apply<PACKED>(f, u, fwd.U[c]);
-      fwd.A[c] = PACKED && (f < 0.0f || fwd.A[c] < 0.0f) ? -1.0f : fwd.A[c] * f;
+    } else if (first + j >= steps) {
+      // past the row's end (rows of stride 0 are read there again) nothing is added, and
+      // what comes in passes through
+      f = A[j] = 1.0f;
+      dh[j] = 0.0f;
     }
-  }
-#pragma unroll
-  for (int j = S - 1; j >= 0; --j)
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const bool cut = PACKED && ((ends | none) >> j & 1);
-      bwd.U[c] = A[j][c] * (dh[j][c] + (cut ? 0.0f : bwd.U[c]));
-      bwd.A[c] = cut || (PACKED && bwd.A[c] < 0.0f) ? -1.0f : bwd.A[c] * A[j][c];
-    }
-  sh[slot][lane] = fwd;
-  sg[slot][lane] = bwd;
-  __syncthreads();
-  Pairs<N> before, behind;
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    before.A[c] = behind.A[c] = 1.0f;
-    before.U[c] = behind.U[c] = 0.0f;
-  }
-  for (int s = 0; s < slot; ++s) after<PACKED>(before, sh[s][lane]);
-  for (int s = SLOTS - 1; s > slot; --s) after<PACKED>(behind, sg[s][lane]);
-  // the states before the steps go into what a step's dr is of its g: f = q - m a h
-  float h[N];
-#pragma unroll
-  for (int c = 0; c < N; ++c) h[c] = apply<PACKED>(before.A[c], before.U[c], start[c]);
-#pragma unroll
-  for (int j = 0; j < S; ++j)
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      if (PACKED && (starts >> j & 1)) h[c] = h0[j][c];
-      const float xv = channel<E>(xw[j], c);
-      q[j][c] = __builtin_fmaf(-ma[j][c], h[c], q[j][c]);
-      h[c] = __builtin_fmaf(A[j][c], h[c], bs[j][c] * xv);
-      if (PACKED && (none >> j & 1)) h[c] = q[j][c] = 0.0f;
-    }
-
-  if (chunks > 1) {
-    Pairs<N> all = behind;
-    unsigned long long* w = word_at<E>(k, turn, group, lane);
-    bool end[N];
-    const bool publishes = slot == 0 && chunk > 0;
-    if (publishes) {
-      after<PACKED>(all, bwd);
-#pragma unroll
-      for (int c = 0; c < N; ++c) {
-        end[c] = turn == 0 || all.A[c] < 0.0f;
-        if (turn == 0) all.U[c] = apply<PACKED>(all.A[c], all.U[c], tail[c]);
-      }
-      publish<E>(w, all, end);
-    }
-    look_back<E>(k, turn, group, slot, lane, tail, sh, in);
-    if (publishes)
-#pragma unroll
-      for (int c = 0; c < N; ++c)
-        if (!end[c]) carry_put(w + c, CARRY_INC, __float_as_uint(__builtin_fmaf(all.A[c], in[c], all.U[c])));
-  } else {
-#pragma unroll
-    for (int c = 0; c < N; ++c) in[c] = tail[c];
-  }
-
-  Rows<E, MODE> dx, dr, di;
-  dx.init_out(a.dx, (b * a.L + t0) * a.D, steps, a.D, first, c0);
-  dr.init_out(a.dr, (b * a.L + t0) * a.D, steps, a.D, first, c0);
-  di.init_out(a.di, (b * a.L + t0) * a.D, steps, a.D, first, c0);
-  float v[N], sum[N];
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    v[c] = apply<PACKED>(behind.A[c], behind.U[c], in[c]);
-    sum[c] = 0.0f;
+    fwd.U[0] = apply<PACKED>(f, u[j], fwd.U[0]);
+    fwd.A[0] = PACKED && (f < 0.0f || fwd.A[0] < 0.0f) ? -1.0f : fwd.A[0] * f;
   }
 #pragma unroll
   for (int j = S - 1; j >= 0; --j) {
-    float ox[N], oi[N], orr[N];
+    const bool cut = PACKED && ((ends | none) >> j & 1);
+    bwd.U[0] = A[j] * (dh[j] + (cut ? 0.0f : bwd.U[0]));
+    bwd.A[0] = cut || (PACKED && bwd.A[0] < 0.0f) ? -1.0f : bwd.A[0] * A[j];
+  }
+  sh[slot][lane] = fwd;
+  sg[slot][lane] = bwd;
+  __syncthreads();
+  Pairs<1> before = {{1.0f}, {0.0f}}, behind = before;
+  for (int s = 0; s < slot; ++s) after<PACKED>(before, sh[s][lane]);
+  for (int s = SLOTS - 1; s > slot; --s) after<PACKED>(behind, sg[s][lane]);
+
+  float in = tail;
+  Pairs<1> all = behind;
+  unsigned long long* w = word_at<G>(k, turn, group, lane);
+  bool end = true;
+  const bool publishes = slot == 0 && chunk > 0;
+  if (publishes) {
+    after<PACKED>(all, bwd);
+    end = turn == 0 || all.A[0] < 0.0f;
+    if (turn == 0) all.U[0] = apply<PACKED>(all.A[0], all.U[0], tail);
+    publish<G>(w, all, &end);
+  }
+  // the states before the steps go into what a step's dr is of its g: q - m a h
+  float h = apply<PACKED>(before.A[0], before.U[0], start);
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const bool cut = PACKED && ((ends | none) >> j & 1);
-      const float g = dh[j][c] + (cut ? 0.0f : v[c]);
-      const float e = g * q[j][c];
-      ox[c] = g * bs[j][c];
-      oi[c] = ox[c] * xi[j][c];
-      orr[c] = e * rest[j][c];
-      sum[c] += PACKED || first + j < steps ? e : 0.0f;
-      v[c] = A[j][c] * g;
-    }
-    dx.put(j, ox);
-    di.put(j, oi);
-    dr.put(j, orr);
-    if (a.dh0 && (PACKED ? starts >> j & 1 : t0 + first + j == 0)) {
-      const int64_t n = PACKED ? sq.seq[first + j] : b;
-#pragma unroll
-      for (int c = 0; c < N; ++c)
-        if (c0 + c < a.D) a.dh0[n * a.D + c0 + c] = v[c];
+  for (int j = 0; j < S; ++j) {
+    if (PACKED && (starts >> j & 1)) {
+      h = a.h0 && there ? a.h0[sq.seq[first + j] * a.D + c0] : 0.0f;
+      q[j] = __builtin_fmaf(-ma[j], h, q[j]);
+      h = u[j];
+    } else if (PACKED && (none >> j & 1)) {
+      h = q[j] = 0.0f;
+    } else {
+      q[j] = __builtin_fmaf(-ma[j], h, q[j]);
+      h = __builtin_fmaf(A[j], h, u[j]);
+      if (!PACKED && first + j >= steps) q[j] = 0.0f;
     }
   }
-  if constexpr (PACKED) {
-    if (a.dh0)  // sequences of no steps
-      for (int64_t n = chunk + slot * chunks; n < a.nseq; n += chunks * SLOTS)
-        if (edge(a, n) >= edge(a, n + 1))
+  if (chunks > 1) {
+    look_back<G>(k, turn, group, slot, lane, &tail, sh, &in);
+    if (publishes && !end) carry_put(w, CARRY_INC, __float_as_uint(__builtin_fmaf(all.A[0], in, all.U[0])));
+  }
+
+  Rows<E, MODE, 1> dx, dr, di;
+  dx.init_out(a.dx, (b * a.L + t0) * a.D, steps, a.D, first, c0);
+  dr.init_out(a.dr, (b * a.L + t0) * a.D, steps, a.D, first, c0);
+  di.init_out(a.di, (b * a.L + t0) * a.D, steps, a.D, first, c0);
+  float v = apply<PACKED>(behind.A[0], behind.U[0], in), sum = 0.0f;
 #pragma unroll
-          for (int c = 0; c < N; ++c)
-            if (c0 + c < a.D) a.dh0[n * a.D + c0 + c] = a.dh_last ? a.dh_last[n * a.D + c0 + c] : 0.0f;
+  for (int j = S - 1; j >= 0; --j) {
+    const bool cut = PACKED && ((ends | none) >> j & 1);
+    const float g = dh[j] + (cut ? 0.0f : v);
+    const float e = g * q[j], gx = g * bs[j], gi = gx * xi[j], gr = e * rest[j];
+    sum += e;
+    v = A[j] * g;
+    dx.put(j, &gx);
+    di.put(j, &gi);
+    dr.put(j, &gr);
+    if (a.dh0 && there && (PACKED ? starts >> j & 1 : t0 + first + j == 0))
+      a.dh0[(PACKED ? sq.seq[first + j] : b) * a.D + c0] = v;
+  }
+  if constexpr (PACKED) {
+    if (a.dh0 && there)  // sequences of no steps
+      for (int64_t n = chunk + slot * chunks; n < a.nseq; n += chunks * SLOTS)
+        if (edge(a, n) >= edge(a, n + 1)) a.dh0[n * a.D + c0] = a.dh_last ? a.dh_last[n * a.D + c0] : 0.0f;
   }
   // lam's gradient: the slots' sums in order, then a row of the partial sums for each chunk
   __syncthreads();
-  float(*fold)[GROUP<E>] = (float(*)[GROUP<E>])&sg[0][0];
-#pragma unroll
-  for (int c = 0; c < N; ++c) fold[slot][lane * N + c] = sum[c];
+  float(*fold)[G::GROUP] = (float(*)[G::GROUP])&sg[0][0];
+  fold[slot][lane] = sum;
   __syncthreads();
-  if (threadIdx.x < GROUP<E> && base + threadIdx.x < a.D) {
+  if (slot == 0 && there) {
     float t = 0.0f;
-    for (int s = 0; s < SLOTS; ++s) t += fold[s][threadIdx.x];
-    part[(b * chunks + chunk) * a.D + base + threadIdx.x] = t * rate_slope(a.lam[base + threadIdx.x]);
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) t += fold[s][lane];
+    part[(b * chunks + chunk) * a.D + c0] = t * rate_slope(a.lam[c0]);
   }
 }
 
@@ -242,15 +195,15 @@ int64_t align64(int64_t n) { return (n + 63) / 64 * 64; }
 // The workspace: words (the forward's before the backward's, if states are formed again),
 // partial sums, states.
 struct Layout {
-  int64_t chunks, words, part, states, total;
+  int64_t chunks, groups, words, part, states, total;
 };
-Layout layout_of(int64_t B, int64_t L, int64_t D, bool bf16, bool ckpt) {
+Layout layout_of(const GatedArgs& a, bool ckpt) {
   Layout l;
-  l.chunks = chunks_of(L, BWD_STEPS);
-  const int64_t w = words_bytes(B, D, l.chunks, bf16);
-  const int64_t f = ckpt ? 0 : words_bytes(B, D, chunks_of(L, FWD_STEPS), bf16);
+  l.chunks = chunks_of(a.L, BWD_STEPS);
+  l.groups = groups_of(a.B, a.D, BwdShape::GROUP);
+  const int64_t w = words_bytes(l.chunks, l.groups, BwdShape::GROUP), f = ckpt ? 0 : fwd_words(a);
   l.words = align64(w > f ? w : f);
-  l.part = align64(B * l.chunks * D * 4);
+  l.part = align64(a.B * l.chunks * a.D * 4);
   l.states = ckpt ? 0 : l.part;
   l.total = l.words + l.part + l.states;
   return l;
@@ -262,7 +215,13 @@ Layout layout_of(int64_t B, int64_t L, int64_t D, bool bf16, bool ckpt) {
 using namespace gated;
 
 int64_t gated_scan_bwd_workspace(int64_t B, int64_t L, int64_t D, bool ckpt) {
-  const int64_t f = layout_of(B, L, D, false, ckpt).total, h = layout_of(B, L, D, true, ckpt).total;
+  GatedArgs a;
+  a.B = B;
+  a.L = L;
+  a.D = D;
+  const int64_t f = layout_of(a, ckpt).total;
+  a.bf16 = true;
+  const int64_t h = layout_of(a, ckpt).total;
   return f > h ? f : h;
 }
 
@@ -279,11 +238,10 @@ int gated_scan_bwd(const GatedArgs& a) {
     }
     return norm::fold_partials(nullptr, 0, a.D, outs, 1, s);
   }
-  const Layout l = layout_of(a.B, a.L, a.D, a.bf16, a.ckpt_in != nullptr);
-  const int64_t groups = groups_of(a.B, a.D, a.bf16);
-  if (l.chunks * groups > SW_MAX_WGS / 2)
+  const Layout l = layout_of(a, a.ckpt_in != nullptr);
+  if (l.chunks * l.groups > SW_MAX_WGS / 2)
     return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
-                (long long)(l.chunks * groups));
+                (long long)(l.chunks * l.groups));
   norm::Partials mem(s);
   if ((st = mem.get(a.ws, a.ws_bytes, (size_t)l.total, "sw_gated_scan_bwd")) != SW_OK) return st;
   char* ws = (char*)mem.p;
@@ -297,23 +255,29 @@ int gated_scan_bwd(const GatedArgs& a) {
     if ((st = run_fwd(f, ws, s)) != SW_OK) return st;
     ckpt = f.ckpt;
   }
-  if (l.chunks > 1 &&
-      (st = zero_words((uint32_t*)ws, (size_t)words_bytes(a.B, a.D, l.chunks, a.bf16) / 4, s)) != SW_OK)
-    return st;
-  const Words k = {(uint32_t*)ws, (unsigned long long*)(ws + 64), groups};
+  const int64_t words = words_bytes(l.chunks, l.groups, BwdShape::GROUP);
+  if (words > 0 && (st = zero_words((uint32_t*)ws, (size_t)words / 4, s)) != SW_OK) return st;
+  const Words k = {(uint32_t*)ws, (unsigned long long*)(ws + 64), l.groups};
   const StepRows* rows[4] = {&a.x, &a.r, &a.i, &a.dh};
-  const void* grads[3] = {a.dx, a.dr, a.di};
-  const Mode mode = mode_of(a, rows, 4, grads, 3);
-#define CALL(MODE, PACKED)                                                                          \
-  do {                                                                                              \
-    if (a.bf16)                                                                                     \
-      hipLaunchKernelGGL((bwd_kernel<uint16_t, MODE, PACKED>), dim3((unsigned)(l.chunks * groups)), \
-                         dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks);                          \
-    else                                                                                            \
-      hipLaunchKernelGGL((bwd_kernel<float, MODE, PACKED>), dim3((unsigned)(l.chunks * groups)),    \
-                         dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks);                          \
+  const bool near = near_rows(a, rows, 4, BWD_STEPS);
+  const dim3 grid((unsigned)(l.chunks * l.groups));
+#define CALL(E, MODE)                                                                                    \
+  do {                                                                                                   \
+    if (a.cu)                                                                                            \
+      hipLaunchKernelGGL((bwd_kernel<E, MODE, true>), grid, dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks); \
+    else                                                                                                 \
+      hipLaunchKernelGGL((bwd_kernel<E, MODE, false>), grid, dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks); \
   } while (0)
-  SW_GATED_PICK(mode, a.cu != nullptr, CALL);
+  if (a.bf16) {
+    if (near)
+      CALL(uint16_t, NEAR);
+    else
+      CALL(uint16_t, FAR);
+  } else if (near) {
+    CALL(float, NEAR);
+  } else {
+    CALL(float, FAR);
+  }
 #undef CALL
   if ((st = check_launch("gated bwd_kernel")) != SW_OK) return st;
   return norm::fold_partials(part, a.B * l.chunks, a.D, outs, 1, s);

@@ -31,27 +31,28 @@ __device__ __forceinline__ float sigmoid(float v, float& e) {
   }
   return __builtin_amdgcn_rcpf(1.0f + e);
 }
-// 1 minus it: e s keeps its digits for v > 0, where s nears 1.
-__device__ __forceinline__ float sigmoid_rest(float v, float e, float s) {
-  return v > 0.0f ? e * s : 1.0f - s;
-}
+// 1 minus it, e s, which keeps its digits where s nears 1.  (An infinite e leaves 1; so does
+// a NaN, which s hands on.)
+__device__ __forceinline__ float sigmoid_rest(float e, float s) { return fminf(e * s, 1.0f); }
 
 template <class E>
 __device__ __forceinline__ float one_minus_square(float m, float a) {
-  const float t = m + m;
-  float p;
+  const float rest = __builtin_fmaf(-a, a, 1.0f);
   if constexpr (sizeof(E) == 2) {  // to t^4 / 120 of the value: 2^-19 at the bound
-    p = t * (1.0f - t * (0.5f - t * (1.0f / 6.0f - t * (1.0f / 24.0f))));
-    return t < 0.125f ? p : __builtin_fmaf(-a, a, 1.0f);
+    float p = __builtin_fmaf(m, -2.0f / 3.0f, 4.0f / 3.0f);
+    p = __builtin_fmaf(-m, p, 2.0f);
+    p = m * __builtin_fmaf(-m, p, 2.0f);
+    return m < 0.0625f ? p : rest;
   } else {  // to t^8 / 9!: 2^-26
-    p = __builtin_fmaf(t, -1.0f / 40320.0f, 1.0f / 5040.0f);
+    const float t = m + m;
+    float p = __builtin_fmaf(t, -1.0f / 40320.0f, 1.0f / 5040.0f);
     p = __builtin_fmaf(-t, p, 1.0f / 720.0f);
     p = __builtin_fmaf(-t, p, 1.0f / 120.0f);
     p = __builtin_fmaf(-t, p, 1.0f / 24.0f);
     p = __builtin_fmaf(-t, p, 1.0f / 6.0f);
     p = __builtin_fmaf(-t, p, 0.5f);
     p = t * __builtin_fmaf(-t, p, 1.0f);
-    return t < 0.5f ? p : __builtin_fmaf(-a, a, 1.0f);
+    return m < 0.25f ? p : rest;
   }
 }
 
@@ -79,25 +80,28 @@ __device__ __forceinline__ void pair_of(float x, float r, float i, float k, floa
 
 // What a step's gradients need.
 struct Step {
-  float a, u, b, si, m, q;  // q = (m / b) a^2
-  float rest_r, rest_i;     // 1 - sigmoid(r), 1 - si
+  float a, bs, q, ma;    // bs = b s, q = (m / b) a^2 s x, ma = m a, with s = sigmoid(i)
+  float rest_r, rest_i;  // 1 - sigmoid(r), 1 - s
 };
+// An infinite m is held where a is zero, so that m a is; a z below 2^-122, where 1 / b would
+// be infinite: both products end there as their limits do, at zero.  (A NaN that a minimum or
+// maximum drops is in a or z still.)
 template <class E>
 __device__ __forceinline__ Step step_of(float x, float r, float i, float k) {
-  Step s;
+  Step t;
   float e;
   const float sr = sigmoid<E>(r, e);
-  s.rest_r = sigmoid_rest(r, e, sr);
-  s.m = k * sr;
-  s.a = __builtin_amdgcn_exp2f(-s.m * LOG2E);
-  const float z = one_minus_square<E>(s.m, s.a);
-  const float inv = z < 1e-37f ? 0.0f : __builtin_amdgcn_rsqf(z);
-  s.b = z * inv;
-  s.q = s.m < 1e3f ? s.m * inv * s.a * s.a : 0.0f * s.a;  // m a^2 of an infinite m
-  s.si = sigmoid<E>(i, e);
-  s.rest_i = sigmoid_rest(i, e, s.si);
-  s.u = s.b * s.si * x;
-  return s;
+  t.rest_r = sigmoid_rest(e, sr);
+  const float m = k * sr;
+  t.a = __builtin_amdgcn_exp2f(-m * LOG2E);
+  const float z = one_minus_square<E>(m, t.a);
+  const float inv = __builtin_amdgcn_rsqf(fmaxf(z, 1e-37f));
+  const float si = sigmoid<E>(i, e);
+  t.rest_i = sigmoid_rest(e, si);
+  t.bs = z * inv * si;
+  t.ma = fminf(m, 1e3f) * t.a;
+  t.q = t.ma * t.a * inv * (si * x);
+  return t;
 }
 
 }  // namespace gated

@@ -9,10 +9,11 @@ namespace {
 // A chunk of 256 steps of a group of channels.
 template <class E, Mode MODE, bool PACKED>
 __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, int64_t chunks) {
-  constexpr int N = VC<E>, S = FWD_S;
-  __shared__ Pairs<N> sh[SLOTS][LANES], back[SLOTS][LANES];
+  using G = FwdShape<E>;
+  constexpr int N = G::N, S = FWD_S, LANES = G::LANES, SLOTS = G::SLOTS;
+  __shared__ Pairs<N> sh[SLOTS][LANES], back[LOOK][LANES];
   __shared__ Sequences<PACKED ? FWD_STEPS : 1> sq;
-  __shared__ float rates[GROUP<E>];
+  __shared__ float rates[G::GROUP];
   __shared__ uint32_t ticket;
   const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
   uint32_t work = blockIdx.x;
@@ -22,18 +23,18 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
     work = ticket;
   }
   const int64_t chunk = work / (uint32_t)k.groups, group = work % (uint32_t)k.groups;
-  const int64_t per = (a.D + GROUP<E> - 1) / GROUP<E>;
-  const int64_t b = group / per, c0 = group % per * GROUP<E> + lane * N;
+  const int64_t per = (a.D + G::GROUP - 1) / G::GROUP;
+  const int64_t b = group / per, c0 = group % per * G::GROUP + lane * N;
   const int64_t t0 = chunk * FWD_STEPS, left = a.L - t0, steps = left < FWD_STEPS ? left : FWD_STEPS;
   const int first = slot * S;
   if constexpr (PACKED) find_sequences(a, t0, sq);
 
-  Rows<E, MODE> x, r, i;
+  Rows<E, MODE, N> x, r, i;
   x.init(a.x.p, b * a.x.sb + t0 * a.x.sl, a.x.sl, steps, a.D, first, c0);
   r.init(a.r.p, b * a.r.sb + t0 * a.r.sl, a.r.sl, steps, a.D, first, c0);
   i.init(a.i.p, b * a.i.sb + t0 * a.i.sl, a.i.sl, steps, a.D, first, c0);
-  const int nrate = (int)(a.D - (c0 - lane * N) < GROUP<E> ? a.D - (c0 - lane * N) : GROUP<E>);
-  if (threadIdx.x < GROUP<E>)
+  const int nrate = (int)(a.D - (c0 - lane * N) < G::GROUP ? a.D - (c0 - lane * N) : G::GROUP);
+  if (threadIdx.x < G::GROUP)
     rates[threadIdx.x] =
         (int)threadIdx.x < nrate && a.L > 0 ? rate_of(a.lam[c0 - lane * N + threadIdx.x], a.c) : 0.0f;
   // pairs of this lane's steps; past the row's end they do not matter
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
           if (n < 0) {
             f = -1.0f;
             u = 0.0f;
-          } else if (sq.first[first + j0 + j]) {
+          } else if (sq.first(first + j0 + j)) {
             if (a.h0 && c0 + c < a.D) u = __builtin_fmaf(f, a.h0[n * a.D + c0 + c], u);
             f = -1.0f;
           }
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
     start[c] = !PACKED && a.h0 && c0 + c < a.D ? a.h0[b * a.D + c0 + c] : 0.0f;
   if (chunks > 1) {
     Pairs<N> all = before;
-    unsigned long long* w = word_at<E>(k, chunk, group, lane);
+    unsigned long long* w = word_at<G>(k, chunk, group, lane);
     bool end[N];
     const bool publishes = slot == SLOTS - 1 && chunk + 1 < chunks;
     if (publishes) {
@@ -112,9 +113,9 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
         end[c] = chunk == 0 || all.A[c] < 0.0f;
         if (chunk == 0) all.U[c] = apply<PACKED>(all.A[c], all.U[c], start[c]);
       }
-      publish<E>(w, all, end);
+      publish<G>(w, all, end);
     }
-    look_back<E>(k, chunk, group, slot, lane, start, back, in);
+    look_back<G>(k, chunk, group, slot, lane, start, back, in);
     if (publishes)
 #pragma unroll
       for (int c = 0; c < N; ++c)
@@ -133,14 +134,14 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
     for (int c = 0; c < N; ++c)
       if (c0 + c < a.D) a.ckpt[row * a.D + c0 + c] = h[c];
   }
-  Rows<E, MODE> out;
+  Rows<E, MODE, N> out;
   out.init_out(a.h, (b * a.L + t0) * a.D, a.h ? steps : 0, a.D, first, c0);
 #pragma unroll
   for (int j = 0; j < S; ++j) {
 #pragma unroll
     for (int c = 0; c < N; ++c) h[c] = apply<PACKED>(A[j][c], U[j][c], h[c]);
     out.put(j, h);
-    if (PACKED ? sq.last[first + j] && a.h_last : a.h_last && t0 + first + j == a.L - 1) {
+    if (PACKED ? sq.last(first + j) && a.h_last : a.h_last && t0 + first + j == a.L - 1) {
       const int64_t n = PACKED ? sq.seq[first + j] : b;
 #pragma unroll
       for (int c = 0; c < N; ++c)
@@ -195,29 +196,47 @@ __global__ __launch_bounds__(256) void step_kernel(GatedStepArgs a) {
 
 }  // namespace
 
+constexpr int group_of(bool bf16) { return bf16 ? FwdShape<uint16_t>::GROUP : FwdShape<float>::GROUP; }
+
+int64_t fwd_words(const GatedArgs& a) {
+  const int g = group_of(a.bf16);
+  return words_bytes(chunks_of(a.L, FWD_STEPS), groups_of(a.B, a.D, g), g);
+}
+
 int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
-  const int64_t chunks = chunks_of(a.L, FWD_STEPS), groups = groups_of(a.B, a.D, a.bf16);
+  const int64_t chunks = chunks_of(a.L, FWD_STEPS), groups = groups_of(a.B, a.D, group_of(a.bf16));
   if (chunks * groups > SW_MAX_WGS / 2)
     return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
                 (long long)(chunks * groups));
   int st;
-  if (chunks > 1 &&
-      (st = zero_words((uint32_t*)ws, (size_t)words_bytes(a.B, a.D, chunks, a.bf16) / 4, s)) != SW_OK)
-    return st;
+  if (chunks > 1 && (st = zero_words((uint32_t*)ws, (size_t)fwd_words(a) / 4, s)) != SW_OK) return st;
   const Words k = {(uint32_t*)ws, (unsigned long long*)((char*)ws + 64), groups};
+  // pairs of bf16 channels go in words where every row begins on one
   const StepRows* rows[3] = {&a.x, &a.r, &a.i};
-  const void* outs[1] = {a.h};
-  const Mode mode = mode_of(a, rows, 3, outs, 1);
-#define CALL(MODE, PACKED)                                                                          \
-  do {                                                                                              \
-    if (a.bf16)                                                                                     \
-      hipLaunchKernelGGL((fwd_kernel<uint16_t, MODE, PACKED>), dim3((unsigned)(chunks * groups)),   \
-                         dim3(THREADS), 0, s, a, k, chunks);                                        \
-    else                                                                                            \
-      hipLaunchKernelGGL((fwd_kernel<float, MODE, PACKED>), dim3((unsigned)(chunks * groups)),      \
-                         dim3(THREADS), 0, s, a, k, chunks);                                        \
+  bool whole = a.D % 2 == 0 && (uintptr_t)a.h % 4 == 0;
+  for (const StepRows* x : rows)
+    whole = whole && (uintptr_t)x->p % 4 == 0 && x->sl % 2 == 0 && x->sb % 2 == 0;
+  const Mode mode = !near_rows(a, rows, 3, FWD_STEPS) ? FAR : whole || !a.bf16 ? NEAR : SPLIT;
+  const dim3 grid((unsigned)(chunks * groups));
+#define CALL(E, MODE)                                                                                  \
+  do {                                                                                                 \
+    if (a.cu)                                                                                          \
+      hipLaunchKernelGGL((fwd_kernel<E, MODE, true>), grid, dim3(THREADS), 0, s, a, k, chunks);        \
+    else                                                                                               \
+      hipLaunchKernelGGL((fwd_kernel<E, MODE, false>), grid, dim3(THREADS), 0, s, a, k, chunks);       \
   } while (0)
-  SW_GATED_PICK(mode, a.cu != nullptr, CALL);
+  if (a.bf16) {
+    if (mode == NEAR)
+      CALL(uint16_t, NEAR);
+    else if (mode == SPLIT)
+      CALL(uint16_t, SPLIT);
+    else
+      CALL(uint16_t, FAR);
+  } else if (mode == NEAR) {
+    CALL(float, NEAR);
+  } else {
+    CALL(float, FAR);
+  }
 #undef CALL
   return check_launch("gated fwd_kernel");
 }
@@ -227,9 +246,13 @@ int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
 using namespace gated;
 
 int64_t gated_scan_fwd_workspace(int64_t B, int64_t L, int64_t D) {
-  // of either type: fp32's groups are half as wide, its words as many
-  const int64_t chunks = chunks_of(L, FWD_STEPS), f = words_bytes(B, D, chunks, false);
-  const int64_t h = words_bytes(B, D, chunks, true);
+  GatedArgs a;
+  a.B = B;
+  a.L = L;
+  a.D = D;
+  const int64_t f = fwd_words(a);
+  a.bf16 = true;
+  const int64_t h = fwd_words(a);
   return f > h ? f : h;
 }
 
@@ -238,7 +261,7 @@ int gated_scan_fwd(const GatedArgs& a) {
   const hipStream_t s = current_stream();
   norm::Partials ws(s);
   int st;
-  const int64_t need = words_bytes(a.B, a.D, chunks_of(a.L, FWD_STEPS), a.bf16);
+  const int64_t need = fwd_words(a);
   if (need > 0 && (st = ws.get(a.ws, a.ws_bytes, (size_t)need, "sw_gated_scan_fwd")) != SW_OK) return st;
   return run_fwd(a, ws.p, s);
 }
