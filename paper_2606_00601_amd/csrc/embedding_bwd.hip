@@ -21,7 +21,7 @@ using norm::store8;
 
 constexpr int MAX_BITS = 11, MAX_BINS = 1 << MAX_BITS;
 constexpr int TILE = 1024, MAX_TILES = 128;  // steps a workgroup ranks at a time; workgroups
-constexpr int FIX = 16;                      // pieces a workgroup of the last launch looks at
+constexpr int FIX = 4;                       // pieces a workgroup of the last launch looks at
 
 struct Entry {
   uint32_t row, t;
@@ -78,10 +78,15 @@ __global__ __launch_bounds__(256) void place_kernel(EmbedArgs a, Sort s, Clear z
   uint32_t mine = 0;
   for (int d = tid * per; d < (tid + 1) * per && d < bins; ++d) {
     uint32_t total = 0, before = 0;
-    for (int q = 0; q < s.tiles; ++q) {
-      const uint32_t n = s.hist[(int64_t)q * bins + d];
-      total += n;
-      before += q < (int)blockIdx.x ? n : 0;
+    for (int q = 0; q < s.tiles; q += 16) {
+      uint32_t n[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) n[u] = q + u < s.tiles ? s.hist[(int64_t)(q + u) * bins + d] : 0;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        total += n[u];
+        before += q + u < (int)blockIdx.x ? n[u] : 0;
+      }
     }
     base[d] = mine + before;
     mine += total;
@@ -168,13 +173,20 @@ __global__ __launch_bounds__(256) void sum_kernel(EmbedArgs a, const Entry* sort
       store8((E*)a.dtable + (int64_t)row * a.D + c, acc, left, VEC);
     }
   };
+  Entry next = {};
   for (int64_t i = i0; i < i1 && row != V; i += U) {
     Entry e[U];
     float v[U][8];
+    if (LPR == 64 && (i - i0) % 64 == 0) next = sorted[i + li < i1 ? i + li : i1 - 1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      e[u] = sorted[i + u < i1 ? i + u : i1 - 1];
-      if (LPR == 64) e[u].t = (uint32_t)__builtin_amdgcn_readfirstlane((int)e[u].t);
+      if constexpr (LPR == 64) {  // a wave's piece: 64 entries in one load
+        const int at = (int)(i - i0) % 64 + u;
+        e[u].row = (uint32_t)__builtin_amdgcn_readlane((int)next.row, at);
+        e[u].t = (uint32_t)__builtin_amdgcn_readlane((int)next.t, at);
+      } else {
+        e[u] = sorted[i + u < i1 ? i + u : i1 - 1];
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -196,47 +208,76 @@ __global__ __launch_bounds__(256) void sum_kernel(EmbedArgs a, const Entry* sort
   flush(row != V && i1 < a.T && sorted[i1].row == row);
 }
 
-// The rows that begin in one piece and end in a later one: the first piece's sum and then
-// those of the pieces they reach, dealt to 16 waves, whose sums are added in order.
+// The rows that begin in one piece and end in a later one: the first piece's sum and then, in
+// order, those of the pieces they reach.  Each quarter of a workgroup takes a piece and 512
+// columns; a row over more than SHORT pieces is left to the whole workgroup, whose 16 waves
+// add every 16th piece and then their sums in order.
+constexpr int SHORT = 32;
+template <class E>
+__device__ __forceinline__ void put_row(const EmbedArgs& a, uint32_t row, int64_t c, float v) {
+  v *= a.scale;
+  if constexpr (sizeof(E) == 4)
+    ((float*)a.dtable)[(int64_t)row * a.D + c] = v;
+  else
+    ((uint16_t*)a.dtable)[(int64_t)row * a.D + c] = (uint16_t)bf16_rne(v);
+}
 template <class E>
 __global__ __launch_bounds__(1024) void join_kernel(EmbedArgs a, const Entry* sorted, float* part, int P,
                                                     int64_t pieces) {
   __shared__ float sh[16][512];
-  __shared__ uint32_t found;
+  __shared__ int64_t lengths[FIX];  // of the rows left to all; else 0
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   const int64_t p0 = blockIdx.x * (int64_t)FIX, c0 = blockIdx.y * 512ll;
-  if (wave == 0) {
-    bool starts = false;
-    const int64_t p = p0 + lane, i0 = p * P, i1 = i0 + P;
-    if (lane < FIX && i1 < a.T) {
-      const uint32_t row = sorted[i1 - 1].row;
-      starts = row != (uint32_t)a.V && sorted[i1].row == row &&
-               (sorted[i0].row != row || i0 == 0 || sorted[i0 - 1].row != row);
+  {
+    const int mine = __builtin_amdgcn_readfirstlane(tid / 256);
+    const int64_t p = p0 + mine, i0 = p * P, i1 = i0 + P;
+    int64_t n = 0;  // the pieces that go on with the row follow one another
+    uint32_t row = 0;
+    if (i1 < a.T) {
+      row = sorted[i1 - 1].row;
+      if (row != (uint32_t)a.V && sorted[i1].row == row &&
+          (sorted[i0].row != row || i0 == 0 || sorted[i0 - 1].row != row)) {
+        uint64_t more;
+        do {
+          const int64_t q = p + 1 + n + lane;
+          more = __ballot(q < pieces && sorted[q * P].row == row);
+          n += __popcll(more);
+        } while (more == ~(uint64_t)0);
+      }
     }
-    const uint64_t m = __ballot(starts);
-    if (lane == 0) found = (uint32_t)m;
+    if (tid % 256 == 0) lengths[mine] = n > SHORT ? n : 0;
+    if (n > 0 && n <= SHORT) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t c = c0 + k * 256 + tid % 256;
+        if (c < a.D) {
+          float t = part_of(part, p, 1, a.D)[c];
+          for (int64_t q = 0; q < n; q += 8) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = q + u < n ? part_of(part, p + 1 + q + u, 0, a.D)[c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t += v[u];
+          }
+          put_row<E>(a, row, c, t);
+        }
+      }
+    }
   }
   __syncthreads();
   const bool vec = a.D % 8 == 0;
-  for (uint32_t m = found; m; m &= m - 1) {
-    const int64_t p = p0 + __builtin_ctz(m);
-    const uint32_t row = sorted[(p + 1) * P - 1].row;
-    int64_t n = 0;  // the pieces that go on with the row follow one another
-    for (;;) {
-      const int64_t q = p + 1 + n + tid;
-      const int more = __syncthreads_count(q < pieces && sorted[q * P].row == row);
-      n += more;
-      if (more < 1024) break;
-    }
+  for (int k = 0; k < FIX; ++k) {
+    const int64_t n = lengths[k], p = p0 + k;
+    if (n == 0) continue;
     float acc[8] = {};
     const int64_t c = c0 + lane * 8;
-    for (int64_t q = wave; q < n; q += 16 * 4) {
-      float v[4][8];
+    for (int64_t q = wave; q < n; q += 16 * 8) {
+      float v[8][8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 8; ++u)
         load8(part_of(part, p + 1 + q + 16 * u, 0, a.D) + c, v[u], q + 16 * u < n ? a.D - c : 0, vec);
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 8; ++u)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += v[u][j];
     }
@@ -247,11 +288,7 @@ __global__ __launch_bounds__(1024) void join_kernel(EmbedArgs a, const Entry* so
       float t = part_of(part, p, 1, a.D)[c0 + tid];
 #pragma unroll
       for (int w = 0; w < 16; ++w) t += sh[w][tid];
-      t *= a.scale;
-      if constexpr (sizeof(E) == 4)
-        ((float*)a.dtable)[(int64_t)row * a.D + c0 + tid] = t;
-      else
-        ((uint16_t*)a.dtable)[(int64_t)row * a.D + c0 + tid] = (uint16_t)bf16_rne(t);
+      put_row<E>(a, sorted[(p + 1) * P - 1].row, c0 + tid, t);
     }
     __syncthreads();
   }

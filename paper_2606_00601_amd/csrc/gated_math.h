@@ -10,6 +10,9 @@
 
 #include "sw_internal.h"
 
+// Which products are fused is written out: the same in every instance, whatever its loads.
+#pragma clang fp contract(off)
+
 namespace sw {
 namespace gated {
 

@@ -191,6 +191,10 @@ inline int64_t bwd_blocks(int64_t M, int64_t D, int64_t width, int cus) {
     else { CALL(512, 4); }                     \
   } while (0)
 
+// Sums of partial rows of D, blocks[i] of them for outs[i], one output's behind another's.
+int fold_partial_rows(const float* part, const int64_t* blocks, int64_t D, float* const* outs, int nout,
+                      hipStream_t s);
+// The same number of rows for each.
 int fold_partials(const float* part, int64_t blocks, int64_t D, float* const* outs, int nout,
                   hipStream_t s);
 

@@ -156,13 +156,15 @@ int bwd_typed(const ResNormArgs& a, float* part, int64_t blocks, bool vec, hipSt
 // in a fixed order; of no rows zero.
 struct Outs {
   float* p[2];
+  int64_t first[2], blocks[2];
 };
 __global__ __launch_bounds__(256) void fold_partials_kernel(const float* __restrict__ part,
-                                                            int64_t blocks, int64_t D, Outs outs) {
+                                                            int64_t D, Outs outs) {
   __shared__ float sh[16][17];
   const int col = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int64_t c = blockIdx.x * 16ll + col;
-  const float* p = part + (int64_t)blockIdx.y * blocks * D + c;
+  const int64_t blocks = outs.blocks[blockIdx.y];
+  const float* p = part + outs.first[blockIdx.y] * D + c;
   float s = 0.0f;
   if (c < D) {
     int64_t i = row;
@@ -189,10 +191,20 @@ __global__ __launch_bounds__(256) void fold_partials_kernel(const float* __restr
 
 int fold_partials(const float* part, int64_t blocks, int64_t D, float* const* outs, int nout,
                   hipStream_t s) {
+  const int64_t each[2] = {blocks, blocks};
+  return fold_partial_rows(part, each, D, outs, nout, s);
+}
+
+int fold_partial_rows(const float* part, const int64_t* blocks, int64_t D, float* const* outs, int nout,
+                      hipStream_t s) {
   Outs o{};
-  for (int i = 0; i < nout; ++i) o.p[i] = outs[i];
+  for (int i = 0; i < nout; ++i) {
+    o.p[i] = outs[i];
+    o.blocks[i] = blocks[i];
+    o.first[i] = i ? o.first[i - 1] + blocks[i - 1] : 0;
+  }
   hipLaunchKernelGGL(fold_partials_kernel, dim3((unsigned)((D + 15) / 16), (unsigned)nout), dim3(256),
-                     0, s, part, blocks, D, o);
+                     0, s, part, D, o);
   return check_launch("fold_partials_kernel");
 }
 
