@@ -13,7 +13,6 @@ import torch
 
 from ._bind import _dense_like, _differentiable_once, _need, _on, _ptr
 from ._lib import SW_DTYPE_BF16, SW_DTYPE_F32, SW_GATED_CKPT, check, fast
-from ._linear import _need_rows
 
 _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
 
@@ -25,16 +24,35 @@ def _rate(c):
     return c
 
 
-def _operands(x, r, i, lam, c, h0, cu_seqlens):
+def _same_rows(ts, names, dt, shape):
+    """The strides of tensors of one type and shape, one after the other's, without the
+    last, which is one."""
+    st = ()
+    for t, name in zip(ts, names):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on a GPU (got {t.device})")
+        if t.dtype is not dt:
+            raise TypeError(f"{name} must be {dt} (got {t.dtype})")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+        s = t.stride()
+        if s[-1] != 1 and shape[-1] > 1 and t.numel():
+            raise ValueError(f"{name} must be contiguous along its last dimension")
+        st += s[:-1]
+    return st
+
+
+def _operands(x, r, i, lam, c, h0, cu_seqlens, *dh):
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise ValueError("x must be a (B, L, D) tensor")
     dt = x.dtype
     if dt not in _DTYPES:
         raise TypeError("x must be float32 or bfloat16")
-    B, L, D = x.shape
-    st = _need_rows(x, "x", dt, x.shape)
-    st += _need_rows(r, "r", dt, x.shape)
-    st += _need_rows(i, "i", dt, x.shape)
+    shape = x.shape
+    B, L, D = shape
+    st = _same_rows((x, r, i, *dh), ("x", "r", "i", "dh"), dt, shape)
     _need(lam, "lam", torch.float32, (D,))
     n = B
     if cu_seqlens is not None:
@@ -99,9 +117,8 @@ def gated_scan_bwd(x, r, i, lam, dh, dh_last=None, *, c=8.0, h0=None, cu_seqlens
     ``ckpt`` what a training forward kept (formed again if None).  Returns a dict: dx,
     dr, di in the inputs' type, dlam (D,) and dh0 (n, D) (when ``want_dh0``) in fp32.
     """
-    sizes, st, dt, c = _operands(x, r, i, lam, c, h0, cu_seqlens)
+    sizes, st, dt, c = _operands(x, r, i, lam, c, h0, cu_seqlens, dh)
     B, L, D, n = sizes
-    st += _need_rows(dh, "dh", x.dtype, x.shape)
     if dh_last is not None:
         _need(dh_last, "dh_last", torch.float32, (n, D))
     if ckpt is not None:
@@ -169,8 +186,7 @@ def gated_scan_step(x, r, i, lam, state, *, c=8.0, slots=None, h=None):
     if dt not in _DTYPES:
         raise TypeError("x must be float32 or bfloat16")
     B, D = x.shape
-    st = tuple(_need_rows(t.unsqueeze(1) if isinstance(t, torch.Tensor) and t.dim() == 2 else t, name, dt,
-                          (B, 1, D))[0] for t, name in ((x, "x"), (r, "r"), (i, "i")))
+    st = _same_rows((x, r, i), ("x", "r", "i"), dt, x.shape)
     _need(lam, "lam", torch.float32, (D,))
     if not isinstance(state, torch.Tensor) or state.dim() != 2:
         raise ValueError("state must be a (pool, D) tensor")

@@ -19,11 +19,13 @@ _DTYPES = {torch.float32: SW_DTYPE_F32, torch.bfloat16: SW_DTYPE_BF16}
 
 
 def _heads(t, name, dtype, lead):
-    """(strides over (B, L, heads), heads) of a (*lead, heads, K) tensor; one leading
-    dimension is B, with L = 1."""
-    st = _need_rows(t if len(lead) == 2 else t.unsqueeze(1), name, dtype,
-                    (lead[0], lead[1] if len(lead) == 2 else 1, *t.shape[-2:]))
-    return st
+    """The strides over (B, L, heads) of a (*lead, heads, K) tensor; one leading dimension
+    is B, with L = 1."""
+    if t.dtype is dtype and t.is_cuda and t.stride(-1) == 1:
+        st = t.stride()
+        return st[:-1] if len(lead) == 2 else (st[0], 0, st[1])
+    return _need_rows(t if len(lead) == 2 else t.unsqueeze(1), name, dtype,
+                      (lead[0], lead[1] if len(lead) == 2 else 1, *t.shape[-2:]))
 
 
 def _head_operands(q, k, weight_q, weight_k, positions, inv_freq, adjacent):
