@@ -30,10 +30,9 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
     work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
   }
   // `turn` counts the chunks from the last one on
-  const int64_t turn = work / (uint32_t)k.groups, group = work % (uint32_t)k.groups;
+  const uint32_t turn = work / k.groups, group = work % k.groups;
   const int64_t chunk = chunks - 1 - turn;
-  const int64_t per = (a.D + G::GROUP - 1) / G::GROUP;
-  const int64_t b = group / per, base = group % per * G::GROUP, c0 = base + lane;
+  const int64_t b = group / k.per, base = (int64_t)(group % k.per) * G::GROUP, c0 = base + lane;
   const int64_t t0 = chunk * BWD_STEPS, left = a.L - t0;
   const int steps = (int)(left < BWD_STEPS ? left : BWD_STEPS), first = slot * S;
   const bool there = c0 < a.D;
@@ -44,7 +43,10 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
   r.init(a.r.p, b * a.r.sb + t0 * a.r.sl, a.r.sl, steps, a.D, first, c0);
   i.init(a.i.p, b * a.i.sb + t0 * a.i.sl, a.i.sl, steps, a.D, first, c0);
   d.init(a.dh.p, b * a.dh.sb + t0 * a.dh.sl, a.dh.sl, steps, a.D, first, c0);
-  uint32_t xw[S], rw[S], iw[S], dw[S];
+  const float lam = there ? a.lam[c0] : 0.0f;
+  const float start = there ? ckpt[(b * chunks + chunk) * a.D + c0] : 0.0f;
+  const float tail = !PACKED && a.dh_last && there ? a.dh_last[b * a.D + c0] : 0.0f;
+  Raw<E, 1> xw[S], rw[S], iw[S], dw[S];
 #pragma unroll
   for (int j = 0; j < S; ++j) {
     xw[j] = x.get(j);
@@ -52,20 +54,18 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
     iw[j] = i.get(j);
     dw[j] = d.get(j);
   }
-  const float start = there ? ckpt[(b * chunks + chunk) * a.D + c0] : 0.0f;
-  float tail = !PACKED && a.dh_last && there ? a.dh_last[b * a.D + c0] : 0.0f;
-  if (slot == 0) rates[lane] = there ? rate_of(a.lam[c0], a.c) : 0.0f;
+  if (slot == 0) rates[lane] = there ? rate_of(lam, a.c) : 0.0f;
   __syncthreads();
   const float rate = rates[lane];
 
   // of each step: a, b s, (m / b) a^2 s x, m a, 1 - sigmoid(r), (1 - s) x, u, dh
   float A[S], bs[S], q[S], ma[S], rest[S], xi[S], u[S], dh[S];
   uint32_t none = 0, starts = 0, ends = 0;  // PACKED: steps of no sequence, first and last ones
-  Pairs<1> fwd = {{1.0f}, {0.0f}}, bwd = fwd;
+  Pairs<1> fwd = identity<1>(), bwd = fwd;
 #pragma unroll
   for (int j = 0; j < S; ++j) {
-    const float xv = channel<E>(xw[j], 0);
-    const Step s = step_of<E>(xv, channel<E>(rw[j], 0), channel<E>(iw[j], 0), rate);
+    const float xv = xw[j].get(0);
+    const Step s = step_of<E>(xv, rw[j].get(0), iw[j].get(0), rate);
     A[j] = s.a;
     bs[j] = s.bs;
     q[j] = s.q;
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
     rest[j] = s.rest_r;
     xi[j] = xv * s.rest_i;
     u[j] = s.bs * xv;
-    dh[j] = channel<E>(dw[j], 0);
+    dh[j] = dw[j].get(0);
     float f = s.a;
     if constexpr (PACKED) {
       const int n = __builtin_amdgcn_readfirstlane(sq.seq[first + j]);
@@ -112,9 +112,8 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
   sh[slot][lane] = fwd;
   sg[slot][lane] = bwd;
   __syncthreads();
-  Pairs<1> before = {{1.0f}, {0.0f}}, behind = before;
-  for (int s = 0; s < slot; ++s) after<PACKED>(before, sh[s][lane]);
-  for (int s = SLOTS - 1; s > slot; --s) after<PACKED>(behind, sg[s][lane]);
+  const Pairs<1> before = first_of<PACKED, false, 4>(sh, slot, lane);
+  const Pairs<1> behind = first_of<PACKED, true, 4>(sg, SLOTS - 1 - slot, lane);
 
   float in = tail;
   Pairs<1> all = behind;
@@ -180,7 +179,7 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
     float t = 0.0f;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) t += fold[s][lane];
-    part[(b * chunks + chunk) * a.D + c0] = t * rate_slope(a.lam[c0]);
+    part[(b * chunks + chunk) * a.D + c0] = t * rate_slope(lam);
   }
 }
 
@@ -195,13 +194,15 @@ int64_t align64(int64_t n) { return (n + 63) / 64 * 64; }
 // The workspace: words (the forward's before the backward's, if states are formed again),
 // partial sums, states.
 struct Layout {
+  int group;
   int64_t chunks, groups, words, part, states, total;
 };
 Layout layout_of(const GatedArgs& a, bool ckpt) {
   Layout l;
   l.chunks = chunks_of(a.L, BWD_STEPS);
-  l.groups = groups_of(a.B, a.D, BwdShape::GROUP);
-  const int64_t w = words_bytes(l.chunks, l.groups, BwdShape::GROUP), f = ckpt ? 0 : fwd_words(a);
+  l.group = BwdShape::GROUP;
+  l.groups = groups_of(a, l.group);
+  const int64_t w = words_bytes(l.chunks, l.groups, l.group), f = ckpt ? 0 : fwd_words(a);
   l.words = align64(w > f ? w : f);
   l.part = align64(a.B * l.chunks * a.D * 4);
   l.states = ckpt ? 0 : l.part;
@@ -219,10 +220,7 @@ int64_t gated_scan_bwd_workspace(int64_t B, int64_t L, int64_t D, bool ckpt) {
   a.B = B;
   a.L = L;
   a.D = D;
-  const int64_t f = layout_of(a, ckpt).total;
-  a.bf16 = true;
-  const int64_t h = layout_of(a, ckpt).total;
-  return f > h ? f : h;
+  return layout_of(a, ckpt).total;
 }
 
 int gated_scan_bwd(const GatedArgs& a) {
@@ -239,9 +237,9 @@ int gated_scan_bwd(const GatedArgs& a) {
     return norm::fold_partials(nullptr, 0, a.D, outs, 1, s);
   }
   const Layout l = layout_of(a, a.ckpt_in != nullptr);
-  if (l.chunks * l.groups > SW_MAX_WGS / 2)
-    return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
-                (long long)(l.chunks * l.groups));
+  const int64_t wgs = l.chunks * l.groups;
+  if (wgs > SW_MAX_WGS / 2)
+    return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit", (long long)wgs);
   norm::Partials mem(s);
   if ((st = mem.get(a.ws, a.ws_bytes, (size_t)l.total, "sw_gated_scan_bwd")) != SW_OK) return st;
   char* ws = (char*)mem.p;
@@ -255,18 +253,18 @@ int gated_scan_bwd(const GatedArgs& a) {
     if ((st = run_fwd(f, ws, s)) != SW_OK) return st;
     ckpt = f.ckpt;
   }
-  const int64_t words = words_bytes(l.chunks, l.groups, BwdShape::GROUP);
+  const int64_t words = words_bytes(l.chunks, l.groups, l.group);
   if (words > 0 && (st = zero_words((uint32_t*)ws, (size_t)words / 4, s)) != SW_OK) return st;
-  const Words k = {(uint32_t*)ws, (unsigned long long*)(ws + 64), l.groups};
-  const StepRows* rows[4] = {&a.x, &a.r, &a.i, &a.dh};
-  const bool near = near_rows(a, rows, 4, BWD_STEPS);
-  const dim3 grid((unsigned)(l.chunks * l.groups));
-#define CALL(E, MODE)                                                                                    \
-  do {                                                                                                   \
-    if (a.cu)                                                                                            \
-      hipLaunchKernelGGL((bwd_kernel<E, MODE, true>), grid, dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks); \
-    else                                                                                                 \
-      hipLaunchKernelGGL((bwd_kernel<E, MODE, false>), grid, dim3(THREADS), 0, s, a, ckpt, part, k, l.chunks); \
+  const Words k = words_of(ws, l.groups, a.B);
+  const bool near = mode_of(a, BWD_STEPS, 1, {&a.x, &a.r, &a.i, &a.dh}, {}) == NEAR;
+#define CALL(E, MODE)                                                                                   \
+  do {                                                                                                  \
+    if (a.cu)                                                                                           \
+      hipLaunchKernelGGL((bwd_kernel<E, MODE, true>), dim3((unsigned)wgs), dim3(THREADS), 0, s, a, ckpt, \
+                         part, k, l.chunks);                                                            \
+    else                                                                                                \
+      hipLaunchKernelGGL((bwd_kernel<E, MODE, false>), dim3((unsigned)wgs), dim3(THREADS), 0, s, a, ckpt, \
+                         part, k, l.chunks);                                                            \
   } while (0)
   if (a.bf16) {
     if (near)

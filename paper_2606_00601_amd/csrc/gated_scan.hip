@@ -6,50 +6,49 @@ namespace sw {
 namespace gated {
 namespace {
 
-// A chunk of 256 steps of a group of channels.
-template <class E, Mode MODE, bool PACKED>
-__global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, int64_t chunks) {
-  using G = FwdShape<E>;
-  constexpr int N = G::N, S = FWD_S, LANES = G::LANES, SLOTS = G::SLOTS;
-  __shared__ Pairs<N> sh[SLOTS][LANES], back[LOOK][LANES];
-  __shared__ Sequences<PACKED ? FWD_STEPS : 1> sq;
-  __shared__ float rates[G::GROUP];
+
+// A chunk of 16 S steps of 64 channels.  16 steps a lane move the fewest words between
+// workgroups; 8 make twice as many workgroups, three a compute unit at a time.
+template <class E, Mode MODE, bool PACKED, int S>
+__global__ __launch_bounds__(THREADS, S == 16 ? 4 : 6) void fwd_kernel(GatedArgs a, Words k, int64_t chunks) {
+  using G = FwdShape;
+  constexpr int N = G::N, LANES = G::LANES, SLOTS = G::SLOTS, GROUP = G::GROUP, STEPS = SLOTS * S;
+  __shared__ Pairs<N> sh[WAVES][LANES], back[LOOK][LANES];
+  __shared__ Sequences<PACKED ? STEPS : 1> sq;
+  __shared__ float rates[GROUP];
   __shared__ uint32_t ticket;
   const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const bool second = slot & 1;
   uint32_t work = blockIdx.x;
   if (chunks > 1) {
     if (threadIdx.x == 0) ticket = atomicAdd(k.ticket, 1u);
     __syncthreads();
-    work = ticket;
+    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
   }
-  const int64_t chunk = work / (uint32_t)k.groups, group = work % (uint32_t)k.groups;
-  const int64_t per = (a.D + G::GROUP - 1) / G::GROUP;
-  const int64_t b = group / per, c0 = group % per * G::GROUP + lane * N;
-  const int64_t t0 = chunk * FWD_STEPS, left = a.L - t0, steps = left < FWD_STEPS ? left : FWD_STEPS;
-  const int first = slot * S;
+  const uint32_t chunk = work / k.groups, group = work % k.groups;
+  const int64_t b = group / k.per, base = (int64_t)(group % k.per) * GROUP, c0 = base + lane * N;
+  const int64_t t0 = (int64_t)chunk * STEPS, left = a.L - t0;
+  const int steps = (int)(left < STEPS ? left : STEPS), first = slot * S;
+  const float lam = threadIdx.x < GROUP && base + threadIdx.x < a.D && a.L > 0 ? a.lam[base + threadIdx.x] : 0.0f;
+  float start[N], in[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+    start[c] = !PACKED && a.h0 && c0 + c < a.D ? a.h0[b * a.D + c0 + c] : 0.0f;
   if constexpr (PACKED) find_sequences(a, t0, sq);
 
   Rows<E, MODE, N> x, r, i;
   x.init(a.x.p, b * a.x.sb + t0 * a.x.sl, a.x.sl, steps, a.D, first, c0);
   r.init(a.r.p, b * a.r.sb + t0 * a.r.sl, a.r.sl, steps, a.D, first, c0);
   i.init(a.i.p, b * a.i.sb + t0 * a.i.sl, a.i.sl, steps, a.D, first, c0);
-  const int nrate = (int)(a.D - (c0 - lane * N) < G::GROUP ? a.D - (c0 - lane * N) : G::GROUP);
-  if (threadIdx.x < G::GROUP)
-    rates[threadIdx.x] =
-        (int)threadIdx.x < nrate && a.L > 0 ? rate_of(a.lam[c0 - lane * N + threadIdx.x], a.c) : 0.0f;
+
   // pairs of this lane's steps; past the row's end they do not matter
-  float A[S][N], U[S][N];
-  Pairs<N> own;
-#pragma unroll
-  for (int c = 0; c < N; ++c) {
-    own.A[c] = 1.0f;
-    own.U[c] = 0.0f;
-  }
+  float A[S][N], U[S][N], rate[N];
+  Pairs<N> own = identity<N>();
   constexpr int BATCH = 8;  // steps whose loads are in flight together
-  float rate[N];
 #pragma unroll
   for (int j0 = 0; j0 < S; j0 += BATCH) {
-    uint32_t xw[BATCH], rw[BATCH], iw[BATCH];
+    Raw<E, N> xw[BATCH], rw[BATCH], iw[BATCH];
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
       xw[j] = x.get(j0 + j);
@@ -57,22 +56,24 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
       iw[j] = i.get(j0 + j);
     }
     if (j0 == 0) {
+      if (threadIdx.x < GROUP) rates[threadIdx.x] = rate_of(lam, a.c);
       __syncthreads();
 #pragma unroll
       for (int c = 0; c < N; ++c) rate[c] = rates[lane * N + c];
     }
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
+      const int n = PACKED ? sq.seq[first + j0 + j] : 0;
+      const bool starts = PACKED && sq.first(first + j0 + j);
 #pragma unroll
       for (int c = 0; c < N; ++c) {
         float f, u;
-        pair_of<E>(channel<E>(xw[j], c), channel<E>(rw[j], c), channel<E>(iw[j], c), rate[c], f, u);
+        pair_of<E>(xw[j].get(c), rw[j].get(c), iw[j].get(c), rate[c], f, u);
         if constexpr (PACKED) {
-          const int n = sq.seq[first + j0 + j];
           if (n < 0) {
             f = -1.0f;
             u = 0.0f;
-          } else if (sq.first(first + j0 + j)) {
+          } else if (starts) {
             if (a.h0 && c0 + c < a.D) u = __builtin_fmaf(f, a.h0[n * a.D + c0 + c], u);
             f = -1.0f;
           }
@@ -80,27 +81,26 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
         A[j0 + j][c] = f;
         U[j0 + j][c] = u;
         own.U[c] = apply<PACKED>(f, u, own.U[c]);
-        if constexpr (PACKED)
-          own.A[c] = f < 0.0f || own.A[c] < 0.0f ? -1.0f : own.A[c] * f;
-        else
-          own.A[c] *= f;
+        own.A[c] = PACKED && (f < 0.0f || own.A[c] < 0.0f) ? -1.0f : own.A[c] * f;
       }
     }
   }
-  sh[slot][lane] = own;
-  __syncthreads();
-  Pairs<N> before;  // the chunk's steps before this slot
+  // what lies before a slot: a wave's halves exchange pairs by lanes, waves by LDS
+  Pairs<N> other;
 #pragma unroll
   for (int c = 0; c < N; ++c) {
-    before.A[c] = 1.0f;
-    before.U[c] = 0.0f;
+    other.A[c] = __shfl_xor(own.A[c], 32);
+    other.U[c] = __shfl_xor(own.U[c], 32);
   }
-  for (int s = 0; s < slot; ++s) after<PACKED>(before, sh[s][lane]);
+  if (!second) {
+    Pairs<N> both = own;
+    after<PACKED>(both, other);
+    sh[wave][lane] = both;
+  }
+  __syncthreads();
+  Pairs<N> before = first_of<PACKED, false, 4>(sh, wave, lane);
+  if (second) after<PACKED>(before, other);
 
-  float start[N], in[N];
-#pragma unroll
-  for (int c = 0; c < N; ++c)
-    start[c] = !PACKED && a.h0 && c0 + c < a.D ? a.h0[b * a.D + c0 + c] : 0.0f;
   if (chunks > 1) {
     Pairs<N> all = before;
     unsigned long long* w = word_at<G>(k, chunk, group, lane);
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
 #pragma unroll
     for (int c = 0; c < N; ++c) h[c] = apply<PACKED>(A[j][c], U[j][c], h[c]);
     out.put(j, h);
-    if (PACKED ? sq.last(first + j) && a.h_last : a.h_last && t0 + first + j == a.L - 1) {
+    if (a.h_last && (PACKED ? sq.last(first + j) : t0 + first + j == a.L - 1)) {
       const int64_t n = PACKED ? sq.seq[first + j] : b;
 #pragma unroll
       for (int c = 0; c < N; ++c)
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(THREADS, 4) void fwd_kernel(GatedArgs a, Words k, i
   // sequences of no steps
   if (a.h_last) {
     if constexpr (PACKED) {
-      for (int64_t n = chunk + slot * chunks; n < a.nseq; n += chunks * SLOTS)
+      for (int64_t n = chunk + (int64_t)slot * chunks; n < a.nseq; n += chunks * SLOTS)
         if (edge(a, n) >= edge(a, n + 1))
 #pragma unroll
           for (int c = 0; c < N; ++c)
@@ -196,48 +196,54 @@ __global__ __launch_bounds__(256) void step_kernel(GatedStepArgs a) {
 
 }  // namespace
 
-constexpr int group_of(bool bf16) { return bf16 ? FwdShape<uint16_t>::GROUP : FwdShape<float>::GROUP; }
+// Steps of a lane: 8 where they hold the row.  (As two chunks for one of 16 they are slower at
+// every size: B=8 L=2048 D=1536 61 us for 59, B=1 L=65536 D=256 96 for 64.)
+int fwd_s(const GatedArgs& a) { return a.L <= FwdShape::SLOTS * FWD_SHORT_S ? FWD_SHORT_S : FWD_S; }
 
 int64_t fwd_words(const GatedArgs& a) {
-  const int g = group_of(a.bf16);
-  return words_bytes(chunks_of(a.L, FWD_STEPS), groups_of(a.B, a.D, g), g);
+  return words_bytes(chunks_of(a.L, FwdShape::SLOTS * fwd_s(a)), groups_of(a, FwdShape::GROUP), FwdShape::GROUP);
 }
 
 int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
-  const int64_t chunks = chunks_of(a.L, FWD_STEPS), groups = groups_of(a.B, a.D, group_of(a.bf16));
+  const int S = fwd_s(a), steps = FwdShape::SLOTS * S;
+  const int64_t chunks = chunks_of(a.L, steps), groups = groups_of(a, FwdShape::GROUP);
   if (chunks * groups > SW_MAX_WGS / 2)
     return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
                 (long long)(chunks * groups));
   int st;
   if (chunks > 1 && (st = zero_words((uint32_t*)ws, (size_t)fwd_words(a) / 4, s)) != SW_OK) return st;
-  const Words k = {(uint32_t*)ws, (unsigned long long*)((char*)ws + 64), groups};
-  // pairs of bf16 channels go in words where every row begins on one
-  const StepRows* rows[3] = {&a.x, &a.r, &a.i};
-  bool whole = a.D % 2 == 0 && (uintptr_t)a.h % 4 == 0;
-  for (const StepRows* x : rows)
-    whole = whole && (uintptr_t)x->p % 4 == 0 && x->sl % 2 == 0 && x->sb % 2 == 0;
-  const Mode mode = !near_rows(a, rows, 3, FWD_STEPS) ? FAR : whole || !a.bf16 ? NEAR : SPLIT;
+  const Words k = words_of(ws, groups, a.B);
+  const Mode mode = mode_of(a, steps, FwdShape::N, {&a.x, &a.r, &a.i}, {a.h});
   const dim3 grid((unsigned)(chunks * groups));
-#define CALL(E, MODE)                                                                                  \
-  do {                                                                                                 \
-    if (a.cu)                                                                                          \
-      hipLaunchKernelGGL((fwd_kernel<E, MODE, true>), grid, dim3(THREADS), 0, s, a, k, chunks);        \
-    else                                                                                               \
-      hipLaunchKernelGGL((fwd_kernel<E, MODE, false>), grid, dim3(THREADS), 0, s, a, k, chunks);       \
+#define LAUNCH(E, MODE, PACKED, S) \
+  hipLaunchKernelGGL((fwd_kernel<E, MODE, PACKED, S>), grid, dim3(THREADS), 0, s, a, k, chunks)
+#define CALL(E, MODE)                       \
+  do {                                      \
+    if (S == FWD_S && a.cu)                 \
+      LAUNCH(E, MODE, true, FWD_S);         \
+    else if (S == FWD_S)                    \
+      LAUNCH(E, MODE, false, FWD_S);        \
+    else if (a.cu)                          \
+      LAUNCH(E, MODE, true, FWD_SHORT_S);   \
+    else                                    \
+      LAUNCH(E, MODE, false, FWD_SHORT_S);  \
   } while (0)
-  if (a.bf16) {
-    if (mode == NEAR)
-      CALL(uint16_t, NEAR);
-    else if (mode == SPLIT)
-      CALL(uint16_t, SPLIT);
-    else
-      CALL(uint16_t, FAR);
-  } else if (mode == NEAR) {
-    CALL(float, NEAR);
-  } else {
-    CALL(float, FAR);
-  }
+#define TYPED(E)          \
+  do {                    \
+    if (mode == NEAR)     \
+      CALL(E, NEAR);      \
+    else if (mode == SPLIT) \
+      CALL(E, SPLIT);     \
+    else                  \
+      CALL(E, FAR);       \
+  } while (0)
+  if (a.bf16)
+    TYPED(uint16_t);
+  else
+    TYPED(float);
+#undef TYPED
 #undef CALL
+#undef LAUNCH
   return check_launch("gated fwd_kernel");
 }
 
@@ -250,10 +256,7 @@ int64_t gated_scan_fwd_workspace(int64_t B, int64_t L, int64_t D) {
   a.B = B;
   a.L = L;
   a.D = D;
-  const int64_t f = fwd_words(a);
-  a.bf16 = true;
-  const int64_t h = fwd_words(a);
-  return f > h ? f : h;
+  return fwd_words(a);
 }
 
 int gated_scan_fwd(const GatedArgs& a) {

@@ -1,8 +1,8 @@
 // gated_walk.h -- what the gated recurrence's walks share (device code).
 //
 // A workgroup of 8 waves holds a chunk of steps of one group of channels in registers: slots
-// of a few steps, each some lanes of N channels.  A slot's steps are one affine pair; the
-// pairs before a slot are composed from LDS, and the chunk's from what the chunks before it
+// of a few steps, each some lanes of one or two channels.  A slot's steps are one affine pair;
+// the pairs before a slot are composed in LDS, and the chunk's from what the chunks before it
 // have published, so each input is read once.
 //
 // Between workgroups: a chunk publishes its own pair as soon as it has it (AGG), and the
@@ -12,6 +12,8 @@
 // AGG without waiting, and the first knows its end, so every wait ends.
 #pragma once
 
+#include <initializer_list>
+
 #include "gated_math.h"
 #include "gated_scan.h"
 #include "selective_common.h"
@@ -19,79 +21,107 @@
 namespace sw {
 namespace gated {
 
-constexpr int THREADS = 512, LOOK = 16;
+constexpr int THREADS = 512, WAVES = THREADS / 64, LOOK = 16;
 template <int N_, int LANES_>
 struct Shape {
   static constexpr int N = N_, LANES = LANES_, SLOTS = THREADS / LANES_, GROUP = N_ * LANES_;
 };
-// The forward: 32 lanes of four bytes each, a row of 128 bytes, 16 slots of 16 steps.
-template <class E>
-using FwdShape = Shape<4 / (int)sizeof(E), 32>;
-// The backward holds more of each value, so a lane takes one channel and 8 steps of it: a
-// wave is a slot.  (Two bf16 channels a lane, 16 values, took 183 us at B=8 L=2048 D=1536
-// with 42 of 128 registers spilled, and 161 with 256 registers and one workgroup a compute
-// unit.)
+// The forward keeps two values of a step: half a wave is a slot, and chunks are long, which
+// makes few of them (16 steps a lane; 8 for short rows).
+using FwdShape = Shape<2, 32>;
+constexpr int FWD_S = 16, FWD_SHORT_S = 8;
+// The backward keeps more of each value, so a lane takes one channel; a wave is a slot, and
+// what depends on the step alone is scalar.
 using BwdShape = Shape<1, 64>;
-constexpr int FWD_S = 16, BWD_S = 8;
-constexpr int FWD_STEPS = 16 * FWD_S, BWD_STEPS = BwdShape::SLOTS * BWD_S;
-static_assert(BWD_STEPS == SW_GATED_CKPT && FWD_STEPS % BWD_STEPS == 0, "a state for each chunk of the backward");
+constexpr int BWD_S = 8, BWD_STEPS = THREADS / 64 * BWD_S;
+static_assert(BWD_STEPS == SW_GATED_CKPT && FwdShape::SLOTS * FWD_SHORT_S % BWD_STEPS == 0,
+              "a state for each chunk of the backward");
 
-// How rows are loaded: NEAR, a lane's channels a load from a buffer over the chunk's rows (out of
-// range reads as zero); SPLIT, the same, a channel a load (odd widths, strides or addresses);
-// FAR, by 64-bit addresses (a chunk's rows reach over 2^31 bytes).
+// How rows are loaded: NEAR, a lane's two channels a load from a buffer over the chunk's
+// rows (out of range reads as zero); SPLIT, the same, a channel a load (odd widths, strides or
+// addresses); FAR, by 64-bit addresses (a chunk's rows reach over 2^31 bytes).
 enum Mode { NEAR, SPLIT, FAR };
+
+// A lane's channels of a step as loaded.
+template <class E, int N>
+struct Raw {
+  uint32_t w[(sizeof(E) * N + 3) / 4];
+  __device__ __forceinline__ float get(int c) const {
+    if constexpr (sizeof(E) == 4)
+      return __uint_as_float(w[c]);
+    else
+      return c ? bf16_hi(w[0]) : bf16_lo(w[0]);
+  }
+};
 
 template <class E, Mode MODE, int N>
 struct Rows {
-  static_assert(N == 1 || sizeof(E) * N == 4, "a word or an element");
   __amdgpu_buffer_rsrc_t rs;
   const char* p;
   uint32_t off;
   int64_t step;
-  int left, chan;  // FAR: steps and channels from here on
+  int left, chan;  // steps (FAR) and channels from here on
 
-  // steps first .. of `steps` in the chunk at row base p0, channels from c
-  __device__ __forceinline__ void init(const void* base, int64_t p0, int64_t sl, int64_t steps, int64_t D,
+  // steps first .. of `steps` in the chunk whose first row begins at element p0, channels from c
+  __device__ __forceinline__ void init(const void* base, int64_t p0, int64_t sl, int steps, int64_t D,
                                        int first, int64_t c) {
     step = sl * (int64_t)sizeof(E);
+    chan = (int)(D - c < N ? D - c : N);
     const char* b = (const char*)base + p0 * (int64_t)sizeof(E);
     if constexpr (MODE == FAR) {
       p = b + first * step + c * (int64_t)sizeof(E);
-      left = (int)(steps - first);
-      chan = (int)(D - c < N ? D - c : N);
+      left = steps - first;
     } else {
       rs = buffer_rsrc(b, steps > 0 ? (uint32_t)((steps - 1) * step + D * (int64_t)sizeof(E)) : 0u);
-      off = (uint32_t)(first * (uint32_t)step + (uint32_t)c * sizeof(E));
+      off = (uint32_t)first * (uint32_t)step + (uint32_t)c * (uint32_t)sizeof(E);
     }
   }
-  // step first + j as raw bits: bf16, both channels in one word
-  __device__ __forceinline__ uint32_t get(int j) const {
+  // an output: lanes whose channels are past D store outside the buffer
+  __device__ __forceinline__ void init_out(void* base, int64_t p0, int steps, int64_t D, int first,
+                                           int64_t c) {
+    init(base, p0, D, steps, D, first, c);
+    if constexpr (MODE != FAR) {
+      if (chan <= 0) off = 0x80000000u;
+    }
+  }
+  __device__ __forceinline__ Raw<E, N> get(int j) const {
+    Raw<E, N> r = {};
+    const int o = (int)(off + (uint32_t)j * (uint32_t)step);
     if constexpr (MODE == FAR) {
-      uint32_t w = 0;
       if (j < left) {
         const E* q = (const E*)(p + j * step);
         if constexpr (sizeof(E) == 4) {
-          if (chan > 0) w = __float_as_uint(q[0]);
+#pragma unroll
+          for (int c = 0; c < N; ++c)
+            if (c < chan) r.w[c] = __float_as_uint(q[c]);
         } else {
-          if (chan > 0) w = q[0];
-          if (N > 1 && chan > 1) w |= (uint32_t)q[1] << 16;
+          if (chan > 0) r.w[0] = q[0];
+          if (N > 1 && chan > 1) r.w[0] |= (uint32_t)q[1] << 16;
         }
       }
-      return w;
-    } else {
-      const int o = (int)(off + (uint32_t)j * (uint32_t)step);
-      if constexpr (sizeof(E) * N == 4 && (MODE == NEAR || N == 1)) {
-        return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
-      } else if constexpr (N == 1) {
-        return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
+    } else if constexpr (sizeof(E) == 4) {
+      if constexpr (N == 1) {
+        r.w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
+      } else if constexpr (MODE == NEAR) {
+        const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, o, 0, 0));
+        r.w[0] = v.x;
+        r.w[1] = v.y;
       } else {
-        const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
-        return lo | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o + 2, 0, 0) << 16;
+        r.w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
+        r.w[1] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, o + 4, 0, 0);
       }
+    } else if constexpr (N == 1) {
+      r.w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
+    } else if constexpr (MODE == NEAR) {
+      r.w[0] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0);
+    } else {
+      const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o, 0, 0);
+      r.w[0] = lo | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, o + 2, 0, 0) << 16;
     }
+    return r;
   }
-  // the lane's channels of an output's step; those past D go nowhere
   __device__ __forceinline__ void put(int j, const float* v) const {
+    const int o = (int)(off + (uint32_t)j * (uint32_t)step);
     if constexpr (MODE == FAR) {
       if (j < left) {
         E* q = (E*)(p + j * step);
@@ -104,42 +134,29 @@ struct Rows {
               q[c] = (uint16_t)bf16_rne(v[c]);
           }
       }
-    } else {
-      const int o = (int)(off + (uint32_t)j * (uint32_t)step);
-      if constexpr (sizeof(E) == 4) {
+    } else if constexpr (sizeof(E) == 4) {
+      if constexpr (N == 1) {
         __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), rs, o, 0, 0);
-      } else if constexpr (N == 1) {
-        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_rne(v[0]), rs, o, 0, 0);
+      } else if constexpr (MODE == NEAR) {
+        const sw_u32x2 w = {__float_as_uint(v[0]), __float_as_uint(v[1])};
+        __builtin_amdgcn_raw_buffer_store_b64(w, rs, o, 0, 0);
       } else {
-        const uint32_t w = bf16x2_rne(v[0], v[1]);
-        if constexpr (MODE == NEAR) {
-          __builtin_amdgcn_raw_buffer_store_b32(w, rs, o, 0, 0);
-        } else {
-          __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w, rs, o, 0, 0);
-          if (chan > 1) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w >> 16), rs, o + 2, 0, 0);
-        }
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), rs, o, 0, 0);
+        if (chan > 1) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[1]), rs, o + 4, 0, 0);
+      }
+    } else if constexpr (N == 1) {
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_rne(v[0]), rs, o, 0, 0);
+    } else {
+      const uint32_t w = bf16x2_rne(v[0], v[1]);
+      if constexpr (MODE == NEAR) {
+        __builtin_amdgcn_raw_buffer_store_b32(w, rs, o, 0, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w, rs, o, 0, 0);
+        if (chan > 1) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w >> 16), rs, o + 2, 0, 0);
       }
     }
   }
-  // an output: lanes whose channels are past D store outside the buffer
-  __device__ __forceinline__ void init_out(void* base, int64_t p0, int64_t steps, int64_t D, int first,
-                                           int64_t c) {
-    init(base, p0, D, steps, D, first, c);
-    chan = (int)(D - c < N ? D - c : N);
-    if constexpr (MODE != FAR) {
-      if (chan <= 0) off = 0x80000000u;
-    }
-  }
 };
-
-template <class E>
-__device__ __forceinline__ float channel(uint32_t w, int c) {
-  if constexpr (sizeof(E) == 4) {
-    return __uint_as_float(w);
-  } else {
-    return c ? bf16_hi(w) : bf16_lo(w);
-  }
-}
 
 // An affine pair: v -> A v + U, or, with A below zero, the constant U (a sequence begins
 // inside: what came before does not reach its end, were it infinite).
@@ -147,6 +164,16 @@ template <int N>
 struct Pairs {
   float A[N], U[N];
 };
+template <int N>
+__device__ __forceinline__ Pairs<N> identity() {
+  Pairs<N> p;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    p.A[c] = 1.0f;
+    p.U[c] = 0.0f;
+  }
+  return p;
+}
 template <bool PACKED, int N>
 __device__ __forceinline__ void after(Pairs<N>& p, const Pairs<N>& later) {
 #pragma unroll
@@ -168,17 +195,34 @@ __device__ __forceinline__ float apply(float A, float U, float v) {
   return PACKED && A < 0.0f ? U : r;
 }
 
+// The composition of the first n of 8 pairs in LDS, from the last one back if `turned`.
+template <bool PACKED, bool TURNED, int DEPTH, int N, int LANES>
+__device__ __forceinline__ Pairs<N> first_of(const Pairs<N> (*sh)[LANES], int n, int lane) {
+  Pairs<N> p = identity<N>();
+#pragma unroll
+  for (int w0 = 0; w0 < 8; w0 += DEPTH) {  // DEPTH in flight at a time
+    Pairs<N> q[DEPTH];
+#pragma unroll
+    for (int e = 0; e < DEPTH; ++e) q[e] = sh[TURNED ? 7 - (w0 + e) : w0 + e][lane];
+#pragma unroll
+    for (int e = 0; e < DEPTH; ++e)
+      if (w0 + e < n) after<PACKED>(p, q[e]);
+  }
+  return p;
+}
+
 // Where the words between workgroups lie: one for each channel of a group's chunk, values,
 // then factors.
 struct Words {
   uint32_t* ticket;
   unsigned long long* w;
-  int64_t groups;
+  uint32_t groups, per;  // groups of channels in all, and of one row of the batch
+  int look;              // chunks a workgroup looks back over at once
 };
 template <class G>
-__device__ __forceinline__ unsigned long long* word_at(const Words& k, int64_t chunk, int64_t group,
+__device__ __forceinline__ unsigned long long* word_at(const Words& k, int64_t chunk, uint32_t group,
                                                        int lane) {
-  return k.w + (chunk * k.groups + group) * (2 * G::GROUP) + lane * G::N;
+  return k.w + (chunk * (int64_t)k.groups + group) * (2 * G::GROUP) + lane * G::N;
 }
 template <class G>
 __device__ __forceinline__ void publish(unsigned long long* w, const Pairs<G::N>& p, const bool* end) {
@@ -194,44 +238,69 @@ __device__ __forceinline__ void publish(unsigned long long* w, const Pairs<G::N>
 // one after the other, exactly as those chunks take it through their own.  So its bits do
 // not depend on which ends were known.  All of the workgroup take part.
 template <class G>
-__device__ __forceinline__ void look_back(const Words& k, int64_t chunk, int64_t group, int slot, int lane,
+__device__ __forceinline__ void look_back(const Words& k, int64_t chunk, uint32_t group, int slot, int lane,
                                           const float* first, Pairs<G::N> (*sh)[G::LANES], float* value) {
-  constexpr int N = G::N, EACH = LOOK / G::SLOTS;  // chunks a slot looks at
+  constexpr int N = G::N;
   bool open;
   do {
-    Pairs<N> p[EACH];  // A < 0: U is the end's value
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int64_t mine = chunk - 1 - (e * G::SLOTS + slot);
-      const unsigned long long* w = word_at<G>(k, mine < 0 ? 0 : mine, group, lane);
+    __syncthreads();
+    for (int at = slot; at < k.look; at += G::SLOTS) {
+      const int64_t mine = chunk - 1 - at;
+      Pairs<N> p;  // A < 0: U is the end's value
 #pragma unroll
       for (int c = 0; c < N; ++c) {
-        p[e].A[c] = -1.0f;
-        p[e].U[c] = first[c];
-        if (mine >= 0) {
-          unsigned long long v;
-          while ((v = carry_get(w + c)) >> 32 == CARRY_EMPTY) __builtin_amdgcn_s_sleep(1);
-          p[e].U[c] = __uint_as_float((uint32_t)v);
-          if (v >> 32 == CARRY_AGG) {
-            while ((v = carry_get(w + G::GROUP + c)) >> 32 == CARRY_EMPTY) __builtin_amdgcn_s_sleep(1);
-            p[e].A[c] = __uint_as_float((uint32_t)v);
+        p.A[c] = -1.0f;
+        p.U[c] = first[c];
+      }
+      if (mine >= 0) {
+        // all words at once: one after the other each would wait for the one before
+        const unsigned long long* w = word_at<G>(k, mine, group, lane);
+        unsigned long long u[N], f[N];
+        bool there;
+        do {
+#pragma unroll
+          for (int c = 0; c < N; ++c) {
+            u[c] = carry_get(w + c);
+            f[c] = carry_get(w + G::GROUP + c);
           }
+          there = true;
+#pragma unroll
+          for (int c = 0; c < N; ++c)
+            there = there && (u[c] >> 32 == CARRY_INC || (u[c] >> 32 == CARRY_AGG && f[c] >> 32 == CARRY_AGG));
+          if (!there) __builtin_amdgcn_s_sleep(1);
+        } while (!there);
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          p.U[c] = __uint_as_float((uint32_t)u[c]);
+          if (u[c] >> 32 == CARRY_AGG) p.A[c] = __uint_as_float((uint32_t)f[c]);
         }
       }
+      sh[at][lane] = p;
     }
     __syncthreads();
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) sh[e * G::SLOTS + slot][lane] = p[e];
-    __syncthreads();
-    open = false;
+    // from the farthest on: an end found on the way replaces what was made up before it
+    bool known[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-      int s = 0;
-      while (s < LOOK - 1 && !(sh[s][lane].A[c] < 0.0f)) ++s;
-      open |= !(sh[s][lane].A[c] < 0.0f);
-      value[c] = sh[s][lane].U[c];
-      while (--s >= 0) value[c] = __builtin_fmaf(sh[s][lane].A[c], value[c], sh[s][lane].U[c]);
+      value[c] = 0.0f;
+      known[c] = false;
     }
+    for (int s = k.look - 4; s >= 0; s -= 4) {
+      Pairs<N> q[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[e] = sh[s + e][lane];
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const bool is = q[e].A[c] < 0.0f;
+          value[c] = is ? q[e].U[c] : __builtin_fmaf(q[e].A[c], value[c], q[e].U[c]);
+          known[c] = known[c] || is;
+        }
+    }
+    open = false;
+#pragma unroll
+    for (int c = 0; c < N; ++c) open = open || !known[c];
   } while (__any(open));  // a wave's lanes hold all of the group's channels: all waves agree
 }
 
@@ -269,22 +338,37 @@ __device__ __forceinline__ void find_sequences(const GatedArgs& a, int64_t t0, S
 }
 
 inline int64_t chunks_of(int64_t L, int steps) { return L > steps ? (L + steps - 1) / steps : 1; }
-inline int64_t groups_of(int64_t B, int64_t D, int group) { return B * ((D + group - 1) / group); }
+inline int64_t groups_of(const GatedArgs& a, int group) { return a.B * ((a.D + group - 1) / group); }
+// Few groups have many chunks under way at once, so they look further back: 4 chunks, or up
+// to 16 where that leaves fewer than 128 for all groups.  (B=1 L=65536 D=256 forward 189, 127,
+// 96 us at 4, 8, 16 chunks; B=1 L=65536 D=5120 569, 581, 618.)
+constexpr int64_t LOOK_ALL = 128;
 // Bytes of the words of a walk, its ticket before them.
 inline int64_t words_bytes(int64_t chunks, int64_t groups, int group) {
   return chunks > 1 ? 64 + chunks * groups * group * 16 : 0;
 }
-// Whether the rows of a chunk reach over less than 2^31 bytes.
-inline bool near_rows(const GatedArgs& a, const StepRows* const* rows, int n, int steps) {
+inline Words words_of(void* ws, int64_t groups, int64_t B) {
+  int look = 4;
+  while (look < LOOK && look * groups < LOOK_ALL) look *= 2;
+  return {(uint32_t*)ws, (unsigned long long*)((char*)ws + 64), (uint32_t)groups, (uint32_t)(groups / B), look};
+}
+// The mode of a walk of `steps` a chunk, `n` channels a lane, over these rows and dense results.
+inline Mode mode_of(const GatedArgs& a, int steps, int n, std::initializer_list<const StepRows*> rows,
+                    std::initializer_list<const void*> outs) {
   const int64_t es = a.bf16 ? 2 : 4, most = (int64_t)1 << 31;
-  bool near = (steps + 1) * a.D * es < most;
-  for (int j = 0; j < n; ++j)
-    near = near && rows[j]->sl < most && steps * rows[j]->sl * es + a.D * es < most;
-  return near;
+  bool near = (steps + 1) * a.D * es < most, pairs = n == 1 || a.D % 2 == 0;
+  for (const StepRows* x : rows) {
+    near = near && x->sl < most && steps * x->sl * es + a.D * es < most;
+    // bf16 pairs are words
+    if (a.bf16 && n > 1) pairs = pairs && (uintptr_t)x->p % 4 == 0 && x->sl % 2 == 0 && x->sb % 2 == 0;
+  }
+  for (const void* p : outs)
+    if (a.bf16 && n > 1) pairs = pairs && (uintptr_t)p % 4 == 0;
+  return !near ? FAR : pairs ? NEAR : SPLIT;
 }
 
-int run_fwd(const GatedArgs& a, void* words, hipStream_t s);
 int64_t fwd_words(const GatedArgs& a);
+int run_fwd(const GatedArgs& a, void* words, hipStream_t s);
 
 }  // namespace gated
 }  // namespace sw
