@@ -76,20 +76,30 @@ __global__ __launch_bounds__(256) void place_kernel(EmbedArgs a, Sort s, Clear z
   // thread tid's bins are next to each other: their totals, then a scan over the threads
   const int per = bins > 256 ? bins / 256 : 1;
   uint32_t mine = 0;
-  for (int d = tid * per; d < (tid + 1) * per && d < bins; ++d) {
-    uint32_t total = 0, before = 0;
-    for (int q = 0; q < s.tiles; q += 16) {
-      uint32_t n[16];
+  for (int k0 = 0; k0 < per; k0 += 2) {
+    uint32_t total[2] = {}, before[2] = {};
+    const int d = tid * per + k0;
+    for (int q = 0; q < s.tiles; q += 16) {  // 32 counts in flight
+      uint32_t n[16][2];
 #pragma unroll
-      for (int u = 0; u < 16; ++u) n[u] = q + u < s.tiles ? s.hist[(int64_t)(q + u) * bins + d] : 0;
+      for (int u = 0; u < 16; ++u)
 #pragma unroll
-      for (int u = 0; u < 16; ++u) {
-        total += n[u];
-        before += q + u < (int)blockIdx.x ? n[u] : 0;
-      }
+        for (int k = 0; k < 2; ++k)
+          n[u][k] = q + u < s.tiles && k0 + k < per && d + k < bins ? s.hist[(int64_t)(q + u) * bins + d + k] : 0;
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          total[k] += n[u][k];
+          before[k] += q + u < (int)blockIdx.x ? n[u][k] : 0;
+        }
     }
-    base[d] = mine + before;
-    mine += total;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (k0 + k < per && d + k < bins) {
+        base[d + k] = mine + before[k];
+        mine += total[k];
+      }
   }
   sums[tid] = mine;
   __syncthreads();
@@ -311,8 +321,9 @@ Plan plan_of(int64_t T, int64_t V, int64_t D) {
   p.tile = (T + (int64_t)TILE * MAX_TILES - 1) / ((int64_t)TILE * MAX_TILES) * TILE;
   p.tiles = (int)((T + p.tile - 1) / p.tile);
   p.cols = (D + 511) / 512;
-  // pieces for some 4096 waves, 16 steps at least
-  p.P = 16;
+  // 32 steps, or pieces for some 4096 waves.  (T=65536 V=256 D=512 fp32 69, 59, 57 us at 16, 32,
+  // 64 steps; T=131072 V=32000 D=256 95, 83, 87; T=7800 V=17000 D=5120 121, 117, 123.)
+  p.P = 32;
   while (p.P < 256 && T * p.cols > (int64_t)p.P * 4096) p.P *= 2;
   p.pieces = (T + p.P - 1) / p.P;
   p.entries = align64(T * (int64_t)sizeof(Entry));

@@ -6,7 +6,6 @@
 //   v_t = a_t (dh_t + v_{t+1}),
 // an affine pair again, composed in slots and between workgroups from the last chunk on.
 #include "gated_walk.h"
-#include "norm_rows.h"
 
 namespace sw {
 namespace gated {
@@ -27,7 +26,7 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
   if (chunks > 1) {
     if (threadIdx.x == 0) ticket = atomicAdd(k.ticket, 1u);
     __syncthreads();
-    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
+    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket) - k.base;
   }
   // `turn` counts the chunks from the last one on
   const uint32_t turn = work / k.groups, group = work % k.groups;
@@ -124,7 +123,7 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
     after<PACKED>(all, bwd);
     end = turn == 0 || all.A[0] < 0.0f;
     if (turn == 0) all.U[0] = apply<PACKED>(all.A[0], all.U[0], tail);
-    publish<G>(w, all, &end);
+    publish<G>(w, k.epoch, all, &end);
   }
   // the states before the steps go into what a step's dr is of its g: q - m a h
   float h = apply<PACKED>(before.A[0], before.U[0], start);
@@ -144,7 +143,7 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
   }
   if (chunks > 1) {
     look_back<G>(k, turn, group, slot, lane, &tail, sh, &in);
-    if (publishes && !end) carry_put(w, CARRY_INC, __float_as_uint(__builtin_fmaf(all.A[0], in, all.U[0])));
+    if (publishes && !end) carry_put(w, carry_status(k.epoch, CARRY_INC), __float_as_uint(__builtin_fmaf(all.A[0], in, all.U[0])));
   }
 
   Rows<E, MODE, 1> dx, dr, di;
@@ -250,12 +249,13 @@ int gated_scan_bwd(const GatedArgs& a) {
     f.h = nullptr;
     f.h_last = nullptr;
     f.ckpt = (float*)(ws + l.words + l.part);
-    if ((st = run_fwd(f, ws, s)) != SW_OK) return st;
+    if ((st = run_fwd(f, ws, (size_t)l.words, s)) != SW_OK) return st;
     ckpt = f.ckpt;
   }
-  const int64_t words = words_bytes(l.chunks, l.groups, l.group);
-  if (words > 0 && (st = zero_words((uint32_t*)ws, (size_t)words / 4, s)) != SW_OK) return st;
-  const Words k = words_of(ws, l.groups, a.B);
+  LaunchWords words(s);
+  if ((st = words.get(ws, (size_t)l.words, l.chunks, l.groups, l.group, a.B, s, "sw_gated_scan_bwd")) != SW_OK)
+    return st;
+  const Words& k = words.k;
   const bool near = mode_of(a, BWD_STEPS, 1, {&a.x, &a.r, &a.i, &a.dh}, {}) == NEAR;
 #define CALL(E, MODE)                                                                                   \
   do {                                                                                                  \
@@ -277,7 +277,7 @@ int gated_scan_bwd(const GatedArgs& a) {
     CALL(float, FAR);
   }
 #undef CALL
-  if ((st = check_launch("gated bwd_kernel")) != SW_OK) return st;
+  if ((st = words.done(check_launch("gated bwd_kernel"))) != SW_OK) return st;
   return norm::fold_partials(part, a.B * l.chunks, a.D, outs, 1, s);
 }
 

@@ -1,6 +1,5 @@
 // gated_scan.hip -- the gated linear recurrence: forward and one step.
 #include "gated_walk.h"
-#include "norm_rows.h"
 
 namespace sw {
 namespace gated {
@@ -24,7 +23,7 @@ __global__ __launch_bounds__(THREADS, S == 16 ? 4 : 6) void fwd_kernel(GatedArgs
   if (chunks > 1) {
     if (threadIdx.x == 0) ticket = atomicAdd(k.ticket, 1u);
     __syncthreads();
-    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket);
+    work = (uint32_t)__builtin_amdgcn_readfirstlane((int)ticket) - k.base;
   }
   const uint32_t chunk = work / k.groups, group = work % k.groups;
   const int64_t b = group / k.per, base = (int64_t)(group % k.per) * GROUP, c0 = base + lane * N;
@@ -113,13 +112,13 @@ __global__ __launch_bounds__(THREADS, S == 16 ? 4 : 6) void fwd_kernel(GatedArgs
         end[c] = chunk == 0 || all.A[c] < 0.0f;
         if (chunk == 0) all.U[c] = apply<PACKED>(all.A[c], all.U[c], start[c]);
       }
-      publish<G>(w, all, end);
+      publish<G>(w, k.epoch, all, end);
     }
     look_back<G>(k, chunk, group, slot, lane, start, back, in);
     if (publishes)
 #pragma unroll
       for (int c = 0; c < N; ++c)
-        if (!end[c]) carry_put(w + c, CARRY_INC, __float_as_uint(__builtin_fmaf(all.A[c], in[c], all.U[c])));
+        if (!end[c]) carry_put(w + c, carry_status(k.epoch, CARRY_INC), __float_as_uint(__builtin_fmaf(all.A[c], in[c], all.U[c])));
   } else {
 #pragma unroll
     for (int c = 0; c < N; ++c) in[c] = start[c];
@@ -204,15 +203,17 @@ int64_t fwd_words(const GatedArgs& a) {
   return words_bytes(chunks_of(a.L, FwdShape::SLOTS * fwd_s(a)), groups_of(a, FwdShape::GROUP), FwdShape::GROUP);
 }
 
-int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
+int run_fwd(const GatedArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {
   const int S = fwd_s(a), steps = FwdShape::SLOTS * S;
   const int64_t chunks = chunks_of(a.L, steps), groups = groups_of(a, FwdShape::GROUP);
   if (chunks * groups > SW_MAX_WGS / 2)
     return fail(SW_ERR_UNSUPPORTED, "%lld chunks of the recurrence exceed the launch limit",
                 (long long)(chunks * groups));
   int st;
-  if (chunks > 1 && (st = zero_words((uint32_t*)ws, (size_t)fwd_words(a) / 4, s)) != SW_OK) return st;
-  const Words k = words_of(ws, groups, a.B);
+  LaunchWords words(s);
+  if ((st = words.get(ws, ws_bytes, chunks, groups, FwdShape::GROUP, a.B, s, "sw_gated_scan_fwd")) != SW_OK)
+    return st;
+  const Words& k = words.k;
   const Mode mode = mode_of(a, steps, FwdShape::N, {&a.x, &a.r, &a.i}, {a.h});
   const dim3 grid((unsigned)(chunks * groups));
 #define LAUNCH(E, MODE, PACKED, S) \
@@ -244,7 +245,7 @@ int run_fwd(const GatedArgs& a, void* ws, hipStream_t s) {
 #undef TYPED
 #undef CALL
 #undef LAUNCH
-  return check_launch("gated fwd_kernel");
+  return words.done(check_launch("gated fwd_kernel"));
 }
 
 }  // namespace gated
@@ -261,12 +262,7 @@ int64_t gated_scan_fwd_workspace(int64_t B, int64_t L, int64_t D) {
 
 int gated_scan_fwd(const GatedArgs& a) {
   if (a.nseq == 0) return SW_OK;
-  const hipStream_t s = current_stream();
-  norm::Partials ws(s);
-  int st;
-  const int64_t need = fwd_words(a);
-  if (need > 0 && (st = ws.get(a.ws, a.ws_bytes, (size_t)need, "sw_gated_scan_fwd")) != SW_OK) return st;
-  return run_fwd(a, ws.p, s);
+  return run_fwd(a, a.ws, a.ws_bytes, current_stream());
 }
 
 int gated_scan_step(const GatedStepArgs& a) {

@@ -16,6 +16,7 @@
 
 #include "gated_math.h"
 #include "gated_scan.h"
+#include "norm_rows.h"
 #include "selective_common.h"
 
 namespace sw {
@@ -218,6 +219,7 @@ struct Words {
   unsigned long long* w;
   uint32_t groups, per;  // groups of channels in all, and of one row of the batch
   int look;              // chunks a workgroup looks back over at once
+  uint32_t base, epoch;  // the ticket this launch starts from, and the tag of its words
 };
 template <class G>
 __device__ __forceinline__ unsigned long long* word_at(const Words& k, int64_t chunk, uint32_t group,
@@ -225,11 +227,12 @@ __device__ __forceinline__ unsigned long long* word_at(const Words& k, int64_t c
   return k.w + (chunk * (int64_t)k.groups + group) * (2 * G::GROUP) + lane * G::N;
 }
 template <class G>
-__device__ __forceinline__ void publish(unsigned long long* w, const Pairs<G::N>& p, const bool* end) {
+__device__ __forceinline__ void publish(unsigned long long* w, uint32_t epoch, const Pairs<G::N>& p,
+                                        const bool* end) {
 #pragma unroll
   for (int c = 0; c < G::N; ++c) {
-    if (!end[c]) carry_put(w + G::GROUP + c, CARRY_AGG, __float_as_uint(p.A[c]));
-    carry_put(w + c, end[c] ? CARRY_INC : CARRY_AGG, __float_as_uint(p.U[c]));
+    if (!end[c]) carry_put(w + G::GROUP + c, carry_status(epoch, CARRY_AGG), __float_as_uint(p.A[c]));
+    carry_put(w + c, carry_status(epoch, end[c] ? CARRY_INC : CARRY_AGG), __float_as_uint(p.U[c]));
   }
 }
 
@@ -241,6 +244,7 @@ template <class G>
 __device__ __forceinline__ void look_back(const Words& k, int64_t chunk, uint32_t group, int slot, int lane,
                                           const float* first, Pairs<G::N> (*sh)[G::LANES], float* value) {
   constexpr int N = G::N;
+  const uint32_t agg = carry_status(k.epoch, CARRY_AGG), inc = carry_status(k.epoch, CARRY_INC);
   bool open;
   do {
     __syncthreads();
@@ -266,13 +270,13 @@ __device__ __forceinline__ void look_back(const Words& k, int64_t chunk, uint32_
           there = true;
 #pragma unroll
           for (int c = 0; c < N; ++c)
-            there = there && (u[c] >> 32 == CARRY_INC || (u[c] >> 32 == CARRY_AGG && f[c] >> 32 == CARRY_AGG));
+            there = there && (u[c] >> 32 == inc || (u[c] >> 32 == agg && f[c] >> 32 == agg));
           if (!there) __builtin_amdgcn_s_sleep(1);
         } while (!there);
 #pragma unroll
         for (int c = 0; c < N; ++c) {
           p.U[c] = __uint_as_float((uint32_t)u[c]);
-          if (u[c] >> 32 == CARRY_AGG) p.A[c] = __uint_as_float((uint32_t)f[c]);
+          if (u[c] >> 32 == agg) p.A[c] = __uint_as_float((uint32_t)f[c]);
         }
       }
       sh[at][lane] = p;
@@ -347,11 +351,49 @@ constexpr int64_t LOOK_ALL = 128;
 inline int64_t words_bytes(int64_t chunks, int64_t groups, int group) {
   return chunks > 1 ? 64 + chunks * groups * group * 16 : 0;
 }
-inline Words words_of(void* ws, int64_t groups, int64_t B) {
-  int look = 4;
-  while (look < LOOK && look * groups < LOOK_ALL) look *= 2;
-  return {(uint32_t*)ws, (unsigned long long*)((char*)ws + 64), (uint32_t)groups, (uint32_t)(groups / B), look};
-}
+// The words of a launch of chunks x groups workgroups, held until it is enqueued: of the
+// stream's scratch, whose words of earlier launches carry other epochs, or of a workspace that
+// is cleared first (a launch and a wait, 4 us) where the stream is capturing or the words
+// pass SCRATCH_MOST bytes, which the scratch would keep.
+constexpr int64_t SCRATCH_MOST = (int64_t)16 << 20;
+struct LaunchWords {
+  Words k = {};
+  ScratchSession scratch;
+  norm::Partials own;
+  bool shared = false;
+  explicit LaunchWords(hipStream_t s) : own(s) {}
+  int get(void* ws, size_t have, int64_t chunks, int64_t groups, int group, int64_t B, hipStream_t s,
+          const char* what) {
+    k.groups = (uint32_t)groups;
+    k.per = (uint32_t)(groups / B);
+    k.look = 4;
+    while (k.look < LOOK && k.look * groups < LOOK_ALL) k.look *= 2;
+    if (chunks <= 1) return SW_OK;
+    const int64_t bytes = words_bytes(chunks, groups, group);
+    int st;
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    if (bytes <= SCRATCH_MOST && hipStreamIsCapturing(s, &cs) == hipSuccess &&
+        cs == hipStreamCaptureStatusNone) {
+      if ((st = scratch.reserve((size_t)(bytes - 64) / 8, (uint32_t)(chunks * groups), s)) != SW_OK) return st;
+      shared = true;
+      k.ticket = scratch.ticket;
+      k.w = scratch.carry;
+      k.base = scratch.ticket_base;
+      k.epoch = scratch.epoch;
+      return SW_OK;
+    }
+    if ((st = own.get(ws, have, (size_t)bytes, what)) != SW_OK) return st;
+    k.ticket = (uint32_t*)own.p;
+    k.w = (unsigned long long*)((char*)own.p + 64);
+    k.epoch = 1;
+    return zero_words(k.ticket, (size_t)bytes / 4, s);
+  }
+  // after the launch
+  int done(int st) {
+    if (st != SW_OK && shared) scratch.invalidate();
+    return st;
+  }
+};
 // The mode of a walk of `steps` a chunk, `n` channels a lane, over these rows and dense results.
 inline Mode mode_of(const GatedArgs& a, int steps, int n, std::initializer_list<const StepRows*> rows,
                     std::initializer_list<const void*> outs) {
@@ -368,7 +410,7 @@ inline Mode mode_of(const GatedArgs& a, int steps, int n, std::initializer_list<
 }
 
 int64_t fwd_words(const GatedArgs& a);
-int run_fwd(const GatedArgs& a, void* words, hipStream_t s);
+int run_fwd(const GatedArgs& a, void* ws, size_t ws_bytes, hipStream_t s);
 
 }  // namespace gated
 }  // namespace sw

@@ -282,11 +282,15 @@ int lanes_of(int64_t K, int64_t R) {
   return lph;  // at most 32: 256 columns are 16 lanes, and one more where R is cut
 }
 
-// Places of a token that work side by side: as few as fill the card, since each
-// forms the token's angles again, and no more than there are heads.
+// Places of a token that work side by side: enough for 1024 lanes a compute unit, but of
+// three heads each at least, over which a lane's weights and angles serve (two places of 16384
+// tokens of 24 heads of 128 bf16 41 us, one 46; of 2048 tokens of 20 + 4 heads four 18 us
+// backward, eight 20, sixteen 24); and of fewer where the card would lie idle, in decoding.
 int places_of(int64_t T, int64_t heads, int lph, int cus) {
   int per = 1;
-  while (per < heads && per * lph < 256 && T * per * lph < (int64_t)cus * 1024) per *= 2;
+  while (per < heads && per * lph < 256 && T * per * lph < (int64_t)cus * 1024 &&
+         (per * 6 <= heads || T * per * lph < (int64_t)cus * 128))
+    per *= 2;
   return per;
 }
 

@@ -388,3 +388,32 @@ def test_refusals(sw):
     with pytest.raises(sw.ScanWeaverError) as e:
         sw.gated_scan_fwd(x, r, i, lam, h=x)
     assert e.value.status == 1 and "overlap" in str(e.value)
+
+
+def test_beside_other_operators_of_the_stream(sw):
+    """Calls of every size, growing and shrinking, in turn with the selective and the bare
+    scan's chained rows on one stream, and on another: the bits of a call alone."""
+    sizes = [(1, 700, 70), (2, 5000, 64), (1, 300, 200), (1, 20000, 300), (1, 257, 1)]
+    cases = [_make(50 + j, *s, "bf16")[0] for j, s in enumerate(sizes)]
+    args = [[t[n] for n in ("x", "r", "i", "lam")] for t in cases]
+    # 8-lane kernels that chain their own chunks: N = 3
+    x, dl = (torch.randn(1, 6, 9000, device="cuda") for _ in range(2))
+    A, Bm = -torch.rand(6, 3, device="cuda"), torch.randn(1, 9000, 3, device="cuda")
+    dl = torch.nn.functional.softplus(dl)
+    bare = torch.rand(1, 2, 100000, device="cuda")
+    others = lambda: (sw.selective_scan_fwd(x, dl, A, Bm, Bm)[0], sw.affine_scan(bare, bare))  # noqa: E731
+    want = [(sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])["dx"]) for a, t in zip(args, cases)]
+    alone = others()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        got, beside = [], []
+        for a, t in zip(args, cases):
+            got.append((sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])["dx"]))
+            beside.append(others())
+            with torch.cuda.stream(side):
+                got.append((sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])["dx"]))
+        torch.cuda.synchronize()
+        for k, pair in enumerate(got):
+            assert all(torch.equal(p, q) for p, q in zip(pair, want[k // 2])), k
+        assert all(torch.allclose(p, q) for one in beside for p, q in zip(one, alone))
