@@ -267,7 +267,10 @@ int gated_scan_fwd(const GatedArgs& a) {
 
 int gated_scan_step(const GatedStepArgs& a) {
   const hipStream_t s = current_stream();
-  const dim3 grid((unsigned)((a.D + 255) / 256), (unsigned)(a.B < 65535 ? a.B : 65535));
+  const int64_t cols = (a.D + 255) / 256;
+  int64_t rows = SW_MAX_WGS / cols;  // the kernel steps through the others
+  rows = a.B < rows ? a.B : rows;
+  const dim3 grid((unsigned)cols, (unsigned)(rows < 65535 ? rows : 65535));
   if (a.bf16)
     hipLaunchKernelGGL(step_kernel<uint16_t>, grid, dim3(256), 0, s, a);
   else

@@ -194,6 +194,33 @@ def test_offsets_past_32_bits(sw):
     assert (g[1:V - 2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tables_and_workspaces_off_16_bytes(sw, dtype):
+    """Through the C ABI: a gradient at any address of its type's alignment, its neighbours
+    untouched; a workspace too small is refused."""
+    from paper_2606_00601_amd._bind import _on
+    dt, code = TYPES[dtype], 0 if dtype == "f32" else 1
+    f = sw.fast()
+    for V, D, off in ((1, 1, 1), (3, 2, 1), (5, 7, 3), (40, 24, 5), (300, 33, 7)):
+        tok = torch.randint(0, V, (50,), device="cuda")
+        dy = torch.randn(50, D, device="cuda").to(dt)
+        want = sw.embedding_bwd(tok, dy, V)
+        buf = torch.full((V * D + 32,), 7.0, device="cuda", dtype=dt)
+        out = buf[off:off + V * D]
+        n = f.sw_embedding_bwd_workspace(50, V, D)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        with _on(tok.device):
+            args = (tok.data_ptr(), dy.data_ptr(), out.data_ptr(), 50, V, D, D, code, code, 1, 1.0)
+            assert f.sw_embedding_bwd(*args, ws.data_ptr(), n - 1) == 1
+            assert f.sw_embedding_bwd(*args, ws.data_ptr(), n) == 0
+        assert torch.equal(out.view(V, D), want)
+        assert (buf[:off] == 7.0).all() and (buf[off + V * D:] == 7.0).all()
+        with _on(tok.device):  # from the pool
+            out.fill_(7.0)
+            assert f.sw_embedding_bwd(*args, None, 0) == 0
+        assert torch.equal(out.view(V, D), want)
+
+
 def test_refusals(sw):
     table = torch.randn(9, 16, device="cuda")
     tok = torch.zeros(4, dtype=torch.int64, device="cuda")

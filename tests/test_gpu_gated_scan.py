@@ -356,6 +356,55 @@ def test_offsets_past_32_bits(sw):
     assert all(torch.equal(a[n], b[n]) for n in a)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_results_off_16_bytes_and_through_the_pool(sw, dtype):
+    """h at an address of its type's alignment only; calls that bring no workspace."""
+    from paper_2606_00601_amd._bind import _on
+    t, _ = _make(41, 2, 700, 66, dtype)
+    args = [t[n] for n in ("x", "r", "i", "lam")]
+    want = sw.gated_scan_fwd(*args, h0=t["h0"])
+    n = 2 * 700 * 66
+    buf = torch.full((n + 8,), 7.0, device="cuda", dtype=TYPES[dtype])
+    h = buf[1:1 + n].view(2, 700, 66)
+    assert torch.equal(sw.gated_scan_fwd(*args, h0=t["h0"], h=h)[0], want[0])
+    assert (buf[:1] == 7.0).all() and (buf[1 + n:] == 7.0).all()
+    f, last = sw.fast(), torch.empty_like(want[1])
+    st = (700 * 66, 66) * 3
+    with _on(h.device):
+        assert f.sw_gated_scan_fwd(*(a.data_ptr() for a in args), t["h0"].data_ptr(), None, h.data_ptr(),
+                                   last.data_ptr(), None, 2, 700, 66, 2, st, int(dtype == "bf16"), 8.0, None,
+                                   0) == 0
+    assert torch.equal(h, want[0]) and torch.equal(last, want[1])
+    # only the last states
+    last.fill_(7.0)
+    with _on(h.device):
+        assert f.sw_gated_scan_fwd(*(a.data_ptr() for a in args), t["h0"].data_ptr(), None, None,
+                                   last.data_ptr(), None, 2, 700, 66, 2, st, int(dtype == "bf16"), 8.0, None,
+                                   0) == 0
+    assert torch.equal(last, want[1])
+
+
+def test_capture_needs_a_workspace(sw):
+    """Without one a call whose chunks pass words is refused while its stream captures, and
+    nothing is recorded for it."""
+    from paper_2606_00601_amd._bind import _on
+    t, _ = _make(43, 1, 900, 40, "f32")
+    h = torch.full((1, 900, 40), 7.0, device="cuda")
+    got = []
+    mark = torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mark.add_(1.0)
+        with _on(h.device):
+            got.append(sw.fast().sw_gated_scan_fwd(
+                *(t[n].data_ptr() for n in ("x", "r", "i", "lam")), None, None, h.data_ptr(), None, None, 1,
+                900, 40, 1, (36000, 40) * 3, 0, 8.0, None, 0))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert got == [2] and (h == 7.0).all() and (mark == 1.0).all()
+
+
 def test_refusals(sw):
     t, _ = _make(23, 2, 6, 8, "f32")
     x, r, i, lam, h0 = (t[n] for n in ("x", "r", "i", "lam", "h0"))
