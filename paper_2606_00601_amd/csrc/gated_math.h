@@ -21,17 +21,16 @@ constexpr float LOG2E = 1.4426950408889634f;
 // 1 / (1 + e^-v), and e = e^-v (infinite below -88).  fp32 inputs: the rounding of v
 // log2 e, which alone would cost 2^-24 |v| of e, is made up for; v is held where e is
 // 0 or infinite already, since an infinite one would make the correction NaN.
+__device__ __forceinline__ float exp_minus(float v) {
+  constexpr float REST = (float)(1.4426950408889634 - (double)LOG2E);
+  const float m = v != v ? v : -__builtin_amdgcn_fmed3f(v, -200.0f, 200.0f);
+  const float h = m * LOG2E;
+  const float r = __builtin_fmaf(m, REST, __builtin_fmaf(m, LOG2E, -h));
+  return __builtin_amdgcn_exp2f(h) * __builtin_fmaf(r, 0.6931471805599453f, 1.0f);
+}
 template <class E>
 __device__ __forceinline__ float sigmoid(float v, float& e) {
-  if constexpr (sizeof(E) == 2) {
-    e = __builtin_amdgcn_exp2f(-v * LOG2E);
-  } else {
-    constexpr float REST = (float)(1.4426950408889634 - (double)LOG2E);
-    const float m = v != v ? v : -__builtin_amdgcn_fmed3f(v, -200.0f, 200.0f);
-    const float h = m * LOG2E;
-    const float r = __builtin_fmaf(m, REST, __builtin_fmaf(m, LOG2E, -h));
-    e = __builtin_amdgcn_exp2f(h) * __builtin_fmaf(r, 0.6931471805599453f, 1.0f);
-  }
+  e = sizeof(E) == 2 ? __builtin_amdgcn_exp2f(-v * LOG2E) : exp_minus(v);
   return __builtin_amdgcn_rcpf(1.0f + e);
 }
 // 1 minus it, e s, which keeps its digits where s nears 1.  (An infinite e leaves 1; so does
@@ -59,17 +58,26 @@ __device__ __forceinline__ float one_minus_square(float m, float a) {
   }
 }
 
-// c softplus(lam).
+// softplus(lam) = max(lam, 0) + log(1 + e), e = e^-|lam|, to a few units of 2^-24: with w = 1 + e
+// as rounded, log(1 + e) = log(w) e / (w - 1).  (The library's functions took some 200
+// instructions of the first wave, which the others wait for.)
+__device__ __forceinline__ float softplus(float lam, float& e) {
+  e = exp_minus(fabsf(lam));
+  const float w = 1.0f + e;
+  const float l = __builtin_amdgcn_logf(w) * 0.6931471805599453f * (e * __builtin_amdgcn_rcpf(w - 1.0f));
+  return fmaxf(lam, 0.0f) + (w == 1.0f ? e : l);
+}
 __device__ __forceinline__ float rate_of(float lam, float c) {
-  return c * (fmaxf(lam, 0.0f) + log1pf(expf(-fabsf(lam))));
+  float e;
+  return c * softplus(lam, e);
 }
 // sigmoid(lam) / softplus(lam), which tends to 1 for lam -> -inf: below -16 it differs by
 // e^lam / 2 < 2^-24.
 __device__ __forceinline__ float rate_slope(float lam) {
-  if (lam < -16.0f) return 1.0f;
-  const float e = expf(-fabsf(lam));
-  const float s = lam > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
-  return s / (fmaxf(lam, 0.0f) + log1pf(e));
+  float e;
+  const float p = softplus(lam, e);
+  const float s = (lam > 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(1.0f + e);
+  return lam < -16.0f ? 1.0f : s * __builtin_amdgcn_rcpf(p);
 }
 
 // A step's pair (a, u).
