@@ -621,8 +621,11 @@ int sw_gated_norm_bwd(const void* dy, const void* x, const void* z, const float*
  *
  * workspace: 16-byte aligned, at least sw_gated_scan_fwd_workspace bytes, that nothing
  * else uses until the call completes, or NULL: from the device's stream-ordered
- * pool for the call (no capture then).  Results do not depend on it; every call
- * of the same inputs gives the same bits.
+ * pool for the call (no capture then).  The words that chunks of a row hand on lie
+ * there; a call whose words take at most 16 MiB keeps them in the per-stream scratch
+ * instead, which spares a launch that clears them, except while its stream is
+ * capturing.  Rows of at most 256 steps need none.  Results depend on neither; every
+ * call of the same inputs gives the same bits.
  */
 enum { SW_GATED_CKPT = 64 };
 int sw_gated_scan_fwd(const void* x, const void* r, const void* i, const float* lam,

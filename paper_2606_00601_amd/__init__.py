@@ -35,6 +35,15 @@ C ABI one function per entry point; ``lib()`` is the same ABI through ctypes.
 * ``residual_norm_fwd(x, weight, residual, ...)`` and ``gated_norm_fwd(x, z,
   weight, ...)``: the norms before and after a block, fused with the residual
   addition and its scale and with the block's gate; ``_bwd`` and ``_fn`` as above.
+* ``gated_scan_fwd(x, r, i, lam, ...)``: a gated linear recurrence for each channel
+  (``a = exp(-c softplus(lam) sigmoid(r))``, ``h = a h + sqrt(1 - a^2) sigmoid(i)
+  x``), batches or packed sequences, returning ``(h, h_last)``; ``gated_scan_bwd`` /
+  ``gated_scan_fn`` are its gradients and the autograd function,
+  ``gated_scan_step(x, r, i, lam, state)`` one token of each sequence in place.
+* ``head_norm_fwd(q, k, weight_q, weight_k, positions=..., inv_freq=...)``: the norm
+  of each head's query and key with the rotation by the token's position;
+  ``embedding_fwd(tokens, table, scale=...)``: the scaled rows of a table, and
+  its gradient in a fixed order; ``_bwd`` and ``_fn`` as above.
 * ``selective_scan_plan(B, D, N, L, ...)``: the kernels, segments and form
   the fused forward would take for those sizes, without launching anything.
 """

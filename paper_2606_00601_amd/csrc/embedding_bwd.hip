@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void count_kernel(EmbedArgs a, Sort s, Clear z
 // workgroups, in earlier waves and in earlier lanes.
 __global__ __launch_bounds__(256) void place_kernel(EmbedArgs a, Sort s, Clear z) {
   if ((int)blockIdx.x >= s.tiles) return clear(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
-  __shared__ uint32_t base[MAX_BINS], wave_n[4][MAX_BINS], sums[256];
+  __shared__ uint32_t base[MAX_BINS], wave_n[4][MAX_BINS], sums[4];
   const int bins = 1 << s.bits, tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   // thread tid's bins are next to each other: their totals, then a scan over the threads
   const int per = bins > 256 ? bins / 256 : 1;
@@ -79,15 +79,15 @@ __global__ __launch_bounds__(256) void place_kernel(EmbedArgs a, Sort s, Clear z
   for (int k0 = 0; k0 < per; k0 += 2) {
     uint32_t total[2] = {}, before[2] = {};
     const int d = tid * per + k0;
-    for (int q = 0; q < s.tiles; q += 16) {  // 32 counts in flight
-      uint32_t n[16][2];
+    for (int q = 0; q < s.tiles; q += 32) {  // 64 counts in flight
+      uint32_t n[32][2];
 #pragma unroll
-      for (int u = 0; u < 16; ++u)
+      for (int u = 0; u < 32; ++u)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           n[u][k] = q + u < s.tiles && k0 + k < per && d + k < bins ? s.hist[(int64_t)(q + u) * bins + d + k] : 0;
 #pragma unroll
-      for (int u = 0; u < 16; ++u)
+      for (int u = 0; u < 32; ++u)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           total[k] += n[u][k];
@@ -101,15 +101,16 @@ __global__ __launch_bounds__(256) void place_kernel(EmbedArgs a, Sort s, Clear z
         mine += total[k];
       }
   }
-  sums[tid] = mine;
-  __syncthreads();
-  for (int d = 1; d < 256; d *= 2) {
-    const uint32_t n = tid >= d ? sums[tid - d] : 0;
-    __syncthreads();
-    sums[tid] += n;
-    __syncthreads();
+  uint32_t upto = mine;  // of the wave's threads up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t n = __shfl_up(upto, d);
+    upto += lane >= d ? n : 0;
   }
-  for (int d = tid * per; d < (tid + 1) * per && d < bins; ++d) base[d] += sums[tid] - mine;
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) upto += sums[w];
+  for (int d = tid * per; d < (tid + 1) * per && d < bins; ++d) base[d] += upto - mine;
 
   const int64_t t0 = blockIdx.x * s.tile, t1 = t0 + s.tile < a.T ? t0 + s.tile : a.T;
   for (int64_t u = t0; u < t1; u += TILE) {
