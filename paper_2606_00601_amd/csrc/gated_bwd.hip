@@ -5,6 +5,13 @@
 // other way, over v_t = a_t g_t, what step t hands to the one before it:
 //   v_t = a_t (dh_t + v_{t+1}),
 // an affine pair again, composed in slots and between workgroups from the last chunk on.
+//
+// Seven values are moved for each, against some 84 vector instructions: B=8 L=2048 D=1536
+// bf16 107 us, 353 MB at 3.3 TB/s with vector issue in 62% of the busy cycles; fp32, packed,
+// 11003 x 2048 144 us, 631 MB at 4.4 TB/s.  A lane's 8 values of one channel take 126
+// registers.  Tried at the first shape, with the same waits: two channels and 4 steps a lane
+// 117 us for 114 in all, two and 8 steps with values aside in LDS 127 (15 registers spilled),
+// six waves a SIMD on 80 registers 118 (7 spilled; fp32 155 for 151).
 #include "gated_walk.h"
 
 namespace sw {
@@ -143,7 +150,9 @@ __global__ __launch_bounds__(THREADS, 4) void bwd_kernel(GatedArgs a, const floa
   }
   if (chunks > 1) {
     look_back<G>(k, turn, group, slot, lane, &tail, sh, &in);
-    if (publishes && !end) carry_put(w, carry_status(k.epoch, CARRY_INC), __float_as_uint(__builtin_fmaf(all.A[0], in, all.U[0])));
+    if (publishes && !end)
+      carry_put(w, carry_status(k.epoch, CARRY_INC),
+                __float_as_uint(__builtin_fmaf(all.A[0], in, all.U[0])));
   }
 
   Rows<E, MODE, 1> dx, dr, di;

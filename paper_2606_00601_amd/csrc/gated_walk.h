@@ -7,8 +7,8 @@
 //
 // Between workgroups: a chunk publishes its own pair as soon as it has it (AGG), and the
 // state at its end once it knows it (INC), as 64-bit words of a status and a value.  To find
-// its incoming state a workgroup looks at the 16 chunks before it at once until one of them
-// has its end's state.  Chunks are handed out in their order by a ticket, a chunk publishes
+// its incoming state a workgroup looks at the 4 to 16 chunks before it at once until one of
+// them has its end's state.  Chunks are handed out in their order by a ticket, a chunk publishes
 // AGG without waiting, and the first knows its end, so every wait ends.
 #pragma once
 
@@ -196,7 +196,7 @@ __device__ __forceinline__ float apply(float A, float U, float v) {
   return PACKED && A < 0.0f ? U : r;
 }
 
-// The composition of the first n of 8 pairs in LDS, from the last one back if `turned`.
+// The composition of the first n of 8 pairs in LDS, from the last one back if TURNED.
 template <bool PACKED, bool TURNED, int DEPTH, int N, int LANES>
 __device__ __forceinline__ Pairs<N> first_of(const Pairs<N> (*sh)[LANES], int n, int lane) {
   Pairs<N> p = identity<N>();
@@ -347,10 +347,12 @@ inline int64_t groups_of(const GatedArgs& a, int group) { return a.B * ((a.D + g
 // to 16 where that leaves fewer than 128 for all groups.  (B=1 L=65536 D=256 forward 189, 127,
 // 96 us at 4, 8, 16 chunks; B=1 L=65536 D=5120 569, 581, 618.)
 constexpr int64_t LOOK_ALL = 128;
+
 // Bytes of the words of a walk, its ticket before them.
 inline int64_t words_bytes(int64_t chunks, int64_t groups, int group) {
   return chunks > 1 ? 64 + chunks * groups * group * 16 : 0;
 }
+
 // The words of a launch of chunks x groups workgroups, held until it is enqueued: of the
 // stream's scratch, whose words of earlier launches carry other epochs, or of a workspace that
 // is cleared first (a launch and a wait, 4 us) where the stream is capturing or the words
@@ -394,6 +396,7 @@ struct LaunchWords {
     return st;
   }
 };
+
 // The mode of a walk of `steps` a chunk, `n` channels a lane, over these rows and dense results.
 inline Mode mode_of(const GatedArgs& a, int steps, int n, std::initializer_list<const StepRows*> rows,
                     std::initializer_list<const void*> outs) {
