@@ -342,6 +342,37 @@ def test_streams(sw):
             assert torch.equal(h, wh) and all(torch.equal(g[n], wg[n]) for n in g)
 
 
+@pytest.mark.parametrize("shared", [False, True])
+def test_two_threads(sw, shared):
+    """Two host threads at once, on streams of their own and on one of both."""
+    import threading
+    cases = [_make(40 + j, 1, 3000 + 700 * j, 72, "f32")[0] for j in range(2)]
+    args = [[t[n] for n in ("x", "r", "i", "lam")] for t in cases]
+    want = [(sw.gated_scan_fwd(*a)[0], sw.gated_scan_bwd(*a, t["dh"])) for a, t in zip(args, cases)]
+    torch.cuda.synchronize()
+    both, errors = torch.cuda.Stream(), []
+
+    def worker(j):
+        try:
+            stream = both if shared else torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    h = sw.gated_scan_fwd(*args[j])[0]
+                    g = sw.gated_scan_bwd(*args[j], cases[j]["dh"])
+                    stream.synchronize()
+                    if not torch.equal(h, want[j][0]) or not all(torch.equal(g[n], want[j][1][n]) for n in g):
+                        errors.append(f"thread {j} differs")
+        except Exception as e:  # reported below
+            errors.append(f"thread {j}: {e!r}")
+
+    threads = [threading.Thread(target=worker, args=(j,)) for j in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(timeout=60)
+    assert not any(t.is_alive() for t in threads) and not errors, errors
+
+
 def test_offsets_past_32_bits(sw):
     """Rows that lie 2^31 elements and more apart."""
     L, D, step = 3, 8, 2 ** 30 + 5

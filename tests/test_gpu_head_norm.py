@@ -281,6 +281,53 @@ def test_graphs_and_no_tokens(sw):
     assert (g["dweight_q"] == 0).all() and (g["dweight_k"] == 0).all()
 
 
+def test_streams(sw):
+    """Calls on several streams at once give the bits of calls one after the other."""
+    t, _, pos = _make(17, 2, 700, 6, 2, 64, "bf16", 500)
+    how = dict(positions=pos.cuda(), inv_freq=_freq(64).cuda())
+
+    def work():
+        y = sw.head_norm_fwd(t["q"], t["k"], t["wq"], t["wk"], **how)
+        return [*y, *sw.head_norm_bwd(*y, t["q"], t["k"], t["wq"], t["wk"], **how).values()]
+
+    want = work()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        got = []
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(work())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for one in got for a, b in zip(one, want))
+
+
+def test_offsets_past_32_bits(sw):
+    """Results whose elements pass 2^32, of one token read again and again; tokens that lie
+    2^31 elements and more apart."""
+    L, H, K = 2 ** 21 + 3, 16, 130
+    one = torch.randn(1, 1, H, K, device="cuda").bfloat16()
+    q, k = one.expand(1, L, H, K), one[:, :, :1].expand(1, L, 1, K)
+    f = _freq(128).cuda()
+    pos = torch.arange(L, device="cuda")[None]
+    y, _ = sw.head_norm_fwd(q, k, inv_freq=f)
+    last = dict(positions=pos[:, -5:], inv_freq=f)
+    assert torch.equal(y[:, -5:], sw.head_norm_fwd(q[:, -5:], k[:, -5:], **last)[0])
+    del y
+    g = sw.head_norm_bwd(q, k, q, k, inv_freq=f, want_dweight=False)["dq"]
+    assert torch.equal(g[:, -5:], sw.head_norm_bwd(q[:, -5:], k[:, -5:], q[:, -5:], k[:, -5:], **last)["dq"])
+    del g
+    step = 2 ** 30 + 8
+    big = torch.zeros(2 * step + H * K, dtype=torch.bfloat16, device="cuda")
+    far = big.as_strided((1, 3, H, K), (0, step, K, 1))
+    far.copy_(torch.randn(1, 3, H, K, device="cuda").bfloat16())
+    near, k = far.contiguous(), one[:, :, :1].expand(1, 3, 1, K)
+    assert all(torch.equal(a, b) for a, b in zip(sw.head_norm_fwd(far, k, inv_freq=f),
+                                                 sw.head_norm_fwd(near, k, inv_freq=f)))
+    a, b = (sw.head_norm_bwd(x, k, x, k, inv_freq=f) for x in (far, near))
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
 def test_refusals(sw):
     t, _, pos = _make(15, 2, 4, 2, 2, 16, "f32")
     q, k, f = t["q"], t["k"], _freq(16).cuda()
