@@ -1,11 +1,11 @@
 // embedding_bwd.hip -- the gradient of an embedding's table: dtable[v] = scale * sum of
 // dy_t over the t whose token is v.
 //
-// The steps are sorted by token, stably (a radix sort of (token, t), 11 bits a pass at most),
-// so that a row's terms lie next to each other in the order of t; then every wave adds a
-// piece of P sorted steps in fp32 and writes the rows that lie in it whole.  A row that
-// crosses pieces leaves partial sums, which a last launch adds in order.  No atomics on
-// sums: the same call gives the same bits.
+// The steps are sorted by token, stably (few by counting, in one launch; many by a radix sort
+// of (token, t), 11 bits a pass at most), so that a row's terms lie next to each other in the
+// order of t; then every wave adds a piece of P sorted steps in fp32 and writes the rows that
+// lie in it whole.  A row that crosses pieces leaves partial sums, which a last launch adds in
+// order.  No atomics on sums: the same call gives the same bits.
 //
 // Bound by memory: dy is read once, the whole table written once.  The sort moves 8 bytes a
 // step and waits on itself, so its launches carry the table's zeros beside it.
@@ -36,7 +36,7 @@ struct Clear {
   int nhead, ntail;
 };
 __device__ __forceinline__ void clear(const Clear& z, int64_t wg, int64_t wgs) {
-  for (int64_t j = z.first + wg * 256 + threadIdx.x; j < z.end; j += wgs * 256)
+  for (int64_t j = z.first + wg * blockDim.x + threadIdx.x; j < z.end; j += wgs * blockDim.x)
     z.words[j] = make_uint4(0, 0, 0, 0);
   if (wg == 0 && (int)threadIdx.x < z.nhead) z.head[threadIdx.x] = 0;
   if (wg == 0 && (int)threadIdx.x < z.ntail) z.tail[threadIdx.x] = 0;
@@ -51,6 +51,59 @@ struct Sort {
 
 __device__ __forceinline__ Entry entry_at(const EmbedArgs& a, const Sort& s, int64_t t) {
   return s.in ? s.in[t] : Entry{row_of(a, t), (uint32_t)t};
+}
+
+// The sort of a few steps in one launch: a step's place is how many steps come before it,
+// those of lower rows and the earlier ones of its own.  A workgroup holds all rows in LDS and
+// places 64 steps, a lane each; its waves count over a share of the rows each.  T^2 compares,
+// so only up to RANK_MOST steps for each pass of the radix sort that it spares.  (The whole
+// gradient at D=256 with this sort and with the other: V=256, one pass, T=600 15 us and 19,
+// 2000 17 and 20, 4096 21 and 20; V=20000, two passes, 600 15 and 29, 8192 33 and 34, 16384 54
+// and 39.)
+constexpr int RANK_MOST = 4096, RANK_WAVES = 8;
+__global__ __launch_bounds__(RANK_WAVES * 64) void rank_kernel(EmbedArgs a, Entry* out, int share, int wgs,
+                                                               Clear z) {
+  if ((int)blockIdx.x >= wgs) return clear(z, blockIdx.x - wgs, gridDim.x - wgs);
+  extern __shared__ uint4 rows4[];  // RANK_WAVES * share rows, those behind the last above every row
+  __shared__ uint32_t counts[RANK_WAVES][64];
+  uint32_t* rows = (uint32_t*)rows4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
+  for (int j = tid; j < RANK_WAVES * share; j += RANK_WAVES * 64 * 8) {
+    uint32_t r[8];  // loads in flight
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int at = j + u * RANK_WAVES * 64;
+      r[u] = row_of(a, at < a.T ? at : a.T - 1);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int at = j + u * RANK_WAVES * 64;
+      if (at < RANK_WAVES * share) rows[at] = at < a.T ? r[u] : ~0u;
+    }
+  }
+  __syncthreads();
+  const int t0 = blockIdx.x * 64, t = t0 + lane, first = wave * share, end = first + share;
+  const uint32_t mine = t < a.T ? rows[t] : 0;
+  uint32_t n = 0;
+  const auto below = [&](int from, int to, uint32_t bound) {
+#pragma unroll 4
+    for (int j = from; j < to; j += 4) {
+      const uint4 r = rows4[j / 4];
+      n += (r.x < bound) + (r.y < bound) + (r.z < bound) + (r.w < bound);
+    }
+  };
+  const int mid = min(max(t0, first), end), hi = min(max(t0 + 64, first), end);
+  below(first, mid, mine + 1);
+  for (int j = mid; j < hi; ++j) n += rows[j] < mine + (j < t);
+  below(hi, end, mine);
+  counts[wave][lane] = n;
+  __syncthreads();
+  if (wave == 0 && t < a.T) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int w = 0; w < RANK_WAVES; ++w) at += counts[w][lane];
+    out[at] = Entry{mine, (uint32_t)t};
+  }
 }
 
 // How many of a workgroup's steps have each digit.
@@ -322,10 +375,13 @@ Plan plan_of(int64_t T, int64_t V, int64_t D) {
   p.tile = (T + (int64_t)TILE * MAX_TILES - 1) / ((int64_t)TILE * MAX_TILES) * TILE;
   p.tiles = (int)((T + p.tile - 1) / p.tile);
   p.cols = (D + 511) / 512;
-  // 32 steps, or pieces for some 4096 waves.  (T=65536 V=256 D=512 fp32 69, 59, 57 us at 16, 32,
-  // 64 steps; T=131072 V=32000 D=256 95, 83, 87; T=7800 V=17000 D=5120 121, 117, 123.)
-  p.P = 32;
-  while (p.P < 256 && T * p.cols > (int64_t)p.P * 4096) p.P *= 2;
+  // 32 steps, or pieces for some 4096 waves; where those are fewer than 1024 waves, 16 or 8.
+  // (T=65536 V=256 D=512 fp32 69, 59, 57 us at 16, 32, 64 steps; T=131072 V=32000 D=256 95, 83, 87;
+  // T=7800 V=17000 D=5120 121, 117, 123; the whole gradient at V=256 D=256 at 8 and 32 steps T=600
+  // 19 and 26 us, 8192 20 and 25.)
+  p.P = 8;
+  while (p.P < 32 && T * p.cols > (int64_t)p.P * 1024) p.P *= 2;
+  while (p.P >= 32 && p.P < 256 && T * p.cols > (int64_t)p.P * 4096) p.P *= 2;
   p.pieces = (T + p.P - 1) / p.P;
   p.entries = align64(T * (int64_t)sizeof(Entry));
   p.hist = align64((int64_t)p.tiles << (p.bits + 2));
@@ -392,7 +448,8 @@ int embedding_bwd(const EmbedArgs& a) {
   Entry* buf[2] = {(Entry*)ws, (Entry*)(ws + p.entries)};
   uint32_t* hist = (uint32_t*)(ws + 2 * p.entries);
   float* part = (float*)(ws + 2 * p.entries + p.hist);
-  const int launches = 2 * p.passes;
+  const bool rank = a.T <= (int64_t)RANK_MOST * p.passes;
+  const int launches = rank ? 1 : 2 * p.passes;
   // each launch clears its share of the table beside its step of the sort
   const auto share = [&](int j) {
     Clear z = whole;
@@ -405,7 +462,14 @@ int embedding_bwd(const EmbedArgs& a) {
   wgs = wgs < 1 ? 1 : wgs > 8 * cus ? 8 * cus : wgs;
   const dim3 grid((unsigned)(p.tiles + wgs));
   const Entry* sorted = nullptr;
-  for (int j = 0; j < p.passes; ++j) {
+  if (rank) {
+    const int steps = (int)((a.T + 63) / 64), share = (int)((a.T + RANK_WAVES * 4 - 1) / (RANK_WAVES * 4)) * 4;
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)(steps + wgs)), dim3(RANK_WAVES * 64),
+                       (size_t)(RANK_WAVES * share) * 4, s, a, buf[0], share, steps, whole);
+    if ((st = check_launch("rank_kernel")) != SW_OK) return st;
+    sorted = buf[0];
+  }
+  for (int j = 0; j < (rank ? 0 : p.passes); ++j) {
     const Sort so = {j ? buf[(j + 1) % 2] : nullptr, buf[j % 2], hist, p.tile, p.tiles, j * p.bits, p.bits};
     hipLaunchKernelGGL(count_kernel, grid, dim3(256), 0, s, a, so, share(2 * j));
     if ((st = check_launch("count_kernel")) != SW_OK) return st;

@@ -80,7 +80,10 @@ def _check(sw, tokens, V, D, types, scale, wide):
     (1, 1, 1, "even"), (1, 50, 8, "even"), (2, 3, 7, "even"), (17, 5, 33, "zipf"), (64, 1000, 64, "even"),
     (300, 7, 65, "zipf"), (1000, 256, 128, "zipf"), (777, 5000, 96, "outside"), (2048, 100, 40, "one"),
     (2049, 3000, 24, "each"), (100, 40, 16, "none"), (5000, 70000, 16, "zipf"), (4097, 2, 256, "even"),
-    (3000, 300, 520, "zipf"), (40, 30, 2050, "even")])
+    (3000, 300, 520, "zipf"), (40, 30, 2050, "even"),
+    # the last and first sizes of the sorts in one launch and by digits
+    (63, 9, 8, "outside"), (65, 9, 8, "one"), (4096, 300, 24, "zipf"), (4097, 300, 24, "outside"),
+    (8191, 5000, 16, "outside"), (8192, 5000, 24, "one"), (8193, 5000, 24, "zipf")])
 def test_values_and_gradients(sw, T, V, D, kind, types):
     print("case embedding", T, V, D, kind, types, flush=True)
     _check(sw, _tokens(kind, T, V, T + V), V, D, types, [1.0, 0.37, -22.6][T % 3], T % 2 == 0)
