@@ -99,9 +99,11 @@ __device__ __forceinline__ void load_angles(const HeadNormArgs& a, const Lane& l
   }
 }
 
-// The lane's pairs turned by their angles, or back by them (sign -1).
+// The lane's pairs turned by their angles, or back by them (sign -1).  A lane of columns that
+// are not turned has none: a turn by nothing, p 1 - q 0, would hand on a q that is not finite.
 template <bool ADJ>
-__device__ __forceinline__ void turn(float* x, const Angles& g, float sign) {
+__device__ __forceinline__ void turn(const Lane& l, float* x, const Angles& g, float sign) {
+  if (l.pair < 0) return;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float& p = x[ADJ ? 2 * j : j];
@@ -158,7 +160,7 @@ __device__ __forceinline__ void fwd_heads(const HeadNormArgs& a, const Heads& x,
     const float inv = rsqrtf(sum[0] / (float)a.K + a.eps);
 #pragma unroll
     for (int j = 0; j < 16; ++j) v[j] *= inv * wt[j];
-    if (a.R) turn<ADJ>(v, g, 1.0f);
+    turn<ADJ>(l, v, g, 1.0f);
     store_head<VEC>(dst + h * a.K, l, v);
   }
 }
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(256, 4) void bwd_kernel(HeadNormArgs a, Side q, Sid
       float v[16], d[16];
       load_head<VEC>(src + h * s.x.sh, l, v);
       load_head<VEC>(up + h * s.dy.sh, l, d);
-      if (a.R) turn<ADJ>(d, g, -1.0f);
+      turn<ADJ>(l, d, g, -1.0f);
       float sum[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
