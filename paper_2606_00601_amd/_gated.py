@@ -141,8 +141,8 @@ class _GatedScanFn(torch.autograd.Function):
     """Autograd glue; no arithmetic happens here."""
 
     @staticmethod
-    def forward(ctx, x, r, i, lam, h0, cu_seqlens, c, want_h_last):
-        h, h_last, ckpt = _forward(x, r, i, lam, c, h0, cu_seqlens, None, want_h_last or None, True)
+    def forward(ctx, x, r, i, lam, h0, cu_seqlens, c, want_h_last, keep):
+        h, h_last, ckpt = _forward(x, r, i, lam, c, h0, cu_seqlens, None, want_h_last or None, keep)
         ctx.save_for_backward(x, r, i, lam, h0, cu_seqlens, ckpt)
         ctx.c = c
         ctx.set_materialize_grads(False)
@@ -160,7 +160,7 @@ class _GatedScanFn(torch.autograd.Function):
             dh_last = dh_last.contiguous().to(torch.float32)
         g = gated_scan_bwd(x, r, i, lam, dh, dh_last, c=ctx.c, h0=h0, cu_seqlens=cu,
                            want_dh0=h0 is not None and ctx.needs_input_grad[4], ckpt=ckpt)
-        grads = g["dx"], g["dr"], g["di"], g["dlam"], g.get("dh0"), None, None, None
+        grads = g["dx"], g["dr"], g["di"], g["dlam"], g.get("dh0"), None, None, None, None
         return _differentiable_once("gated_scan_fn", grads, (x, r, i, lam, h0, dh, dh_last))
 
 
@@ -168,7 +168,9 @@ def gated_scan_fn(x, r, i, lam, *, c=8.0, h0=None, cu_seqlens=None, return_last_
     """Differentiable gated recurrence: :func:`gated_scan_fwd` forward,
     :func:`gated_scan_bwd` backward through torch autograd.  With
     ``return_last_state`` returns ``(h, h_last)``, both differentiable."""
-    h, h_last = _GatedScanFn.apply(x, r, i, lam, h0, cu_seqlens, c, bool(return_last_state))
+    # states for the backward only where there can be one
+    keep = torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in (x, r, i, lam, h0))
+    h, h_last = _GatedScanFn.apply(x, r, i, lam, h0, cu_seqlens, c, bool(return_last_state), keep)
     return (h, h_last) if return_last_state else h
 
 
