@@ -39,7 +39,8 @@ int check_sizes(const GatedArgs& a) {
     return fail(SW_ERR_UNSUPPORTED, "L=%lld steps", (long long)a.L);
   if (a.D >= (int64_t)1 << 28) return fail(SW_ERR_UNSUPPORTED, "D=%lld channels", (long long)a.D);
   int64_t n;
-  // the largest workspace is 8 bytes a value beside states every 64 steps
+  // the largest workspace holds 24 bytes a channel for every 64 steps begun, of groups of 64
+  // channels: words of 16, a partial sum and a state
   if (!mul_ok(a.B, a.L + 1, &n) || !mul_ok(n, a.D + 64, &n) || !mul_ok(n, 32, &n) ||
       !mul_ok(a.nseq, a.D, &n) || !mul_ok(n, 16, &n))
     return fail(SW_ERR_UNSUPPORTED, "sizes overflow");

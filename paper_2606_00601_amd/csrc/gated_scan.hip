@@ -8,8 +8,8 @@ namespace {
 // A chunk of 16 S steps of 64 channels.  Between memory and vector issue, some 45 slots a value
 // of which the six transcendental instructions take 24: B=1 L=65536 D=5120 bf16 541 us, 2.68 GB
 // at 5.0 TB/s (a copy reaches 5.1); B=8 L=2048 D=1536, one and a half rounds of workgroups,
-// 54 us, 3.7 TB/s.  Looking back is a tenth of the latter (53 us without, 58 with it, of a
-// form that cleared its words).
+// 53 us, 3.8 TB/s, and 91 with a channel a load (D=1537).  Looking back is a fourteenth of the
+// latter shape (49 us without it) and a third at B=1 L=65536 D=256 (38 us without, 56 with).
 template <class E, Mode MODE, bool PACKED, int S>
 __global__ __launch_bounds__(THREADS, S == 16 ? 4 : 6) void fwd_kernel(GatedArgs a, Words k, int64_t chunks) {
   using G = FwdShape;
@@ -199,8 +199,8 @@ __global__ __launch_bounds__(256) void step_kernel(GatedStepArgs a) {
 
 }  // namespace
 
-// Steps of a lane: 8 where they hold the row.  (As two chunks for one of 16 they are slower at
-// every size: B=8 L=2048 D=1536 61 us for 59, B=1 L=65536 D=256 96 for 64.)
+// Steps of a lane: 8 where they hold the row.  (Two chunks for one of 16 are slower in bf16, B=8
+// L=2048 D=1536 65 us for 52, B=1 L=65536 D=256 108 for 57, and no faster in fp32, 91 for 90.)
 int fwd_s(const GatedArgs& a) { return a.L <= FwdShape::SLOTS * FWD_SHORT_S ? FWD_SHORT_S : FWD_S; }
 
 int64_t fwd_words(const GatedArgs& a) {

@@ -344,8 +344,9 @@ __device__ __forceinline__ void find_sequences(const GatedArgs& a, int64_t t0, S
 inline int64_t chunks_of(int64_t L, int steps) { return L > steps ? (L + steps - 1) / steps : 1; }
 inline int64_t groups_of(const GatedArgs& a, int group) { return a.B * ((a.D + group - 1) / group); }
 // Few groups have many chunks under way at once, so they look further back: 4 chunks, or up
-// to 16 where that leaves fewer than 128 for all groups.  (B=1 L=65536 D=256 forward 189, 127,
-// 96 us at 4, 8, 16 chunks; B=1 L=65536 D=5120 569, 581, 618.)
+// to 16 where that leaves fewer than 128 for all groups.  (bf16 at 4, 8, 16 chunks: B=1 L=65536
+// D=256 forward 95, 67, 56 us, backward 235, 148, 105; D=1024 134, 131, 134 and 322, 286, 307;
+// D=5120 forward 551, 563, 587; B=8 L=2048 D=1536 52, 53, 54 and 107, 106, 112.)
 constexpr int64_t LOOK_ALL = 128;
 
 // Bytes of the words of a walk, its ticket before them.

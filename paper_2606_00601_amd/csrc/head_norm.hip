@@ -166,7 +166,8 @@ __device__ __forceinline__ void fwd_heads(const HeadNormArgs& a, const Heads& x,
 }
 
 // Lanes: (token, one of `per` places of it, lane of the head); queries first, then keys.
-// 16384 tokens of 12 + 12 heads of 128, bf16: 41 us, 201 MB at 4.9 TB/s.
+// 16384 tokens of 12 + 12 heads of 128, bf16: 41 us, 201 MB at 4.9 TB/s; fp32 87 us, 4.6; heads
+// of 100, R = 50, an element a load, bf16 133 us, 157 MB at 1.2 TB/s.
 template <class E, int LPH, bool ADJ, bool VEC>
 __global__ __launch_bounds__(256) void fwd_kernel(HeadNormArgs a, int per) {
   extern __shared__ float2 angles[];
@@ -223,6 +224,7 @@ __device__ __forceinline__ void put_partial(const Lane& l, float* dw, float* lds
 }
 
 // dx = inv (w g - n mean(w g n)), n = x inv, with g the gradient turned back; dw += g n.
+// At the shape above 69 us, 302 MB at 4.4 TB/s; fp32 128 us, 4.7; heads of 100 181 us, 1.3.
 template <class E, int LPH, bool ADJ, bool VEC>
 __global__ __launch_bounds__(256, 4) void bwd_kernel(HeadNormArgs a, Side q, Side k) {
   extern __shared__ float2 angles[];
